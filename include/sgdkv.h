@@ -362,6 +362,162 @@ sgdkv_status sgdkv_decode_attention_noalloc(const sgdkv_decode_desc* desc, const
                                             void* stream);
 
 /* ------------------------------------------------------------------ */
+/* Paged per-head cache: several new tokens at a time (device).        */
+
+/* After compression every KV head of every sequence -- a segment, s = b*Hkv + h
+ * -- holds its own number of rows. Here the segments live in pages of one
+ * pool: row p of segment s is slot tables[s][p / P]*P + p % P, P = page_size.
+ * A serving step is sgdkv_page_update (pages and slots for the new rows),
+ * sgdkv_norm_rope_store (new queries, keys and values; the keys and values
+ * into their slots) and sgdkv_paged_attention; sgdkv_paged_store brings the
+ * rows of a compressed cache into their slots. Every length is read on the
+ * device, so a captured step replays with what they have become. The calls
+ * run on the current device, which the stream and all pointers belong to. */
+typedef struct sgdkv_page_pool {
+  void* k_pages;      /* device [num_pages][page_size][head_dim] dtype */
+  void* v_pages;      /* the same shape */
+  int64_t num_pages;  /* >= 1; num_pages * page_size <= 2^31 - 1 */
+  int32_t page_size;  /* a power of two, 16 to 1024 */
+  int32_t head_dim;   /* d: 64 or 128 */
+  int32_t dtype;      /* SGDKV_DTYPE_F32 or SGDKV_DTYPE_BF16 */
+  int32_t reserved;   /* must be 0 */
+} sgdkv_page_pool;
+
+/* Status values page_update writes on the device. */
+#define SGDKV_PAGES_OK 0
+#define SGDKV_PAGES_SHORT 1      /* the free stack holds too few pages */
+#define SGDKV_PAGES_ROWS 2       /* a segment's rows, before or after, do not fit its table */
+#define SGDKV_PAGES_STACK 3      /* head outside [0, num_free], or more given back than was taken */
+#define SGDKV_PAGES_SLOTS 4      /* more new rows than num_slots */
+
+typedef struct sgdkv_page_desc {
+  int32_t batch;         /* B >= 1 sequences */
+  int32_t num_kv_heads;  /* Hkv >= 1; B*Hkv <= 4096 */
+  int32_t page_size;     /* P: a power of two, 16 to 1024 */
+  int32_t max_pages;     /* columns of tables, >= 1; max_pages * P <= 2^31 - 1 */
+  int32_t by_segment;    /* 0: add and slots per sequence and token; 1: per segment */
+  int32_t reserved;      /* must be 0 */
+  int64_t num_free;      /* entries of free_pages, 1 to 2^31 - 1 */
+  int64_t num_slots;     /* rows of slots, >= 0 (times Hkv by token: <= 2^31 - 1) */
+} sgdkv_page_desc;
+
+/* Pages for the rows that segments gain or lose, and the slots of the new ones.
+ * rows:  device [B*Hkv] int32, each segment's rows now.
+ * add:   device int32, rows gained (negative: given up, from the end; never
+ *        below 0): [B], for all KV heads of a sequence, or [B*Hkv] (by_segment).
+ * tables: device [B*Hkv][max_pages] int32, updated in place: the entries of
+ *        the pages a segment gains. Entries past a segment's pages mean nothing.
+ * free_pages: device [num_free] int32, a stack of page numbers: entries from
+ *        head on are free, those before it were handed out. Pages given up go
+ *        back on it below head, in (segment, position) order; then each segment
+ *        takes its new pages from it, in that order.
+ * head:  device [1] int32.
+ * rows_out [B*Hkv], head_out [1]: rows and head afterwards; each may be the
+ *        input itself.
+ * cu_out: device int32, the new rows before each sequence [B+1] (by_segment:
+ *        before each segment [B*Hkv+1]): max(add, 0) summed up.
+ * slots: by token [num_slots][Hkv] int32, row t for token t of the step
+ *        (sequence by sequence); by_segment [num_slots], segment by segment,
+ *        the row order of a compressed cache. Rows behind the last new one
+ *        are -1, which the row-storing calls skip.
+ * status: device [1] int32, SGDKV_PAGES_*. Other than OK: tables, free_pages,
+ *        rows and head keep their values (rows_out and head_out get the old
+ *        ones), all slots are -1 and cu_out is all 0.
+ * Only rows_out and head_out may overlap other arguments.
+ * Errors (nothing enqueued): sizes out of range; more than 4096 segments
+ * (UNSUPPORTED); NULL or misaligned pointers (slots may be NULL with
+ * num_slots 0); reserved not 0. */
+sgdkv_status sgdkv_page_update(const sgdkv_page_desc* desc, const int32_t* rows, const int32_t* add, int32_t* tables,
+                               int32_t* free_pages, const int32_t* head, int32_t* rows_out, int32_t* head_out,
+                               int32_t* cu_out, int32_t* slots, int32_t* status, void* stream);
+
+/* Copies row i of k_rows and v_rows (device [n][d], the pool's dtype) to slot
+ * slots[i] (device [n] int32). A slot outside the pool, -1 say, keeps nothing.
+ * A slot given twice ends up with either row, or with pieces of both.
+ * Errors (nothing enqueued): a bad pool; n < 0 or n*d beyond 2^40; NULL or
+ * misaligned pointers (with n > 0). */
+sgdkv_status sgdkv_paged_store(const sgdkv_page_pool* pool, const void* k_rows, const void* v_rows,
+                               const int32_t* slots, int64_t n, void* stream);
+
+typedef struct sgdkv_norm_rope_desc {
+  int64_t num_tokens;    /* T >= 0 */
+  int32_t num_q_heads;   /* Hq >= 0 (0: keys and values only) */
+  int32_t num_kv_heads;  /* Hkv >= 1 */
+  int64_t q_stride;      /* elements from one token's heads to the next one's, */
+  int64_t k_stride;      /* >= heads * d and a multiple of 16 bytes: the parts */
+  int64_t v_stride;      /* of one fused projection's output can be passed */
+  int32_t rot_dim;       /* rotated elements per head: 0 to d, a multiple of 16 */
+  int32_t interleaved;   /* pairs (2i, 2i+1) instead of (i, i + rot_dim/2) */
+  float eps;             /* >= 0 */
+  int32_t reserved;      /* must be 0 */
+} sgdkv_norm_rope_desc;
+
+/* New tokens' heads in one pass: queries and keys normalised per head and
+ * rotated by their positions, queries to q_out, keys and values to their
+ * slots. Per head, in fp32 and rounded once at the end:
+ *   x <- x * weight / sqrt(mean(x^2) + eps)          (with a weight)
+ *   (a, b) <- (a cos t - b sin t, b cos t + a sin t)  t = position * inv_freq[i]
+ * for the pairs i < rot_dim/2; t is exact to 2^-31 turns whatever the position.
+ * Values are copied.
+ * q [T][Hq][d], k and v [T][Hkv][d]: device, the pool's dtype, strides above.
+ * positions: device [T] int32. slots: device [T][Hkv] int32; a slot outside
+ * the pool keeps nothing, one given twice ends up with either row or pieces
+ * of both. inv_freq: device [rot_dim/2] fp32. q_weight, k_weight: device [d],
+ * the pool's dtype, or NULL for no norm. q_out: device [T][Hq][d], dense; it
+ * may be q itself if that is dense too.
+ * Errors (nothing enqueued): a bad pool; sizes, strides or eps out of range;
+ * T*Hq or T*Hkv beyond 2^31 - 1; missing or misaligned pointers; reserved
+ * not 0. */
+sgdkv_status sgdkv_norm_rope_store(const sgdkv_page_pool* pool, const sgdkv_norm_rope_desc* desc, const void* q,
+                                   const void* k, const void* v, const int32_t* positions, const int32_t* slots,
+                                   const float* inv_freq, const void* q_weight, const void* k_weight, void* q_out,
+                                   void* stream);
+
+typedef struct sgdkv_paged_desc {
+  int32_t batch;         /* B >= 1 */
+  int32_t num_q_heads;   /* Hq */
+  int32_t num_kv_heads;  /* Hkv, Hq % Hkv == 0, at most 16 query heads per KV head */
+  int32_t out_dtype;     /* dtype of out */
+  int64_t num_tokens;    /* T >= 0: tokens of q, out and lse_out */
+  int32_t max_new;       /* >= 1: at least the longest sequence's new tokens */
+  int32_t max_pages;     /* columns of tables, >= 1 */
+  int32_t causal;        /* 1: a token sees the rows up to its own; 0: all of its segment's */
+  float scale;           /* logit scale; 0 selects 1/sqrt(head_dim) */
+} sgdkv_paged_desc;
+
+/* Bytes of device workspace for sgdkv_paged_attention. Depends on the pool's
+ * dtype and head_dim, the head counts and max_new (of the pool, the pages are
+ * not looked at); at most 70 MB. Nothing in it needs to persist; calls that
+ * may overlap in time, replays of captured ones included, need one each. */
+sgdkv_status sgdkv_paged_attention_workspace_size(const sgdkv_page_pool* pool, const sgdkv_paged_desc* desc,
+                                                  size_t* bytes);
+
+/* Attention of the new tokens over their segments' rows, their own included.
+ * Sequence b has the n tokens cu_new[b] .. cu_new[b+1]-1 of q; segment
+ * s = (b, h) has rows[s] rows, the last n of them the new tokens'. Token i,
+ * query head q of KV head h = q/G:
+ *   out = sum_r softmax_r(scale*<q, k_r>) v_r,  lse = log sum_r exp(scale*<q, k_r>)
+ * over the rows r <= rows[s] - n + i (causal) or all rows. A token that sees
+ * no row (rows[s] < n) gets out = 0 and lse = -inf. Rows past a segment's
+ * last one are not read into a result, whatever they hold.
+ * q: device [T][Hq][d], the pool's dtype. tables: device [B*Hkv][max_pages]
+ * int32; an entry in use that is not a page of the pool counts as a page of
+ * zero rows. rows: device [B*Hkv] int32, cu_new: device [B+1] int32 (both as
+ * sgdkv_page_update leaves them); they are cut to [0, max_pages*page_size] and
+ * [0, T]. out: device [T][Hq][d] out_dtype, lse_out: optional device [T][Hq]
+ * fp32; tokens in no sequence, and those past a sequence's first max_new,
+ * keep what these held.
+ * Probabilities are rounded to bf16 for bf16 out; for fp32 out of bf16 inputs
+ * they keep 16 bits.
+ * Errors (nothing enqueued): a bad pool; sizes out of range; Hq % Hkv; more
+ * than 16 query heads per KV head, 8192 query heads or 65535 segments
+ * (UNSUPPORTED); max_pages * page_size beyond 2^31 - 1; missing or misaligned
+ * pointers; small workspace (WORKSPACE). */
+sgdkv_status sgdkv_paged_attention(const sgdkv_page_pool* pool, const sgdkv_paged_desc* desc, const void* q,
+                                   const int32_t* tables, const int32_t* rows, const int32_t* cu_new, void* out,
+                                   float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------ */
 /* Kernel timing for benchmarks (not part of the method).             */
 
 /* While enabled (on != 0), every kernel the library launches is bracketed by

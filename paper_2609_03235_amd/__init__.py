@@ -10,6 +10,8 @@ Entry points (same names as the C ABI without the ``sgdkv_`` prefix):
   allocate_budgets, total_from_ratio, reduce_query_head_scores   (host)
   compress_workspace_size, compress_layer                        (device)
   decode_workspace_size, decode_attention                        (device)
+  page_update, paged_store, norm_rope_store                      (device)
+  paged_attention_workspace_size, paged_attention                (device)
 """
 from __future__ import annotations
 
@@ -29,7 +31,9 @@ SYMBOLS = ("sgdkv_last_error", "sgdkv_version", "sgdkv_reduce_query_head_scores"
            "sgdkv_compress_workspace_size",
            "sgdkv_compress_layer", "sgdkv_compress_layer_ex",
            "sgdkv_decode_workspace_size", "sgdkv_decode_attention", "sgdkv_decode_workspace_size_ex",
-           "sgdkv_decode_attention_ex", "sgdkv_decode_attention_noalloc", "sgdkv_append_kv", "sgdkv_profile_enable",
+           "sgdkv_decode_attention_ex", "sgdkv_decode_attention_noalloc", "sgdkv_append_kv", "sgdkv_page_update",
+           "sgdkv_paged_store", "sgdkv_norm_rope_store", "sgdkv_paged_attention_workspace_size",
+           "sgdkv_paged_attention", "sgdkv_profile_enable",
            "sgdkv_profile_reset", "sgdkv_profile_read")
 
 
@@ -94,6 +98,11 @@ def load_library():
         "sgdkv_decode_attention_ex": [P, P, P, P, P, P, P, P, P, P, ctypes.c_size_t, P],
         "sgdkv_decode_attention_noalloc": [P, P, P, P, P, P, P, P, P, P],
         "sgdkv_append_kv": [P, P, P, P, P, i64, i64, P],
+        "sgdkv_page_update": [P, P, P, P, P, P, P, P, P, P, P, P],
+        "sgdkv_paged_store": [P, P, P, P, i64, P],
+        "sgdkv_norm_rope_store": [P, P, P, P, P, P, P, P, P, P, P, P],
+        "sgdkv_paged_attention_workspace_size": [P, P, P],
+        "sgdkv_paged_attention": [P, P, P, P, P, P, P, P, P, ctypes.c_size_t, P],
         "sgdkv_profile_enable": [i32],
         "sgdkv_profile_reset": [],
         "sgdkv_profile_read": [i32, P, P, P, P],
@@ -337,6 +346,246 @@ def append_kv(q_like, k_step, v_step, k_new, v_new, slot: int, stream=None):
     desc = decode_desc(q_like, k_step.shape[1])
     _check(load_library().sgdkv_append_kv(ctypes.byref(desc), _ptr(k_step), _ptr(v_step), _ptr(k_new), _ptr(v_new),
                                           int(k_new.shape[2]), int(slot), _stream(stream)))
+
+
+# --------------------------------------------------------- paged cache
+class PagePool(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("num_pages", ctypes.c_int64),
+                ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class PageDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("by_segment", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("num_free", ctypes.c_int64), ("num_slots", ctypes.c_int64)]
+
+
+class NormRopeDesc(ctypes.Structure):
+    _fields_ = [("num_tokens", ctypes.c_int64), ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("reserved", ctypes.c_int32)]
+
+
+class PagedDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32), ("num_tokens", ctypes.c_int64), ("max_new", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("causal", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+PAGES_OK, PAGES_SHORT, PAGES_ROWS, PAGES_STACK, PAGES_SLOTS = range(5)
+
+
+class _on_stream:
+    """Makes the tensors' device current and `stream` (None: that device's current stream) torch's current
+    stream, so that what a call allocates belongs to the stream it is used on. Enters as the raw handle."""
+
+    def __init__(self, device, stream):
+        import torch
+        self.guards = [torch.cuda.device(device)]
+        if stream is not None:
+            if not hasattr(stream, "cuda_stream"):
+                stream = torch.cuda.ExternalStream(int(stream), device=device)
+            if stream.device != device:
+                raise SgdkvError(ERR_INVALID_ARG, f"the stream is on {stream.device}, the tensors on {device}")
+            self.guards.append(torch.cuda.stream(stream))
+
+    def __enter__(self):
+        import torch
+        for g in self.guards:
+            g.__enter__()
+        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+    def __exit__(self, *exc):
+        for g in reversed(self.guards):
+            g.__exit__(*exc)
+
+
+def _need(cond: bool, message: str):
+    if not cond:
+        raise SgdkvError(ERR_INVALID_ARG, message)
+
+
+def _need_same(device, **tensors):
+    """Every given tensor is on `device` (a GPU)."""
+    _need(device.type == "cuda", f"tensors must be on a GPU, not on {device}")
+    for name, t in tensors.items():
+        _need(t is None or t.device == device, f"{name} is on another device than {device}")
+
+
+def _need_int32(shape=None, **tensors):
+    import torch
+    for name, t in tensors.items():
+        _need(t.dtype == torch.int32, f"{name} must be int32, not {t.dtype}")
+        _need(t.is_contiguous(), f"{name} must be contiguous")
+        _need(shape is None or tuple(t.shape) == tuple(shape), f"{name} has shape {tuple(t.shape)}, not {shape}")
+
+
+def page_pool(k_pages, v_pages) -> PagePool:
+    """The descriptor of a pool k_pages, v_pages [num_pages, page_size, d]."""
+    _need(k_pages.dim() == 3 and k_pages.shape == v_pages.shape and k_pages.dtype == v_pages.dtype,
+          "k_pages and v_pages must be [num_pages, page_size, d] of one dtype")
+    _need(k_pages.is_contiguous() and v_pages.is_contiguous(), "k_pages and v_pages must be contiguous")
+    n, page, d = k_pages.shape
+    return PagePool(k_pages.data_ptr(), v_pages.data_ptr(), n, page, d, _dtype_code(k_pages), 0)
+
+
+def page_update(rows, add, tables, free_pages, head, *, page_size: int, n_slots: int, by_segment: bool = False,
+                rows_out=None, head_out=None, slots=None, cu=None, status=None, stream=None) -> dict:
+    """Pages and slots for the rows that segments gain or lose (sgdkv_page_update). rows [B * Hkv], tables
+    [B * Hkv, max_pages] (updated in place), free_pages [n] (a stack, updated in place) and head [1] are int32;
+    add is int32 [B], or [B * Hkv] with by_segment. Returns slots ([n_slots, Hkv] or [n_slots]), rows, head, cu,
+    status and the updated tables and free_pages. rows_out and head_out may be rows and head."""
+    import torch
+    dev = rows.device
+    _need_same(dev, add=add, tables=tables, free_pages=free_pages, head=head, rows_out=rows_out, head_out=head_out,
+               slots=slots, cu=cu, status=status)
+    _need(rows.dim() == 1 and add.dim() == 1 and tables.dim() == 2 and free_pages.dim() == 1,
+          "rows, add and free_pages must have one dimension and tables two")
+    S, n_add = rows.numel(), add.numel()
+    _need(S > 0 and tables.shape[0] == S, f"tables has {tables.shape[0]} rows for {S} segments")
+    _need(n_add == S if by_segment else n_add > 0 and S % n_add == 0, f"add holds {n_add} values for {S} segments")
+    B = 1 if by_segment else n_add
+    Hkv = S // B
+    n_slots = int(n_slots)
+    _need(n_slots >= 0, "n_slots must be >= 0")
+    _need_int32(rows=rows, add=add, tables=tables, free_pages=free_pages)
+    _need_int32((1,), head=head)
+    with _on_stream(dev, stream) as s:
+        new = lambda *shape: torch.empty(shape, dtype=torch.int32, device=dev)
+        rows_out = new(S) if rows_out is None else rows_out
+        head_out = new(1) if head_out is None else head_out
+        cu = new(n_add + 1) if cu is None else cu
+        status = new(1) if status is None else status
+        shape = (n_slots,) if by_segment else (n_slots, Hkv)
+        slots = new(*shape) if slots is None else slots
+        _need_int32((S,), rows_out=rows_out)
+        _need_int32((1,), head_out=head_out, status=status)
+        _need_int32((n_add + 1,), cu=cu)
+        _need_int32(shape, slots=slots)
+        desc = PageDesc(B, Hkv, int(page_size), tables.shape[1], int(bool(by_segment)), 0, free_pages.numel(), n_slots)
+        _check(load_library().sgdkv_page_update(
+            ctypes.byref(desc), _ptr(rows), _ptr(add), _ptr(tables), _ptr(free_pages), _ptr(head), _ptr(rows_out),
+            _ptr(head_out), _ptr(cu), _ptr(slots), _ptr(status), s))
+    return dict(slots=slots, rows=rows_out, head=head_out, cu=cu, status=status, tables=tables, free_pages=free_pages)
+
+
+def paged_store(k_rows, v_rows, slots, k_pages, v_pages, *, stream=None):
+    """Copy rows [n, d] to their slots (sgdkv_paged_store): slots int32 [n], -1 for none."""
+    dev = k_pages.device
+    _need_same(dev, v_pages=v_pages, k_rows=k_rows, v_rows=v_rows, slots=slots)
+    pool = page_pool(k_pages, v_pages)
+    _need(k_rows.dim() == 2 and k_rows.shape == v_rows.shape and k_rows.shape[1] == pool.head_dim
+          and k_rows.dtype == v_rows.dtype == k_pages.dtype, "k_rows and v_rows must be [n, d] of the pool's dtype")
+    n = k_rows.shape[0]
+    _need_int32((n,), slots=slots)
+    with _on_stream(dev, stream) as s:
+        _check(load_library().sgdkv_paged_store(ctypes.byref(pool), _ptr(k_rows), _ptr(v_rows), _ptr(slots), n, s))
+
+
+def _token_stride(t, name, heads, d):
+    """Elements between tokens of t [T, heads, d], whose heads must be dense."""
+    _need(heads == 0 or t.shape[0] == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == d)),
+          f"the heads of a token of {name} must be dense")
+    return t.stride(0) if t.shape[0] > 1 else heads * d
+
+
+def norm_rope_store(q, k, v, positions, slots, k_pages, v_pages, *, inv_freq=None, q_weight=None, k_weight=None,
+                    eps: float = 1e-6, interleaved: bool = False, q_out=None, stream=None):
+    """New tokens' heads in one pass (sgdkv_norm_rope_store): queries [T, Hq, d] and keys [T, Hkv, d] normalised per
+    head (with q_weight, k_weight [d]) and rotated by positions (int32 [T]) with inv_freq (fp32 [rot_dim / 2];
+    None: no rotation), keys and values stored to slots (int32 [T, Hkv], -1 for none). q, k and v may be parts of
+    one projection's output. q may be None. Returns q_out [T, Hq, d]."""
+    import torch
+    dev = k_pages.device
+    _need_same(dev, v_pages=v_pages, q=q, k=k, v=v, positions=positions, slots=slots, inv_freq=inv_freq,
+               q_weight=q_weight, k_weight=k_weight, q_out=q_out)
+    pool = page_pool(k_pages, v_pages)
+    dt, d = k_pages.dtype, pool.head_dim
+    _need(k.dim() == 3 and v.shape == k.shape and k.shape[2] == d and k.dtype == v.dtype == dt,
+          "k and v must be [T, Hkv, d] of the pool's dtype")
+    T, Hkv = k.shape[:2]
+    Hq = 0 if q is None else q.shape[1]
+    _need(q is None or (q.dim() == 3 and q.shape[0] == T and q.shape[2] == d and q.dtype == dt),
+          "q must be [T, Hq, d] of the pool's dtype")
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        _need(w is None or (tuple(w.shape) == (d,) and w.dtype == dt and w.is_contiguous()),
+              f"{name} must be [d] of the pool's dtype")
+    _need(inv_freq is None or (inv_freq.dim() == 1 and inv_freq.dtype == torch.float32 and inv_freq.is_contiguous()),
+          "inv_freq must be fp32 with one dimension")
+    _need_int32((T,), positions=positions)
+    _need_int32((T, Hkv), slots=slots)
+    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+    with _on_stream(dev, stream) as s:
+        if Hq and q_out is None:
+            q_out = torch.empty((T, Hq, d), dtype=dt, device=dev)
+        _need(not Hq or (tuple(q_out.shape) == (T, Hq, d) and q_out.dtype == dt and q_out.is_contiguous()),
+              "q_out must be a dense [T, Hq, d] of the pool's dtype")
+        desc = NormRopeDesc(T, Hq, Hkv, 0 if not Hq else _token_stride(q, "q", Hq, d), _token_stride(k, "k", Hkv, d),
+                            _token_stride(v, "v", Hkv, d), rot, int(bool(interleaved)), float(eps), 0)
+        _check(load_library().sgdkv_norm_rope_store(
+            ctypes.byref(pool), ctypes.byref(desc), q.data_ptr() if Hq else None, k.data_ptr(), v.data_ptr(),
+            _ptr(positions), _ptr(slots), _ptr(inv_freq), _ptr(q_weight), _ptr(k_weight),
+            _ptr(q_out) if Hq else None, s))
+    return q_out
+
+
+def _paged_desc(q, num_kv_heads, batch, max_new, max_pages, out_dtype, causal, scale) -> PagedDesc:
+    import torch
+    T, Hq, _ = q.shape
+    _need(out_dtype in (None, torch.bfloat16, torch.float32), f"out_dtype {out_dtype}")
+    od = _dtype_code(q) if out_dtype is None else (DTYPE_BF16 if out_dtype == torch.bfloat16 else DTYPE_F32)
+    return PagedDesc(int(batch), Hq, int(num_kv_heads), od, T, int(max_new), int(max_pages), int(bool(causal)),
+                     float(scale))
+
+
+def paged_attention_workspace_size(q, num_kv_heads: int, batch: int, *, max_new: int) -> int:
+    """Bytes of workspace of paged_attention for queries like q [T, Hq, d] and chunks of up to max_new tokens."""
+    pool = PagePool(None, None, 1, 16, q.shape[2], _dtype_code(q), 0)
+    desc = _paged_desc(q, num_kv_heads, batch, max_new, 1, None, True, 0.0)
+    n = ctypes.c_size_t(0)
+    _check(load_library().sgdkv_paged_attention_workspace_size(ctypes.byref(pool), ctypes.byref(desc),
+                                                                ctypes.byref(n)))
+    return int(n.value)
+
+
+def paged_attention(q, k_pages, v_pages, tables, rows, cu_new, num_kv_heads: int, *, max_new: int, causal: bool = True,
+                    scale: float = 0.0, out_dtype=None, with_lse: bool = True, out=None, lse=None, workspace=None,
+                    stream=None):
+    """Attention of the new tokens q [T, Hq, d] over the paged rows of their segments, their own included
+    (sgdkv_paged_attention): tables int32 [B * Hkv, max_pages], rows int32 [B * Hkv], cu_new int32 [B + 1], all on
+    the GPU; max_new is at least the longest sequence's number of new tokens. Returns (out, lse)."""
+    import torch
+    dev = q.device
+    _need_same(dev, k_pages=k_pages, v_pages=v_pages, tables=tables, rows=rows, cu_new=cu_new, out=out, lse=lse,
+               workspace=workspace)
+    pool = page_pool(k_pages, v_pages)
+    _need(q.dim() == 3 and q.shape[2] == pool.head_dim and q.dtype == k_pages.dtype and q.is_contiguous(),
+          "q must be a dense [T, Hq, d] of the pool's dtype")
+    _need(tables.dim() == 2 and rows.dim() == 1 and cu_new.dim() == 1 and cu_new.numel() >= 2,
+          "tables must be [B * Hkv, max_pages], rows [B * Hkv] and cu_new [B + 1]")
+    B, (T, Hq, d) = cu_new.numel() - 1, q.shape
+    _need(rows.numel() == tables.shape[0] == B * int(num_kv_heads),
+          f"{rows.numel()} rows and {tables.shape[0]} tables for {B} sequences of {num_kv_heads} KV heads")
+    _need_int32(tables=tables, rows=rows, cu_new=cu_new)
+    desc = _paged_desc(q, num_kv_heads, B, max_new, tables.shape[1], out_dtype, causal, scale)
+    with _on_stream(dev, stream) as s:
+        od = torch.bfloat16 if desc.out_dtype == DTYPE_BF16 else torch.float32
+        if out is None:
+            out = torch.empty((T, Hq, d), dtype=od, device=dev)
+        if with_lse and lse is None:
+            lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
+        _need(tuple(out.shape) == (T, Hq, d) and out.dtype == od and out.is_contiguous(),
+              f"out must be a dense {(T, Hq, d)} of {od}")
+        _need(not with_lse or (tuple(lse.shape) == (T, Hq) and lse.dtype == torch.float32 and lse.is_contiguous()),
+              f"lse must be a dense fp32 {(T, Hq)}")
+        if workspace is None:
+            workspace = alloc_workspace(paged_attention_workspace_size(q, num_kv_heads, B, max_new=max_new), dev)
+        _check(load_library().sgdkv_paged_attention(
+            ctypes.byref(pool), ctypes.byref(desc), _ptr(q), _ptr(tables), _ptr(rows), _ptr(cu_new), _ptr(out),
+            _ptr(lse) if with_lse else None, _ptr(workspace), workspace.numel() * workspace.element_size(), s))
+    return out, (lse if with_lse else None)
 
 
 # ------------------------------------------------------- kernel timing

@@ -27,8 +27,9 @@ DEVICE = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-p
 ILP = ["-mllvm", "-amdgpu-sched-strategy=max-ilp"]
 FILE_FLAGS = {"lse_kernels_ilp.hip": ILP, "score_kernels_ilp.hip": ILP}
 KERNEL_SOURCES = ["lse_kernels.hip", "lse_kernels_ilp.hip", "score_kernels.hip", "score_kernels_ilp.hip",
-                  "select_kernels.hip", "decode_kernels.hip", "decode_scratch.hip"]
-HOST_SOURCES = ["sgdkv_host.cpp", "profile.cpp"]
+                  "select_kernels.hip", "decode_kernels.hip", "decode_scratch.hip", "paged_cache.hip", "paged_few.hip",
+                  "paged_many.hip"]
+HOST_SOURCES = ["sgdkv_host.cpp", "paged_host.cpp", "profile.cpp"]
 
 
 def _run(cmd):

@@ -1,0 +1,216 @@
+// Attention of new tokens over a paged per-head KV cache (gfx950): shared by the instances for few query
+// rows (paged_few.hip) and for many (paged_many.hip).
+//
+// Segment (b, h) holds the rows of KV head h of sequence b, the new tokens' own rows last. Token i of the n
+// new ones sees rows 0 .. rows - n + i; the G query heads of the group see the same rows, so the n * G query
+// rows are cut into tiles of whole tokens (`tokens` of them, the G heads of a token together) and every key
+// row is read once per tile. S^T = K Q^T is computed rather than S: a lane then holds one query row's logits
+// (keys down the accumulator registers), so the softmax statistics need no cross-lane work until the end, and
+// the probabilities are already the B operand of O^T = V^T P^T, with the keys of a step in the order the
+// accumulator left them. V^T takes the same key order and comes out of LDS through the transposing read.
+//
+// Work is shared by cost, not by tile: the tiles in (segment, tile) order form one line whose length is the
+// key rows each has to see, cut into equal pieces, one per workgroup. A piece covers whole tiles and at most
+// two part ones, whose partial results (m, s, o) go to the workspace; the merge kernel joins them in order.
+// The lengths are read on the device, so a captured call replays with whatever they have become.
+#pragma once
+
+#include "device_common.h"
+#include "mfma_frag.h"
+#include "paged_internal.h"
+#include "sgdkv_internal.h"
+
+namespace sgdkv {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kAttnBlock = 256;
+constexpr int kAttnWaves = kAttnBlock / 64;
+
+// A segment as a workgroup sees it. Lengths that do not fit the buffers are cut to them.
+struct PagedSeg {
+  int t0;      // first token
+  int n;       // tokens computed
+  int rows;    // rows of the segment
+  int base;    // token i sees base + i + 1 rows (clamped to [0, rows])
+  int tiles;   // query tiles
+};
+
+__device__ __forceinline__ PagedSeg paged_seg(const PagedAttnArgs& a, int seg) {
+  PagedSeg s;
+  const int b = seg / a.Hkv;
+  int c0 = a.cu[b], c1 = a.cu[b + 1];
+  c0 = min(max(c0, 0), a.T);
+  c1 = min(max(c1, c0), a.T);
+  const int64_t most = (int64_t)a.max_pages << a.page_shift;
+  const int r = max(a.rows[seg], 0);
+  s.rows = r > most ? (int)most : r;
+  s.t0 = c0;
+  s.n = min(c1 - c0, a.max_new);
+  s.base = s.rows - (c1 - c0);
+  s.tiles = (s.n + a.tokens - 1) / a.tokens;
+  return s;
+}
+
+// Rows that token i sees, and those that query tile t sees (its last token's).
+__device__ __forceinline__ int seen_by(const PagedAttnArgs& a, const PagedSeg& s, int i) {
+  return a.causal ? max(s.base + i + 1, 0) : s.rows;
+}
+__device__ __forceinline__ int tile_rows(const PagedAttnArgs& a, const PagedSeg& s, int t) {
+  return seen_by(a, s, min((t + 1) * a.tokens, s.n) - 1);
+}
+// A tile costs the rows it sees, at least one (its results are written all the same). The first m tiles:
+__device__ __forceinline__ int64_t cost_of(const PagedAttnArgs& a, const PagedSeg& s, int m) {
+  if (!a.causal) return (int64_t)m * max(s.rows, 1);
+  if (m <= 0) return 0;
+  const int64_t full = m < s.tiles ? m : s.tiles - 1;  // tiles whose last token is number (t + 1) * tokens
+  int64_t blind = s.base < 0 ? -(int64_t)s.base / a.tokens : 0;  // those that see nothing
+  if (blind > full) blind = full;
+  int64_t sum = blind + (full - blind) * s.base + (int64_t)a.tokens * (full * (full + 1) - blind * (blind + 1)) / 2;
+  if (m == s.tiles) sum += max(s.base + s.n, 1);
+  return sum;
+}
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)v >> 32));
+  return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+// A place on the line: a tile and where it starts.
+struct LineTile {
+  int seg, tile;
+  int64_t start;
+};
+
+struct LineScratch {
+  int64_t wave_sum[kAttnWaves];
+  int64_t start;
+  int seg;
+};
+
+// Adds the segments up (the whole workgroup); total = the line's length. Then finds the tile that holds
+// place x (the same for every thread) where x < total. The total decides a worker's share, so x comes from
+// place(total).
+template <typename F>
+__device__ __forceinline__ bool find_tile(const PagedAttnArgs& a, LineScratch& sc, int64_t& total, F place,
+                                          LineTile& at) {
+  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+  const int per = (a.S + kAttnBlock - 1) / kAttnBlock;
+  const int s0 = min(tid * per, a.S), s1 = min(s0 + per, a.S);
+  int64_t mine = 0;
+  for (int s = s0; s < s1; ++s) {
+    const PagedSeg g = paged_seg(a, s);
+    mine += cost_of(a, g, g.tiles);
+  }
+  int64_t x = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t y = __shfl_up((long long)x, o, 64);
+    if (lane >= o) x += y;
+  }
+  if (lane == 63) sc.wave_sum[wid] = x;
+  __syncthreads();
+  int64_t before = x - mine;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kAttnWaves; ++w) {
+    if (w < wid) before += sc.wave_sum[w];
+    total += sc.wave_sum[w];
+  }
+  total = uniform(total);
+  const int64_t want = place(total);
+  if (want >= total) return false;
+  if (want >= before && want < before + mine) {
+    int64_t run = before;
+    for (int s = s0; s < s1; ++s) {
+      const PagedSeg g = paged_seg(a, s);
+      const int64_t c = cost_of(a, g, g.tiles);
+      if (want < run + c) {
+        sc.seg = s;
+        sc.start = run;
+        break;
+      }
+      run += c;
+    }
+  }
+  __syncthreads();
+  at.seg = uniform(sc.seg);
+  const int64_t seg_start = uniform(sc.start);
+  const PagedSeg g = paged_seg(a, at.seg);
+  int lo = 0, hi = g.tiles;  // the last tile that starts at or before `want`
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (seg_start + cost_of(a, g, mid) <= want) lo = mid;
+    else hi = mid;
+  }
+  at.tile = uniform(lo);
+  at.start = uniform(seg_start + cost_of(a, g, lo));
+  return true;
+}
+
+// A worker's share of the line: at least min_cost key rows.
+__device__ __forceinline__ int64_t share_of(const PagedAttnArgs& a, int64_t total) {
+  const int64_t q = (total + a.workers - 1) / a.workers;
+  return q < a.min_cost ? a.min_cost : q;
+}
+
+// Neighbouring workers on one XCD (workgroups go to the eight XCDs in turn): they read the same segment's
+// rows, from one L2.
+__device__ __forceinline__ int worker_of(const PagedAttnArgs& a) {
+  const int bid = blockIdx.x;
+  return a.workers % 8 == 0 ? (bid & 7) * (a.workers >> 3) + (bid >> 3) : bid;
+}
+
+// Buffer over the 16-row group of a segment that starts at row r0, `valid` rows of it (0 or fewer: none).
+// A table entry outside the pool gives an empty buffer, whose reads are zeros.
+__device__ __forceinline__ int group_page(const PagedAttnArgs& a, const int32_t* table, int r0, int limit) {
+  return r0 < limit ? table[r0 >> a.page_shift] : -1;
+}
+__device__ __forceinline__ rsrc_t group_rsrc(const PagedAttnArgs& a, const void* pool, int page, int r0, int valid,
+                                             int row_bytes) {
+  const bool ok = page >= 0 && page < a.num_pages && valid > 0;
+  const int64_t row = ok ? ((int64_t)page << a.page_shift) + (r0 & ((1 << a.page_shift) - 1)) : 0;
+  const int n = ok ? min(valid, 16) : 0;
+  return make_rsrc(static_cast<const char*>(pool) + row * row_bytes, (uint64_t)(n * row_bytes));
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
+  f32x2 v = {x, y};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+// What packing rounded away.
+__device__ __forceinline__ uint32_t pack_bf16_rest(float x, float y, uint32_t hi) {
+  return pack_bf16(x - bf16_lo(hi), y - bf16_hi(hi));
+}
+
+// Four keys (rows) by the wave's 16-lane groups' columns, transposed: lane i of a group receives column i of
+// the four rows whose pieces the group's lanes point at (lane 4r + c at row r, columns 4c .. 4c + 3).
+__device__ __forceinline__ u32x2 lds_transposed(const char* p) {
+  typedef __attribute__((address_space(3))) bf16x4* lds_ptr;
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)(p)));
+}
+
+// Four consecutive columns of an output row.
+__device__ __forceinline__ void store_out4(const PagedAttnArgs& a, int64_t row, int D, int col, f32x4 v) {
+  if (a.out_dtype) {
+    u32x2 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    *reinterpret_cast<u32x2*>(static_cast<char*>(a.out) + (row * D + col) * 2) = w;
+  } else {
+    *reinterpret_cast<f32x4*>(static_cast<char*>(a.out) + (row * D + col) * 4) = v;
+  }
+}
+
+constexpr float kLn2 = 0.693147180559945309f;
+__device__ __forceinline__ float lse_of(float m, float s) {
+  return s > 0.f ? (m + fast_log2(s)) * kLn2 : (s == 0.f ? -INFINITY : s);
+}
+
+hipError_t launch_paged_few(const PagedAttnArgs& a, int rows, hipStream_t stream);
+hipError_t launch_paged_many(const PagedAttnArgs& a, hipStream_t stream);
+
+}  // namespace sgdkv

@@ -19,6 +19,7 @@
 #include <string>
 #include <vector>
 
+#include "host_common.h"
 #include "sgdkv_internal.h"
 
 namespace {
@@ -73,6 +74,16 @@ sgdkv_status check_device(int* cus_out = nullptr) {
   if (cus_out) *cus_out = cus[dev];
   return SGDKV_OK;
 }
+
+}  // namespace
+
+namespace sgdkv {
+sgdkv_status host_fail(sgdkv_status code, const char* message) { return fail(code, "%s", message); }
+sgdkv_status host_ok() { return ok(); }
+sgdkv_status host_check_device(int* cus_out) { return check_device(cus_out); }
+}  // namespace sgdkv
+
+namespace {
 
 // ----------------------------------------------------------------- budgets
 struct Ranked {
