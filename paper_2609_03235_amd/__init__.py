@@ -378,55 +378,69 @@ PAGES_OK, PAGES_SHORT, PAGES_ROWS, PAGES_STACK, PAGES_SLOTS = range(5)
 
 
 class _on_stream:
-    """Makes the tensors' device current and `stream` (None: that device's current stream) torch's current
-    stream, so that what a call allocates belongs to the stream it is used on. Enters as the raw handle."""
+    """Makes GPU `index` current and `stream` (None: that GPU's current stream) torch's current stream, so that
+    what a call allocates belongs to the stream it is used on. Enters as the raw handle. Where both are current
+    already, the usual call, nothing is switched (a serving step makes several calls of a few us each)."""
+    __slots__ = ("guards",)
 
-    def __init__(self, device, stream):
+    def __init__(self, index, stream):
         import torch
-        self.guards = [torch.cuda.device(device)]
-        if stream is not None:
-            if not hasattr(stream, "cuda_stream"):
-                stream = torch.cuda.ExternalStream(int(stream), device=device)
-            if stream.device != device:
-                raise SgdkvError(ERR_INVALID_ARG, f"the stream is on {stream.device}, the tensors on {device}")
-            self.guards.append(torch.cuda.stream(stream))
+        self.guards = ()
+        if stream is not None or torch.cuda.current_device() != index:
+            guards = [torch.cuda.device(index)]
+            if stream is not None:
+                if not hasattr(stream, "cuda_stream"):
+                    stream = torch.cuda.ExternalStream(int(stream), device=torch.device("cuda", index))
+                if stream.device.index != index:
+                    _refuse(f"the stream is on {stream.device}, the tensors on cuda:{index}")
+                guards.append(torch.cuda.stream(stream))
+            self.guards = guards
 
     def __enter__(self):
         import torch
         for g in self.guards:
             g.__enter__()
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        return torch.cuda.current_stream().cuda_stream
 
     def __exit__(self, *exc):
         for g in reversed(self.guards):
             g.__exit__(*exc)
 
 
-def _need(cond: bool, message: str):
-    if not cond:
-        raise SgdkvError(ERR_INVALID_ARG, message)
+def _refuse(message: str):
+    raise SgdkvError(ERR_INVALID_ARG, message)
 
 
-def _need_same(device, **tensors):
-    """Every given tensor is on `device` (a GPU)."""
-    _need(device.type == "cuda", f"tensors must be on a GPU, not on {device}")
-    for name, t in tensors.items():
-        _need(t is None or t.device == device, f"{name} is on another device than {device}")
+def _gpu_of(first, *others) -> int:
+    """The index of the GPU that every given tensor is on."""
+    index = first.get_device()
+    if index < 0:
+        _refuse(f"tensors must be on a GPU, not on {first.device}")
+    for t in others:
+        if t is not None and t.get_device() != index:
+            _refuse(f"a tensor is on {t.device}, the others are on cuda:{index}")
+    return index
 
 
-def _need_int32(shape=None, **tensors):
+def _check_int32(t, name, shape=None):
     import torch
-    for name, t in tensors.items():
-        _need(t.dtype == torch.int32, f"{name} must be int32, not {t.dtype}")
-        _need(t.is_contiguous(), f"{name} must be contiguous")
-        _need(shape is None or tuple(t.shape) == tuple(shape), f"{name} has shape {tuple(t.shape)}, not {shape}")
+    if t.dtype is not torch.int32 or not t.is_contiguous():
+        _refuse(f"{name} must be contiguous int32, not {t.dtype}")
+    if shape is not None and t.shape != shape:
+        _refuse(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+
+
+def _check_dense(t, name, shape, dtype):
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
+        _refuse(f"{name} must be a dense {tuple(shape)} of {dtype}, not {tuple(t.shape)} of {t.dtype}")
 
 
 def page_pool(k_pages, v_pages) -> PagePool:
     """The descriptor of a pool k_pages, v_pages [num_pages, page_size, d]."""
-    _need(k_pages.dim() == 3 and k_pages.shape == v_pages.shape and k_pages.dtype == v_pages.dtype,
-          "k_pages and v_pages must be [num_pages, page_size, d] of one dtype")
-    _need(k_pages.is_contiguous() and v_pages.is_contiguous(), "k_pages and v_pages must be contiguous")
+    if k_pages.dim() != 3 or k_pages.shape != v_pages.shape or k_pages.dtype is not v_pages.dtype:
+        _refuse("k_pages and v_pages must be [num_pages, page_size, d] of one dtype")
+    if not (k_pages.is_contiguous() and v_pages.is_contiguous()):
+        _refuse("k_pages and v_pages must be contiguous")
     n, page, d = k_pages.shape
     return PagePool(k_pages.data_ptr(), v_pages.data_ptr(), n, page, d, _dtype_code(k_pages), 0)
 
@@ -436,59 +450,69 @@ def page_update(rows, add, tables, free_pages, head, *, page_size: int, n_slots:
     """Pages and slots for the rows that segments gain or lose (sgdkv_page_update). rows [B * Hkv], tables
     [B * Hkv, max_pages] (updated in place), free_pages [n] (a stack, updated in place) and head [1] are int32;
     add is int32 [B], or [B * Hkv] with by_segment. Returns slots ([n_slots, Hkv] or [n_slots]), rows, head, cu,
-    status and the updated tables and free_pages. rows_out and head_out may be rows and head."""
+    status and the updated tables and free_pages. rows_out and head_out may be rows and head. Results that the
+    caller does not bring share one allocation."""
     import torch
-    dev = rows.device
-    _need_same(dev, add=add, tables=tables, free_pages=free_pages, head=head, rows_out=rows_out, head_out=head_out,
-               slots=slots, cu=cu, status=status)
-    _need(rows.dim() == 1 and add.dim() == 1 and tables.dim() == 2 and free_pages.dim() == 1,
-          "rows, add and free_pages must have one dimension and tables two")
-    S, n_add = rows.numel(), add.numel()
-    _need(S > 0 and tables.shape[0] == S, f"tables has {tables.shape[0]} rows for {S} segments")
-    _need(n_add == S if by_segment else n_add > 0 and S % n_add == 0, f"add holds {n_add} values for {S} segments")
+    index = _gpu_of(rows, add, tables, free_pages, head, rows_out, head_out, slots, cu, status)
+    if rows.dim() != 1 or add.dim() != 1 or tables.dim() != 2 or free_pages.dim() != 1:
+        _refuse("rows, add and free_pages must have one dimension and tables two")
+    S, n_add, n_slots = rows.shape[0], add.shape[0], int(n_slots)
+    if S == 0 or tables.shape[0] != S:
+        _refuse(f"tables has {tables.shape[0]} rows for {S} segments")
+    if n_add != S if by_segment else n_add == 0 or S % n_add:
+        _refuse(f"add holds {n_add} values for {S} segments")
+    if n_slots < 0:
+        _refuse("n_slots must be >= 0")
     B = 1 if by_segment else n_add
     Hkv = S // B
-    n_slots = int(n_slots)
-    _need(n_slots >= 0, "n_slots must be >= 0")
-    _need_int32(rows=rows, add=add, tables=tables, free_pages=free_pages)
-    _need_int32((1,), head=head)
-    with _on_stream(dev, stream) as s:
-        new = lambda *shape: torch.empty(shape, dtype=torch.int32, device=dev)
-        rows_out = new(S) if rows_out is None else rows_out
-        head_out = new(1) if head_out is None else head_out
-        cu = new(n_add + 1) if cu is None else cu
-        status = new(1) if status is None else status
-        shape = (n_slots,) if by_segment else (n_slots, Hkv)
-        slots = new(*shape) if slots is None else slots
-        _need_int32((S,), rows_out=rows_out)
-        _need_int32((1,), head_out=head_out, status=status)
-        _need_int32((n_add + 1,), cu=cu)
-        _need_int32(shape, slots=slots)
-        desc = PageDesc(B, Hkv, int(page_size), tables.shape[1], int(bool(by_segment)), 0, free_pages.numel(), n_slots)
+    shape = (n_slots,) if by_segment else (n_slots, Hkv)
+    for t, name, want in ((rows, "rows", None), (add, "add", None), (tables, "tables", None),
+                          (free_pages, "free_pages", None), (head, "head", (1,)), (rows_out, "rows_out", (S,)),
+                          (head_out, "head_out", (1,)), (cu, "cu", (n_add + 1,)), (status, "status", (1,)),
+                          (slots, "slots", shape)):
+        if t is not None:
+            _check_int32(t, name, want)
+    with _on_stream(index, stream) as s:
+        if slots is None or rows_out is None or cu is None or head_out is None or status is None:
+            # each at a multiple of 16 bytes
+            n = n_slots if by_segment else n_slots * Hkv
+            sizes = (n, -n % 4, S, -S % 4, n_add + 1, (3 - n_add) % 4, 1, 3, 1)
+            parts = torch.empty(sum(sizes), dtype=torch.int32, device=rows.device).split_with_sizes(sizes)
+            if slots is None:
+                slots = parts[0] if by_segment else parts[0].view(shape)
+            rows_out = parts[2] if rows_out is None else rows_out
+            cu = parts[4] if cu is None else cu
+            head_out = parts[6] if head_out is None else head_out
+            status = parts[8] if status is None else status
+        desc = PageDesc(B, Hkv, page_size, tables.shape[1], 1 if by_segment else 0, 0, free_pages.shape[0], n_slots)
         _check(load_library().sgdkv_page_update(
-            ctypes.byref(desc), _ptr(rows), _ptr(add), _ptr(tables), _ptr(free_pages), _ptr(head), _ptr(rows_out),
-            _ptr(head_out), _ptr(cu), _ptr(slots), _ptr(status), s))
+            ctypes.byref(desc), rows.data_ptr(), add.data_ptr(), tables.data_ptr(), free_pages.data_ptr(),
+            head.data_ptr(), rows_out.data_ptr(), head_out.data_ptr(), cu.data_ptr(), slots.data_ptr(),
+            status.data_ptr(), s))
     return dict(slots=slots, rows=rows_out, head=head_out, cu=cu, status=status, tables=tables, free_pages=free_pages)
 
 
 def paged_store(k_rows, v_rows, slots, k_pages, v_pages, *, stream=None):
     """Copy rows [n, d] to their slots (sgdkv_paged_store): slots int32 [n], -1 for none."""
-    dev = k_pages.device
-    _need_same(dev, v_pages=v_pages, k_rows=k_rows, v_rows=v_rows, slots=slots)
+    index = _gpu_of(k_pages, v_pages, k_rows, v_rows, slots)
     pool = page_pool(k_pages, v_pages)
-    _need(k_rows.dim() == 2 and k_rows.shape == v_rows.shape and k_rows.shape[1] == pool.head_dim
-          and k_rows.dtype == v_rows.dtype == k_pages.dtype, "k_rows and v_rows must be [n, d] of the pool's dtype")
-    n = k_rows.shape[0]
-    _need_int32((n,), slots=slots)
-    with _on_stream(dev, stream) as s:
-        _check(load_library().sgdkv_paged_store(ctypes.byref(pool), _ptr(k_rows), _ptr(v_rows), _ptr(slots), n, s))
+    if k_rows.dim() != 2:
+        _refuse("k_rows and v_rows must be [n, d]")
+    shape = (k_rows.shape[0], k_pages.shape[2])
+    _check_dense(k_rows, "k_rows", shape, k_pages.dtype)
+    _check_dense(v_rows, "v_rows", shape, k_pages.dtype)
+    _check_int32(slots, "slots", shape[:1])
+    with _on_stream(index, stream) as s:
+        _check(load_library().sgdkv_paged_store(ctypes.byref(pool), k_rows.data_ptr(), v_rows.data_ptr(),
+                                                slots.data_ptr(), shape[0], s))
 
 
-def _token_stride(t, name, heads, d):
+def _token_stride(t, name, d):
     """Elements between tokens of t [T, heads, d], whose heads must be dense."""
-    _need(heads == 0 or t.shape[0] == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == d)),
-          f"the heads of a token of {name} must be dense")
-    return t.stride(0) if t.shape[0] > 1 else heads * d
+    T, heads, _ = t.shape
+    if T and heads and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != d)):
+        _refuse(f"the heads of a token of {name} must be dense")
+    return t.stride(0) if T > 1 else heads * d
 
 
 def norm_rope_store(q, k, v, positions, slots, k_pages, v_pages, *, inv_freq=None, q_weight=None, k_weight=None,
@@ -498,46 +522,47 @@ def norm_rope_store(q, k, v, positions, slots, k_pages, v_pages, *, inv_freq=Non
     None: no rotation), keys and values stored to slots (int32 [T, Hkv], -1 for none). q, k and v may be parts of
     one projection's output. q may be None. Returns q_out [T, Hq, d]."""
     import torch
-    dev = k_pages.device
-    _need_same(dev, v_pages=v_pages, q=q, k=k, v=v, positions=positions, slots=slots, inv_freq=inv_freq,
-               q_weight=q_weight, k_weight=k_weight, q_out=q_out)
+    index = _gpu_of(k_pages, v_pages, q, k, v, positions, slots, inv_freq, q_weight, k_weight, q_out)
     pool = page_pool(k_pages, v_pages)
-    dt, d = k_pages.dtype, pool.head_dim
-    _need(k.dim() == 3 and v.shape == k.shape and k.shape[2] == d and k.dtype == v.dtype == dt,
-          "k and v must be [T, Hkv, d] of the pool's dtype")
-    T, Hkv = k.shape[:2]
-    Hq = 0 if q is None else q.shape[1]
-    _need(q is None or (q.dim() == 3 and q.shape[0] == T and q.shape[2] == d and q.dtype == dt),
-          "q must be [T, Hq, d] of the pool's dtype")
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        _need(w is None or (tuple(w.shape) == (d,) and w.dtype == dt and w.is_contiguous()),
-              f"{name} must be [d] of the pool's dtype")
-    _need(inv_freq is None or (inv_freq.dim() == 1 and inv_freq.dtype == torch.float32 and inv_freq.is_contiguous()),
-          "inv_freq must be fp32 with one dimension")
-    _need_int32((T,), positions=positions)
-    _need_int32((T, Hkv), slots=slots)
-    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
-    with _on_stream(dev, stream) as s:
+    dt, d = k_pages.dtype, k_pages.shape[2]
+    if k.dim() != 3 or v.shape != k.shape or k.shape[2] != d or k.dtype is not dt or v.dtype is not dt:
+        _refuse("k and v must be [T, Hkv, d] of the pool's dtype")
+    T, Hkv, _ = k.shape
+    Hq = q_stride = 0
+    if q is not None:
+        if q.dim() != 3 or q.shape[0] != T or q.shape[2] != d or q.dtype is not dt:
+            _refuse("q must be [T, Hq, d] of the pool's dtype")
+        Hq = q.shape[1]
+        q_stride = _token_stride(q, "q", d)
+        if q_out is not None:
+            _check_dense(q_out, "q_out", (T, Hq, d), dt)
+    if q_weight is not None:
+        _check_dense(q_weight, "q_weight", (d,), dt)
+    if k_weight is not None:
+        _check_dense(k_weight, "k_weight", (d,), dt)
+    if inv_freq is not None:
+        _check_dense(inv_freq, "inv_freq", (inv_freq.numel(),), torch.float32)
+    _check_int32(positions, "positions", (T,))
+    _check_int32(slots, "slots", (T, Hkv))
+    desc = NormRopeDesc(T, Hq, Hkv, q_stride, _token_stride(k, "k", d), _token_stride(v, "v", d),
+                        0 if inv_freq is None else 2 * inv_freq.shape[0], 1 if interleaved else 0, eps, 0)
+    with _on_stream(index, stream) as s:
         if Hq and q_out is None:
-            q_out = torch.empty((T, Hq, d), dtype=dt, device=dev)
-        _need(not Hq or (tuple(q_out.shape) == (T, Hq, d) and q_out.dtype == dt and q_out.is_contiguous()),
-              "q_out must be a dense [T, Hq, d] of the pool's dtype")
-        desc = NormRopeDesc(T, Hq, Hkv, 0 if not Hq else _token_stride(q, "q", Hq, d), _token_stride(k, "k", Hkv, d),
-                            _token_stride(v, "v", Hkv, d), rot, int(bool(interleaved)), float(eps), 0)
+            q_out = torch.empty((T, Hq, d), dtype=dt, device=q.device)
         _check(load_library().sgdkv_norm_rope_store(
             ctypes.byref(pool), ctypes.byref(desc), q.data_ptr() if Hq else None, k.data_ptr(), v.data_ptr(),
-            _ptr(positions), _ptr(slots), _ptr(inv_freq), _ptr(q_weight), _ptr(k_weight),
-            _ptr(q_out) if Hq else None, s))
+            positions.data_ptr(), slots.data_ptr(), None if inv_freq is None else inv_freq.data_ptr(),
+            None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+            q_out.data_ptr() if Hq else None, s))
     return q_out
 
 
 def _paged_desc(q, num_kv_heads, batch, max_new, max_pages, out_dtype, causal, scale) -> PagedDesc:
     import torch
-    T, Hq, _ = q.shape
-    _need(out_dtype in (None, torch.bfloat16, torch.float32), f"out_dtype {out_dtype}")
-    od = _dtype_code(q) if out_dtype is None else (DTYPE_BF16 if out_dtype == torch.bfloat16 else DTYPE_F32)
-    return PagedDesc(int(batch), Hq, int(num_kv_heads), od, T, int(max_new), int(max_pages), int(bool(causal)),
-                     float(scale))
+    if out_dtype is not None and out_dtype is not torch.bfloat16 and out_dtype is not torch.float32:
+        _refuse(f"out_dtype {out_dtype}")
+    od = _dtype_code(q) if out_dtype is None else (DTYPE_BF16 if out_dtype is torch.bfloat16 else DTYPE_F32)
+    return PagedDesc(batch, q.shape[1], num_kv_heads, od, q.shape[0], max_new, max_pages, 1 if causal else 0, scale)
 
 
 def paged_attention_workspace_size(q, num_kv_heads: int, batch: int, *, max_new: int) -> int:
@@ -557,34 +582,37 @@ def paged_attention(q, k_pages, v_pages, tables, rows, cu_new, num_kv_heads: int
     (sgdkv_paged_attention): tables int32 [B * Hkv, max_pages], rows int32 [B * Hkv], cu_new int32 [B + 1], all on
     the GPU; max_new is at least the longest sequence's number of new tokens. Returns (out, lse)."""
     import torch
-    dev = q.device
-    _need_same(dev, k_pages=k_pages, v_pages=v_pages, tables=tables, rows=rows, cu_new=cu_new, out=out, lse=lse,
-               workspace=workspace)
+    index = _gpu_of(q, k_pages, v_pages, tables, rows, cu_new, out, lse, workspace)
     pool = page_pool(k_pages, v_pages)
-    _need(q.dim() == 3 and q.shape[2] == pool.head_dim and q.dtype == k_pages.dtype and q.is_contiguous(),
-          "q must be a dense [T, Hq, d] of the pool's dtype")
-    _need(tables.dim() == 2 and rows.dim() == 1 and cu_new.dim() == 1 and cu_new.numel() >= 2,
-          "tables must be [B * Hkv, max_pages], rows [B * Hkv] and cu_new [B + 1]")
-    B, (T, Hq, d) = cu_new.numel() - 1, q.shape
-    _need(rows.numel() == tables.shape[0] == B * int(num_kv_heads),
-          f"{rows.numel()} rows and {tables.shape[0]} tables for {B} sequences of {num_kv_heads} KV heads")
-    _need_int32(tables=tables, rows=rows, cu_new=cu_new)
+    if q.dim() != 3 or q.shape[2] != k_pages.shape[2] or q.dtype is not k_pages.dtype or not q.is_contiguous():
+        _refuse("q must be a dense [T, Hq, d] of the pool's dtype")
+    if tables.dim() != 2 or rows.dim() != 1 or cu_new.dim() != 1 or cu_new.shape[0] < 2:
+        _refuse("tables must be [B * Hkv, max_pages], rows [B * Hkv] and cu_new [B + 1]")
+    B, shape = cu_new.shape[0] - 1, q.shape
+    if not rows.shape[0] == tables.shape[0] == B * num_kv_heads:
+        _refuse(f"{rows.shape[0]} rows and {tables.shape[0]} tables for {B} sequences of {num_kv_heads} KV heads")
+    _check_int32(tables, "tables")
+    _check_int32(rows, "rows")
+    _check_int32(cu_new, "cu_new")
     desc = _paged_desc(q, num_kv_heads, B, max_new, tables.shape[1], out_dtype, causal, scale)
-    with _on_stream(dev, stream) as s:
-        od = torch.bfloat16 if desc.out_dtype == DTYPE_BF16 else torch.float32
+    od = torch.bfloat16 if desc.out_dtype == DTYPE_BF16 else torch.float32
+    if out is not None:
+        _check_dense(out, "out", shape, od)
+    if workspace is not None and not workspace.is_contiguous():
+        _refuse("workspace must be contiguous")
+    if with_lse and lse is not None:
+        _check_dense(lse, "lse", shape[:2], torch.float32)
+    with _on_stream(index, stream) as s:
         if out is None:
-            out = torch.empty((T, Hq, d), dtype=od, device=dev)
+            out = torch.empty(shape, dtype=od, device=q.device)
         if with_lse and lse is None:
-            lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
-        _need(tuple(out.shape) == (T, Hq, d) and out.dtype == od and out.is_contiguous(),
-              f"out must be a dense {(T, Hq, d)} of {od}")
-        _need(not with_lse or (tuple(lse.shape) == (T, Hq) and lse.dtype == torch.float32 and lse.is_contiguous()),
-              f"lse must be a dense fp32 {(T, Hq)}")
+            lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device)
         if workspace is None:
-            workspace = alloc_workspace(paged_attention_workspace_size(q, num_kv_heads, B, max_new=max_new), dev)
+            workspace = alloc_workspace(paged_attention_workspace_size(q, num_kv_heads, B, max_new=max_new), q.device)
         _check(load_library().sgdkv_paged_attention(
-            ctypes.byref(pool), ctypes.byref(desc), _ptr(q), _ptr(tables), _ptr(rows), _ptr(cu_new), _ptr(out),
-            _ptr(lse) if with_lse else None, _ptr(workspace), workspace.numel() * workspace.element_size(), s))
+            ctypes.byref(pool), ctypes.byref(desc), q.data_ptr(), tables.data_ptr(), rows.data_ptr(),
+            cu_new.data_ptr(), out.data_ptr(), lse.data_ptr() if with_lse else None, workspace.data_ptr(),
+            workspace.numel() * workspace.element_size(), s))
     return out, (lse if with_lse else None)
 
 

@@ -41,7 +41,7 @@ struct PagedSeg {
 
 __device__ __forceinline__ PagedSeg paged_seg(const PagedAttnArgs& a, int seg) {
   PagedSeg s;
-  const int b = seg / a.Hkv;
+  const int b = (int)((uint32_t)seg * a.inv_hkv >> 32);
   int c0 = a.cu[b], c1 = a.cu[b + 1];
   c0 = min(max(c0, 0), a.T);
   c1 = min(max(c1, c0), a.T);
@@ -51,7 +51,7 @@ __device__ __forceinline__ PagedSeg paged_seg(const PagedAttnArgs& a, int seg) {
   s.t0 = c0;
   s.n = min(c1 - c0, a.max_new);
   s.base = s.rows - (c1 - c0);
-  s.tiles = (s.n + a.tokens - 1) / a.tokens;
+  s.tiles = (int)((uint32_t)(s.n + a.tokens - 1) / (uint32_t)a.tokens);
   return s;
 }
 
@@ -67,7 +67,7 @@ __device__ __forceinline__ int64_t cost_of(const PagedAttnArgs& a, const PagedSe
   if (!a.causal) return (int64_t)m * max(s.rows, 1);
   if (m <= 0) return 0;
   const int64_t full = m < s.tiles ? m : s.tiles - 1;  // tiles whose last token is number (t + 1) * tokens
-  int64_t blind = s.base < 0 ? -(int64_t)s.base / a.tokens : 0;  // those that see nothing
+  int64_t blind = s.base < 0 ? (int)((uint32_t)-s.base / (uint32_t)a.tokens) : 0;  // those that see nothing
   if (blind > full) blind = full;
   int64_t sum = blind + (full - blind) * s.base + (int64_t)a.tokens * (full * (full + 1) - blind * (blind + 1)) / 2;
   if (m == s.tiles) sum += max(s.base + s.n, 1);
@@ -151,6 +151,14 @@ __device__ __forceinline__ bool find_tile(const PagedAttnArgs& a, LineScratch& s
   at.tile = uniform(lo);
   at.start = uniform(seg_start + cost_of(a, g, lo));
   return true;
+}
+
+// What a worker leaves for the merge (see PagedAttnArgs::shared). `at` is its last tile, of nkt key tiles.
+__device__ __forceinline__ void leave_shared(const PagedAttnArgs& a, int w, int64_t share, const LineTile& at, int nkt) {
+  const int64_t own = share * w;
+  const int last = (int)((at.start + (int64_t)(nkt - 1) * a.key_tile) / share);
+  const bool left = at.start >= own && last > w;
+  if (threadIdx.x == 0) a.shared[w] = make_int4(at.seg, at.tile, left ? last : -1, at.start > own ? 1 : 0);
 }
 
 // A worker's share of the line: at least min_cost key rows.

@@ -11,6 +11,8 @@
 //
 // All three are bound by latency or by HBM. The pools may pass 4 GiB, so their rows are addressed with
 // 64-bit pointers; every slot is compared with the pool's size first.
+#include <algorithm>
+
 #include "device_common.h"
 #include "paged_internal.h"
 #include "sgdkv_internal.h"
@@ -22,47 +24,45 @@ namespace {
 constexpr int kWavesPerBlock = kPageBlock / 64;
 
 // ------------------------------------------------------------------ page update
-// What one segment gains or loses.
-struct Change {
-  int64_t before, after;  // rows
-  int64_t p0, p1;         // pages before and after
-};
-
-__device__ __forceinline__ Change change_of(const PageArgs& a, int s) {
-  Change c;
-  c.before = a.rows[s];
-  const int64_t add = a.add[a.by_segment ? s : s / a.Hkv];
-  c.after = c.before + add < 0 ? 0 : c.before + add;
-  const int64_t mask = ((int64_t)1 << a.page_shift) - 1;
-  c.p0 = (c.before + mask) >> a.page_shift;
-  c.p1 = (c.after + mask) >> a.page_shift;
-  return c;
+// Pages of a segment of `rows` rows, cut to the table's width (more is reported as a failure).
+__device__ __forceinline__ int pages_of(const PageArgs& a, int64_t rows) {
+  const int64_t p = (rows + ((int64_t)1 << a.page_shift) - 1) >> a.page_shift;
+  return p > a.max_pages ? a.max_pages : (int)p;
 }
 
-// Exclusive prefix sum over the workgroup's threads; total receives the sum. tmp: one entry per wave.
-__device__ __forceinline__ int64_t block_prefix(int64_t v, int64_t* tmp, int64_t& total) {
+// Exclusive prefix sums over the workgroup's threads of new rows, pages taken and pages given back.
+struct Gains {
+  int64_t fresh;
+  int taken, given;
+};
+__device__ __forceinline__ Gains block_prefix(Gains v, Gains* tmp, Gains& total) {
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-  int64_t x = v;
+  Gains x = v;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up((long long)x, o, 64);
-    if (lane >= o) x += y;
+    const int64_t f = __shfl_up((long long)x.fresh, o, 64);
+    const int t = __shfl_up(x.taken, o, 64), g = __shfl_up(x.given, o, 64);
+    if (lane >= o) {
+      x.fresh += f;
+      x.taken += t;
+      x.given += g;
+    }
   }
-  __syncthreads();
   if (lane == 63) tmp[wid] = x;
   __syncthreads();
-  int64_t before = 0;
-  total = 0;
+  Gains before{x.fresh - v.fresh, x.taken - v.taken, x.given - v.given};
+  total = Gains{0, 0, 0};
 #pragma unroll
-  for (int w = 0; w < kWavesPerBlock; ++w) {
-    if (w < wid) before += tmp[w];
-    total += tmp[w];
+  for (int w = 0; w < kPageBlock / 64; ++w) {
+    const Gains y = tmp[w];
+    if (w < wid) before = Gains{before.fresh + y.fresh, before.taken + y.taken, before.given + y.given};
+    total = Gains{total.fresh + y.fresh, total.taken + y.taken, total.given + y.given};
   }
-  return before + x - v;
+  return before;
 }
 
 // The last entry of the ascending prefix p[0 .. n) that is <= i, where empty pieces share a value.
-__device__ __forceinline__ int piece_of(const int32_t* p, int n, int64_t i) {
+__device__ __forceinline__ int piece_of(const int32_t* p, int n, int i) {
   int lo = 0, hi = n;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -72,130 +72,126 @@ __device__ __forceinline__ int piece_of(const int32_t* p, int n, int64_t i) {
   return lo;
 }
 
-// Every workgroup computes the same prefix sums over the segments (they are few beside the slots) and
-// then does its share of the entries, so one launch does what two with a scan between them would; where
-// there are several workgroups a second, one-workgroup launch (FINAL) writes rows_out and head_out, which
-// may be the inputs themselves. Nothing that one workgroup writes is read by another: table entries past
-// a segment's old pages are written and those within them read; the stack is written below its head (the
-// pages given back, looked up in their tables by those who take them in the same call) and read from its
-// head on.
+// Every workgroup reads the segments' lengths and computes the same prefix sums into LDS (they are few
+// beside the slots), then does its share of the table entries and slots: one launch, no scan before it. Bound
+// by latency: about four dependent memory reads and the scan; 512 segments and slots take 7 us, 524288 slots 11
+// (one workgroup with the lengths read again at every use took 22 and more).
+// Nothing that one workgroup writes is read by another: table entries past a segment's old pages are written
+// and those within them read; the stack is written below its head (the pages given back, looked up in their
+// tables by those who take them in the same call) and read from its head on. rows_out and head_out may be the
+// inputs themselves: where several workgroups read those, a second launch of one workgroup writes them (FINAL).
 template <bool FINAL>
-__global__ __launch_bounds__(kPageBlock) void page_update_kernel(PageArgs a, int single) {
+__global__ __launch_bounds__(kPageBlock) void page_update_kernel(PageArgs a, int write_rows) {
   extern __shared__ int32_t lds[];
-  int32_t* cu = lds;                // [pieces + 1] new rows before a segment (a sequence)
   const int pieces = a.by_segment ? a.S : a.B;
-  int32_t* taken = cu + pieces + 1;  // [S + 1] pages taken before a segment
+  int32_t* taken = lds;              // [S + 1] pages taken before a segment
   int32_t* given = taken + a.S + 1;  // [S + 1] pages given back before a segment
-  __shared__ int64_t tmp[kWavesPerBlock];
+  int32_t* rows = given + a.S + 1;   // [S]
+  int32_t* cu = rows + a.S;          // [pieces + 1] new rows before a segment (a sequence)
+  __shared__ Gains tmp[kPageBlock / 64];
   const int tid = threadIdx.x;
+  const int64_t head = a.head[0];
 
-  // prefix sums; a thread takes consecutive segments
+  // A thread takes consecutive segments (and, by token, the sequences that begin among them).
   const int per = (a.S + kPageBlock - 1) / kPageBlock;
   const int s0 = min(tid * per, a.S), s1 = min(s0 + per, a.S);
   const int64_t most = (int64_t)a.max_pages << a.page_shift;
-  int64_t n_taken = 0, n_given = 0;
+  Gains mine{0, 0, 0};
   int bad = 0;
   for (int s = s0; s < s1; ++s) {
-    const Change c = change_of(a, s);
-    bad |= c.before < 0 || c.before > most || c.after > most;
-    n_taken += c.p1 > c.p0 ? c.p1 - c.p0 : 0;
-    n_given += c.p0 > c.p1 ? c.p0 - c.p1 : 0;
+    const int b = a.by_segment ? s : s / a.Hkv;
+    const int64_t before = a.rows[s], add = a.add[b], after = max(before + add, (int64_t)0);
+    bad |= before < 0 || before > most || after > most;
+    rows[s] = (int)before;
+    const int d = pages_of(a, after) - pages_of(a, max(before, (int64_t)0));
+    mine.taken += max(d, 0);
+    mine.given += max(-d, 0);
+    if (a.by_segment || s == b * a.Hkv) mine.fresh += max(add, (int64_t)0);
   }
-  int64_t all_taken, all_given, all_new, any_bad;
-  int64_t run_t = block_prefix(n_taken, tmp, all_taken);
-  int64_t run_g = block_prefix(n_given, tmp, all_given);
-  block_prefix(bad, tmp, any_bad);
+  const int any_bad = __syncthreads_or(bad);
+  Gains all;
+  Gains run = block_prefix(mine, tmp, all);
+  const int64_t base = head - all.given;
+  const int status = any_bad                                      ? 2
+                     : head < 0 || head > a.num_free || base < 0  ? 3
+                     : all.fresh > a.num_slots                    ? 4
+                     : base + all.taken > a.num_free              ? 1
+                                                                  : 0;
   for (int s = s0; s < s1; ++s) {
-    const Change c = change_of(a, s);
-    taken[s] = (int32_t)run_t;
-    given[s] = (int32_t)run_g;
-    run_t += c.p1 > c.p0 ? c.p1 - c.p0 : 0;
-    run_g += c.p0 > c.p1 ? c.p0 - c.p1 : 0;
+    const int b = a.by_segment ? s : s / a.Hkv;
+    const int64_t before = rows[s], add = a.add[b], after = max(before + add, (int64_t)0);
+    const int d = pages_of(a, after) - pages_of(a, max(before, (int64_t)0));
+    taken[s] = run.taken;
+    given[s] = run.given;
+    run.taken += max(d, 0);
+    run.given += max(-d, 0);
+    if (a.by_segment || s == b * a.Hkv) {
+      cu[b] = (int)run.fresh;
+      run.fresh += max(add, (int64_t)0);
+    }
+    if (write_rows && blockIdx.x == 0) a.rows_out[s] = (int)(status ? before : after);
   }
-  const int pper = (pieces + kPageBlock - 1) / kPageBlock;
-  const int i0 = min(tid * pper, pieces), i1 = min(i0 + pper, pieces);
-  int64_t n_new = 0;
-  for (int i = i0; i < i1; ++i) n_new += max(a.add[i], 0);
-  int64_t run_n = block_prefix(n_new, tmp, all_new);
-  for (int i = i0; i < i1; ++i) {
-    cu[i] = (int32_t)run_n;
-    run_n += max(a.add[i], 0);
-  }
-  const int64_t head = a.head[0], base = head - all_given;
-  const int status = any_bad                                        ? 2
-                     : head < 0 || head > a.num_free || base < 0    ? 3
-                     : all_new > a.num_slots                        ? 4
-                     : base + all_taken > a.num_free                ? 1
-                                                                    : 0;
   if (tid == 0) {
-    cu[pieces] = (int32_t)all_new;
-    taken[a.S] = (int32_t)all_taken;
-    given[a.S] = (int32_t)all_given;
+    taken[a.S] = all.taken;
+    given[a.S] = all.given;
+    cu[pieces] = (int)all.fresh;
+    if (write_rows && blockIdx.x == 0) a.head_out[0] = (int)(status ? head : base + all.taken);
   }
+  if (FINAL) return;
   __syncthreads();
 
-  if (!FINAL) {
-    const int64_t stride = (int64_t)gridDim.x * kPageBlock, first = (int64_t)blockIdx.x * kPageBlock + tid;
-    if (blockIdx.x == 0) {
-      for (int i = tid; i <= pieces; i += kPageBlock) a.cu_out[i] = status ? 0 : cu[i];
-      if (tid == 0) a.status[0] = status;
-    }
-    // the page at stack index i: given back in this call below the old head, else the stack's
-    auto page_at = [&](int64_t i) -> int32_t {
-      if (i >= head) return a.free_pages[i];
-      const int g = piece_of(given, a.S, i - base);
-      return a.tables[(int64_t)g * a.max_pages + change_of(a, g).p1 + (i - base - given[g])];
-    };
-    if (status == 0) {
-      for (int64_t i = first; i < all_taken; i += stride) {
-        const int s = piece_of(taken, a.S, i);
-        a.tables[(int64_t)s * a.max_pages + change_of(a, s).p0 + (i - taken[s])] = page_at(base + i);
-      }
-      for (int64_t i = first; i < all_given; i += stride) a.free_pages[base + i] = page_at(base + i);
-    }
-    // slots: a thread takes four consecutive ones
-    const int64_t n = a.num_slots * (a.by_segment ? 1 : a.Hkv);
-    for (int64_t at = first * 4; at < n; at += stride * 4) {
-      int32_t out[4] = {-1, -1, -1, -1};
-      int64_t item = a.by_segment ? at : at / a.Hkv;
-      int h = a.by_segment ? 0 : (int)(at - item * a.Hkv);
-      int piece = -1, seg_of = -1;
-      Change c{};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (status == 0 && item < all_new) {
-          if (piece < 0 || item >= cu[piece + 1]) piece = piece_of(cu, pieces, item);
-          const int s = a.by_segment ? piece : piece * a.Hkv + h;
-          if (s != seg_of) {
-            c = change_of(a, s);
-            seg_of = s;
-          }
-          const int64_t pos = c.before + (item - cu[piece]), j = pos >> a.page_shift;
-          const int32_t page = j < c.p0 ? a.tables[(int64_t)s * a.max_pages + j]
-                                        : page_at(base + taken[s] + (j - c.p0));
-          const int64_t slot = ((int64_t)page << a.page_shift) + (pos & (((int64_t)1 << a.page_shift) - 1));
-          out[e] = slot < 0 || slot > 0x7FFFFFFF ? -1 : (int32_t)slot;
-        }
-        if (a.by_segment || ++h == a.Hkv) {
-          h = 0;
-          ++item;
-        }
-      }
-      if (at + 4 <= n) {
-        *reinterpret_cast<int4*>(a.slots + at) = make_int4(out[0], out[1], out[2], out[3]);
-      } else {
-        for (int e = 0; e < 4 && at + e < n; ++e) a.slots[at + e] = out[e];
-      }
-    }
+  const int64_t stride = (int64_t)gridDim.x * kPageBlock, first = (int64_t)blockIdx.x * kPageBlock + tid;
+  if (blockIdx.x == 0) {
+    for (int i = tid; i <= pieces; i += kPageBlock) a.cu_out[i] = status ? 0 : cu[i];
+    if (tid == 0) a.status[0] = status;
   }
-  if (FINAL || single) {
-    // one workgroup: every read of rows and head above is done
-    __syncthreads();
-    for (int s = tid; s < a.S; s += kPageBlock) {
-      const Change c = change_of(a, s);
-      a.rows_out[s] = (int32_t)(status ? c.before : c.after);
+  // the page at stack index i: given back in this call below the old head, else the stack's
+  auto page_at = [&](int64_t i) -> int32_t {
+    if (i >= head) return a.free_pages[i];
+    const int at = (int)(i - base), g = piece_of(given, a.S, at);
+    const int left = pages_of(a, rows[g]) - (given[g + 1] - given[g]);  // its pages afterwards
+    return a.tables[(int64_t)g * a.max_pages + left + (at - given[g])];
+  };
+  if (status == 0) {
+    for (int64_t i = first; i < all.taken; i += stride) {
+      const int s = piece_of(taken, a.S, (int)i);
+      a.tables[(int64_t)s * a.max_pages + pages_of(a, rows[s]) + ((int)i - taken[s])] = page_at(base + i);
     }
-    if (tid == 0) a.head_out[0] = (int32_t)(status ? head : base + all_taken);
+    for (int64_t i = first; i < all.given; i += stride) a.free_pages[base + i] = page_at(base + i);
+  }
+  // slots: a thread takes four consecutive ones
+  const uint32_t per_row = a.by_segment ? 1 : a.Hkv;
+  const int64_t n = a.num_slots * per_row;
+  const int in_page = (1 << a.page_shift) - 1;
+  for (int64_t at = first * 4; at < n; at += stride * 4) {
+    int32_t out[4] = {-1, -1, -1, -1};
+    uint32_t item = (uint32_t)at / per_row, h = (uint32_t)at - item * per_row;
+    int piece = -1, seg = -1, entry = -1, page = 0;  // neighbours mostly share these
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (status == 0 && item < (uint32_t)all.fresh) {
+        if (piece < 0 || (int)item >= cu[piece + 1]) piece = piece_of(cu, pieces, (int)item);
+        const int s = a.by_segment ? piece : piece * a.Hkv + (int)h;
+        const int pos = rows[s] + ((int)item - cu[piece]), j = pos >> a.page_shift;
+        if (s != seg || j != entry) {
+          const int had = pages_of(a, rows[s]);
+          page = j < had ? a.tables[(int64_t)s * a.max_pages + j] : page_at(base + taken[s] + (j - had));
+          seg = s;
+          entry = j;
+        }
+        const int64_t slot = ((int64_t)page << a.page_shift) + (pos & in_page);
+        out[e] = slot < 0 || slot > 0x7FFFFFFF ? -1 : (int32_t)slot;
+      }
+      if (++h == per_row) {
+        h = 0;
+        ++item;
+      }
+    }
+    if (at + 4 <= n) {
+      *reinterpret_cast<int4*>(a.slots + at) = make_int4(out[0], out[1], out[2], out[3]);
+    } else {
+      for (int e = 0; e < 4 && at + e < n; ++e) a.slots[at + e] = out[e];
+    }
   }
 }
 
@@ -361,16 +357,18 @@ __global__ __launch_bounds__(kPageBlock) void norm_rope_kernel(NormRopeArgs a) {
 }  // namespace
 
 hipError_t launch_page_update(const PageArgs& a, int cus, hipStream_t stream) {
-  const size_t lds = ((size_t)(a.by_segment ? a.S : a.B) + 2 * (size_t)a.S + 3) * sizeof(int32_t);
-  const int64_t items = a.num_slots * (a.by_segment ? 1 : a.Hkv);
-  // one workgroup up to 4 rounds of slots
-  int64_t wgs = (items + 4 * kPageBlock * 4 - 1) / (4 * kPageBlock * 4);
-  if (wgs < 1) wgs = 1;
-  if (wgs > cus) wgs = cus;
-  const int single = wgs == 1;
+  const size_t lds = (3 * (size_t)a.S + (a.by_segment ? a.S : a.B) + 3) * sizeof(int32_t);
+  // One workgroup per four rounds of slots, up to two per compute unit. How many pages change hands is known
+  // on the device only, at most all table entries: one workgroup per 4096 of those, up to 64.
+  const int64_t rounds = (a.num_slots * (a.by_segment ? 1 : a.Hkv) + 4 * kPageBlock - 1) / (4 * kPageBlock);
+  const int64_t entries = (int64_t)a.S * a.max_pages;
+  const int wgs = (int)std::max({(int64_t)1, std::min<int64_t>((rounds + 3) / 4, 2 * cus),
+                                 std::min<int64_t>(entries / 4096, 64)});
+  const bool in_place = a.rows_out == a.rows || a.head_out == a.head;
+  const bool second = wgs > 1 && in_place;
   prof_begin("page_update", stream);
-  page_update_kernel<false><<<dim3((unsigned)wgs), dim3(kPageBlock), lds, stream>>>(a, single);
-  if (!single) page_update_kernel<true><<<dim3(1), dim3(kPageBlock), lds, stream>>>(a, 0);
+  page_update_kernel<false><<<dim3(wgs), dim3(kPageBlock), lds, stream>>>(a, !second);
+  if (second) page_update_kernel<true><<<dim3(1), dim3(kPageBlock), lds, stream>>>(a, 1);
   prof_end(stream);
   return hipGetLastError();
 }

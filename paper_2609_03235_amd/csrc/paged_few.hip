@@ -5,6 +5,8 @@
 // the workgroup's 128 key rows per step on its own (no barrier in the loop): keys go from memory straight
 // into the MFMA's A layout, values through 32 rows of LDS that only this wave uses, for the transposing
 // read. The next step's rows are in flight while a step is computed.
+#include <algorithm>
+
 #include "paged_attention.h"
 
 namespace sgdkv {
@@ -60,6 +62,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
   const int w = worker_of(a);
   int64_t total, share = 0, pos = 0;
   LineTile at;
+  if (tid == 0) a.shared[w] = make_int4(0, 0, -1, 0);
   if (!find_tile(a, sc, total, [&](int64_t all) {
         share = share_of(a, all);
         pos = share * w;
@@ -262,79 +265,70 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
       }
       __syncthreads();
     }
-    at.start += max(limit, 1);
+    const int64_t next = at.start + max(limit, 1);
+    if (next >= end) leave_shared(a, w, share, at, nkt);
+    at.start = pos = next;
     ++at.tile;
-    pos = at.start;
   }
 }
 
-// Joins the parts of the query tiles that several workers shared. Workgroup (w, y) looks at the tile that
-// worker w began and left to the next ones, if any, and joins rows y, y + gridDim.y, ... of it: groups of
-// D / 4 lanes take the parts in turn with a running maximum, then the groups are joined in order.
-template <int D>
+// Joins the parts of the query tiles that several workers shared: workgroup (w, y) looks at the tile that
+// worker w began and left to the next ones, if any. Lanes in groups of D / 4 hold a row, four columns each.
+//   MANY = false: tiles of few rows and up to hundreds of parts. A workgroup takes one row; the groups take its
+//     parts in turn with a running maximum and are then joined in order.
+//   MANY = true: tiles of many rows and seldom more than three parts. A group takes a row of its own (the rows
+//     one after the other with the groups on the parts took 17 us for what takes 5 so).
+template <int D, bool MANY>
 __global__ __launch_bounds__(kAttnBlock) void paged_merge_kernel(PagedAttnArgs a) {
-  const int M = a.tile_rows, key_tile = a.key_tile;
   constexpr int LPS = D / 4, NG = kAttnBlock / LPS;
-  __shared__ LineScratch sc;
   __shared__ float ms[NG], ss[NG];
   __shared__ __attribute__((aligned(16))) float os[NG][D];
   const int tid = threadIdx.x, grp = tid / LPS, col = 4 * (tid % LPS);
   const int w = blockIdx.x;
-  int64_t total, share = 0, x = 0;
-  LineTile at;
-  if (!find_tile(a, sc, total, [&](int64_t all) {
-        share = share_of(a, all);
-        x = share * (w + 1);
-        return x;
-      }, at))
-    return;
-  if (at.start == x || at.start < share * w) return;  // begins with the next worker, or began before this one
-  const PagedSeg g = paged_seg(a, at.seg);
-  const int limit = uniform(tile_rows(a, g, at.tile));
-  const int nkt = max((limit + key_tile - 1) / key_tile, 1);
-  const int last = (int)((at.start + (int64_t)(nkt - 1) * key_tile) / share);
-  if (last == w) return;
-  const int h = at.seg % a.Hkv, tok0 = at.tile * a.tokens;
-  const int nrow = min(a.tokens, g.n - tok0) * a.G, parts = last - w + 1;
-  for (int r = blockIdx.y; r < nrow; r += gridDim.y) {
-    float m = -INFINITY, s = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int i = grp; i < parts; i += NG) {
-      const int64_t at_slot = (2 * (int64_t)(w + i) + (at.start > share * (w + i) ? 1 : 0)) * M + r;
-      const float pm = a.part_ms[at_slot * 2], ps = a.part_ms[at_slot * 2 + 1];
-      const f32x4 po = *reinterpret_cast<const f32x4*>(a.part + at_slot * D + col);
-      const float mn = fmaxf(m, pm), ref = mn == -INFINITY ? 0.f : mn;
-      const float fo = fast_exp2(m - ref), fn = fast_exp2(pm - ref);
-      m = mn;
-      s = s * fo + ps * fn;
-      o = o * fo + po * fn;
-    }
-    __syncthreads();
+  const int4 left = a.shared[w];
+  if (left.z < 0) return;
+  const PagedSeg g = paged_seg(a, left.x);
+  const int M = a.tile_rows, h = left.x % a.Hkv, tok0 = left.y * a.tokens;
+  const int nrow = min(a.tokens, g.n - tok0) * a.G, parts = left.z - w + 1;
+  const int r = MANY ? blockIdx.y * NG + grp : blockIdx.y;
+  if (r >= nrow) return;
+  float m = -INFINITY, s = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int i = MANY ? 0 : grp; i < parts; i += MANY ? 1 : NG) {
+    const int64_t at = (2 * (int64_t)(w + i) + (i == 0 ? left.w : 0)) * M + r;
+    const float pm = a.part_ms[at * 2], ps = a.part_ms[at * 2 + 1];
+    const f32x4 po = *reinterpret_cast<const f32x4*>(a.part + at * D + col);
+    const float mn = fmaxf(m, pm), ref = mn == -INFINITY ? 0.f : mn;
+    const float fo = fast_exp2(m - ref), fn = fast_exp2(pm - ref);
+    m = mn;
+    s = s * fo + ps * fn;
+    o = o * fo + po * fn;
+  }
+  if (!MANY) {
     if (col == 0) {
       ms[grp] = m;
       ss[grp] = s;
     }
     *reinterpret_cast<f32x4*>(&os[grp][col]) = o;
     __syncthreads();
-    if (grp == 0) {
-      float mm = -INFINITY;
+    if (grp != 0) return;
+    m = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < NG; ++i) mm = fmaxf(mm, ms[i]);
-      const float ref = mm == -INFINITY ? 0.f : mm;
-      float sum = 0.f;
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < NG; ++i) m = fmaxf(m, ms[i]);
+    const float ref = m == -INFINITY ? 0.f : m;
+    s = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        const float f = fast_exp2(ms[i] - ref);
-        sum += ss[i] * f;
-        acc += *reinterpret_cast<const f32x4*>(&os[i][col]) * f;
-      }
-      const int tok = r / a.G, hd = r - tok * a.G;
-      const int64_t row = (int64_t)(g.t0 + tok0 + tok) * a.Hq + h * a.G + hd;
-      store_out4(a, row, D, col, acc * (sum == 0.f ? 0.f : 1.0f / sum));
-      if (a.lse && col == 0) a.lse[row] = lse_of(mm, sum);
+    for (int i = 0; i < NG; ++i) {
+      const float f = fast_exp2(ms[i] - ref);
+      s += ss[i] * f;
+      o += *reinterpret_cast<const f32x4*>(&os[i][col]) * f;
     }
   }
+  const int tok = r / a.G, hd = r - tok * a.G;
+  const int64_t row = (int64_t)(g.t0 + tok0 + tok) * a.Hq + h * a.G + hd;
+  store_out4(a, row, D, col, o * (s == 0.f ? 0.f : 1.0f / s));
+  if (a.lse && col == 0) a.lse[row] = lse_of(m, s);
 }
 
 template <typename T, int D, int QB>
@@ -373,9 +367,16 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream) {
   prof_end(stream);
   if (e != hipSuccess || a.workers == 1) return e;  // one worker shares no tile
   prof_begin("paged_merge", stream);
-  const dim3 grid(a.workers, a.tile_rows <= 32 ? a.tile_rows : 16);
-  if (a.D == 128) paged_merge_kernel<128><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
-  else paged_merge_kernel<64><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
+  if (a.tile_rows <= 32) {
+    const dim3 grid(a.workers, std::min(a.max_new, a.tokens) * a.G);
+    if (a.D == 128) paged_merge_kernel<128, false><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
+    else paged_merge_kernel<64, false><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
+  } else {
+    const int per = kAttnBlock / (a.D / 4);  // rows of a workgroup
+    const dim3 grid(a.workers, (std::min(a.max_new, a.tokens) * a.G + per - 1) / per);
+    if (a.D == 128) paged_merge_kernel<128, true><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
+    else paged_merge_kernel<64, true><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
+  }
   prof_end(stream);
   return hipGetLastError();
 }

@@ -88,9 +88,6 @@ sgdkv_status launched(hipError_t e, const char* what) {
 // depend on the device.
 constexpr int kPagedWorkers = 512;
 
-// Key rows a worker takes at least.
-constexpr int64_t kPagedMinCost = 256;
-
 sgdkv_status plan_paged(const sgdkv_page_pool* pool, const sgdkv_paged_desc* d, sgdkv::PagedAttnArgs& a,
                         size_t& bytes) {
   if (sgdkv_status st = check_pool_shape(pool)) return st;
@@ -121,6 +118,7 @@ sgdkv_status plan_paged(const sgdkv_page_pool* pool, const sgdkv_paged_desc* d, 
   a.G = G;
   a.D = pool->head_dim;
   a.S = (int)nseg;
+  a.inv_hkv = ((uint64_t(1) << 32) + a.Hkv - 1) / a.Hkv;
   a.T = (int)d->num_tokens;
   a.dtype = pool->dtype;
   a.out_dtype = d->out_dtype;
@@ -129,15 +127,15 @@ sgdkv_status plan_paged(const sgdkv_page_pool* pool, const sgdkv_paged_desc* d, 
   a.max_new = (int)std::min<int64_t>(d->max_new, std::max<int64_t>(d->num_tokens, 1));
   const double scale = d->scale == 0.f ? 1.0 / std::sqrt((double)a.D) : (double)d->scale;
   a.c2 = (float)(scale * 1.4426950408889634074);
-  a.min_cost = kPagedMinCost;
   const sgdkv::PagedAttnShape shape = sgdkv::paged_attn_shape(a.dtype, G, a.max_new);
   a.tile_rows = shape.rows;
   a.key_tile = shape.key_tile;
   a.tokens = shape.rows / G;
   a.workers = kPagedWorkers;
+  a.min_cost = shape.rows <= 32 ? shape.key_tile : 2 * shape.key_tile;
   // The workspace follows the bound the caller gave, whatever the tokens of this call.
   const int most_rows = sgdkv::paged_attn_shape(a.dtype, G, d->max_new).rows;
-  bytes = 2 * (size_t)kPagedWorkers * most_rows * (a.D + 2) * sizeof(float);
+  bytes = (size_t)kPagedWorkers * (sizeof(int4) + 2 * (size_t)most_rows * (a.D + 2) * sizeof(float));
   return SGDKV_OK;
 }
 
@@ -158,6 +156,8 @@ sgdkv_status sgdkv_page_update(const sgdkv_page_desc* desc, const int32_t* rows,
   if (sgdkv_status st = check_page_size(desc->page_size)) return st;
   if (desc->max_pages < 1 || desc->max_pages > kMaxInt / desc->page_size)
     return fail(SGDKV_ERR_INVALID_ARG, "max_pages %d outside [1, (2^31 - 1) / page_size]", desc->max_pages);
+  if (nseg * desc->max_pages > kMaxInt)
+    return fail(SGDKV_ERR_UNSUPPORTED, "%lld segments of %d table columns", (long long)nseg, desc->max_pages);
   if (desc->by_segment != 0 && desc->by_segment != 1)
     return fail(SGDKV_ERR_INVALID_ARG, "by_segment %d is not 0 or 1", desc->by_segment);
   if (desc->num_free < 1 || desc->num_free > kMaxInt)
@@ -342,7 +342,8 @@ sgdkv_status sgdkv_paged_attention(const sgdkv_page_pool* pool, const sgdkv_page
   a.cu = cu_new;
   a.out = out;
   a.lse = lse_out;
-  a.part = static_cast<float*>(workspace);
+  a.shared = static_cast<int4*>(workspace);
+  a.part = reinterpret_cast<float*>(a.shared + a.workers);
   a.part_ms = a.part + 2 * (size_t)a.workers * a.tile_rows * a.D;
   (void)hipGetLastError();
   return launched(sgdkv::launch_paged_attention(a, stream_of(stream)), "paged attention");

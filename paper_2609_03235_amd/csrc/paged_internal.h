@@ -9,7 +9,7 @@
 namespace sgdkv {
 
 constexpr int kPageBlock = 256;       // threads per workgroup of the page and row kernels
-constexpr int kMaxPageSegs = 4096;    // segments of one page update (their three prefix sums fill 48 KB of LDS)
+constexpr int kMaxPageSegs = 4096;    // segments of one page update (their lengths and prefix sums fill 64 KB of LDS)
 constexpr int kMinPage = 16;          // rows per page: every 16-row group of a segment lies in one page
 constexpr int kMaxPage = 1024;
 constexpr int kMaxPagedGroup = 16;    // query heads per KV head
@@ -76,6 +76,7 @@ struct PagedAttnArgs {
   int page_shift, max_pages, max_new;
   int64_t num_pages;
   float c2;          // scale * log2(e)
+  uint64_t inv_hkv;  // ceil(2^32 / Hkv): seg * inv_hkv >> 32 is seg / Hkv for seg below 65536
   int tile_rows;     // query rows per tile (M)
   int key_tile;      // key rows per step of a workgroup (KT)
   int tokens;        // new tokens per query tile
@@ -89,6 +90,9 @@ struct PagedAttnArgs {
   const int32_t* cu;
   void* out;
   float* lse;        // optional
+  // workspace
+  int4* shared;      // [workers]: the query tile that a worker began and left to the next ones: segment, tile,
+                     // the last worker (-1: none) and 1 if the tile starts after the worker's share does
   float* part;       // [2 * workers][M][D]: o of a query tile that several workers share
   float* part_ms;    // [2 * workers][M][2]
 };

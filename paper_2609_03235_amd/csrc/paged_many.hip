@@ -39,6 +39,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
   const int w = worker_of(a);
   int64_t total, share = 0, pos = 0;
   LineTile at;
+  if (tid == 0) a.shared[w] = make_int4(0, 0, -1, 0);
   if (!find_tile(a, sc, total, [&](int64_t all) {
         share = share_of(a, all);
         pos = share * w;
@@ -266,9 +267,10 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
         }
       }
     }
-    at.start += max(limit, 1);
+    const int64_t next = at.start + max(limit, 1);
+    if (next >= end) leave_shared(a, w, share, at, nkt);
+    at.start = pos = next;
     ++at.tile;
-    pos = at.start;
   }
 }
 

@@ -638,3 +638,12 @@ def test_another_stream():
     out, _ = c.call(stream=side.cuda_stream)
     side.synchronize()
     assert torch.equal(out, want)
+
+
+def test_page_update_of_the_most_segments():
+    """4096 segments by segment: lengths and prefix sums fill the most LDS a call takes."""
+    _say("page_update 4096 segments")
+    rows = [(i * 13) % 40 for i in range(4096)]
+    add = [(i * 29) % 50 - 12 for i in range(4096)]
+    tables, free, head = _start(rows, 16, 6, 20000, 2)
+    _update_both(rows, add, tables, free, head, 16, sum(max(x, 0) for x in add) + 3, 1, True)
