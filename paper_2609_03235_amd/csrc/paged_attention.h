@@ -81,58 +81,82 @@ __device__ __forceinline__ int64_t uniform(int64_t v) {
   return (int64_t)(((uint64_t)hi << 32) | lo);
 }
 
-// A place on the line: a tile and where it starts.
+// A place on the line: a tile, its segment, and where it starts.
 struct LineTile {
   int seg, tile;
   int64_t start;
+  PagedSeg g;
 };
 
 struct LineScratch {
-  int64_t wave_sum[kAttnWaves];
+  int64_t wave_sum[kAttnWaves][2];
   int64_t start;
   int seg;
+  PagedSeg g;
 };
 
-// Adds the segments up (the whole workgroup); total = the line's length. Then finds the tile that holds
-// place x (the same for every thread) where x < total. The total decides a worker's share, so x comes from
-// place(total).
-template <typename F>
-__device__ __forceinline__ bool find_tile(const PagedAttnArgs& a, LineScratch& sc, int64_t& total, F place,
-                                          LineTile& at) {
+__device__ __forceinline__ PagedSeg uniform(const PagedSeg& g) {
+  return PagedSeg{uniform(g.t0), uniform(g.n), uniform(g.rows), uniform(g.base), uniform(g.tiles)};
+}
+
+// The whole workgroup adds the segments up and finds worker w's piece of the line, [at.., end): false if there
+// is none. share receives the pieces' length: an equal part, at least min_cost.
+// PAD (segments of one tile): where all workers' least pieces cover the segments rounded up to whole pieces,
+// the line is that, and no worker has parts of two tiles. Short calls are bound by latency: one token over four
+// segments of 8K rows took 14.9 us with, 9 without the three workers that had two.
+template <bool PAD>
+__device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, LineScratch& sc, int w, int64_t& share,
+                                           int64_t& end, bool& padded, LineTile& at) {
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
   const int per = (a.S + kAttnBlock - 1) / kAttnBlock;
   const int s0 = min(tid * per, a.S), s1 = min(s0 + per, a.S);
-  int64_t mine = 0;
+  int64_t mine[2] = {0, 0};
+  PagedSeg g{};
+  auto pad = [&](int64_t c) { return (c + a.min_cost - 1) & ~(a.min_cost - 1); };  // min_cost is a power of two
   for (int s = s0; s < s1; ++s) {
-    const PagedSeg g = paged_seg(a, s);
-    mine += cost_of(a, g, g.tiles);
+    g = paged_seg(a, s);
+    const int64_t c = cost_of(a, g, g.tiles);
+    mine[0] += c;
+    if (PAD) mine[1] += pad(c);
   }
-  int64_t x = mine;
+  int64_t before[2], total[2] = {0, 0};
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up((long long)x, o, 64);
-    if (lane >= o) x += y;
+  for (int k = 0; k < (PAD ? 2 : 1); ++k) {
+    int64_t x = mine[k];
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t y = __shfl_up((long long)x, o, 64);
+      if (lane >= o) x += y;
+    }
+    if (lane == 63) sc.wave_sum[wid][k] = x;
+    before[k] = x - mine[k];
   }
-  if (lane == 63) sc.wave_sum[wid] = x;
   __syncthreads();
-  int64_t before = x - mine;
-  total = 0;
 #pragma unroll
-  for (int w = 0; w < kAttnWaves; ++w) {
-    if (w < wid) before += sc.wave_sum[w];
-    total += sc.wave_sum[w];
-  }
-  total = uniform(total);
-  const int64_t want = place(total);
-  if (want >= total) return false;
-  if (want >= before && want < before + mine) {
-    int64_t run = before;
+  for (int k = 0; k < (PAD ? 2 : 1); ++k)
+#pragma unroll
+    for (int i = 0; i < kAttnWaves; ++i) {
+      const int64_t y = sc.wave_sum[i][k];
+      if (i < wid) before[k] += y;
+      total[k] += y;
+    }
+  padded = PAD && total[1] <= a.workers * a.min_cost;
+  const int64_t all = uniform(padded ? total[1] : total[0]);
+  share = uniform((all + a.workers - 1) / a.workers);
+  if (share < a.min_cost) share = a.min_cost;
+  const int64_t want = share * w;
+  if (want >= all) return false;
+  end = min(want + share, all);
+  int64_t run = padded ? before[1] : before[0];
+  if (want >= run && want < run + (padded ? mine[1] : mine[0])) {
     for (int s = s0; s < s1; ++s) {
-      const PagedSeg g = paged_seg(a, s);
-      const int64_t c = cost_of(a, g, g.tiles);
+      if (per > 1) g = paged_seg(a, s);
+      int64_t c = cost_of(a, g, g.tiles);
+      if (padded) c = pad(c);
       if (want < run + c) {
         sc.seg = s;
         sc.start = run;
+        sc.g = g;
         break;
       }
       run += c;
@@ -140,16 +164,16 @@ __device__ __forceinline__ bool find_tile(const PagedAttnArgs& a, LineScratch& s
   }
   __syncthreads();
   at.seg = uniform(sc.seg);
+  at.g = uniform(sc.g);
   const int64_t seg_start = uniform(sc.start);
-  const PagedSeg g = paged_seg(a, at.seg);
-  int lo = 0, hi = g.tiles;  // the last tile that starts at or before `want`
+  int lo = 0, hi = at.g.tiles;  // the last tile that starts at or before `want`
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (seg_start + cost_of(a, g, mid) <= want) lo = mid;
+    if (seg_start + cost_of(a, at.g, mid) <= want) lo = mid;
     else hi = mid;
   }
   at.tile = uniform(lo);
-  at.start = uniform(seg_start + cost_of(a, g, lo));
+  at.start = uniform(seg_start + cost_of(a, at.g, lo));
   return true;
 }
 
@@ -159,12 +183,6 @@ __device__ __forceinline__ void leave_shared(const PagedAttnArgs& a, int w, int6
   const int last = (int)((at.start + (int64_t)(nkt - 1) * a.key_tile) / share);
   const bool left = at.start >= own && last > w;
   if (threadIdx.x == 0) a.shared[w] = make_int4(at.seg, at.tile, left ? last : -1, at.start > own ? 1 : 0);
-}
-
-// A worker's share of the line: at least min_cost key rows.
-__device__ __forceinline__ int64_t share_of(const PagedAttnArgs& a, int64_t total) {
-  const int64_t q = (total + a.workers - 1) / a.workers;
-  return q < a.min_cost ? a.min_cost : q;
 }
 
 // Neighbouring workers on one XCD (workgroups go to the eight XCDs in turn): they read the same segment's

@@ -50,7 +50,8 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
   constexpr int EB = S::EB, RB = S::RB, NC = S::NC, ND = D / 16;
   constexpr int VP = EB == 2 ? RB + 16 : RB + 16;  // pitch of a value row in LDS
   constexpr int kStage = kStep * VP;
-  constexpr int kMerge = 16 * QB * D * 4;
+  constexpr int OP = D + 4;  // pitch of a row of o in LDS, in floats: the rows' writes spread over the banks
+  constexpr int kMerge = 16 * QB * OP * 4;
   constexpr int kWaveLds = kStage > kMerge ? kStage : kMerge;
   __shared__ __attribute__((aligned(16))) char lds[kAttnWaves][kWaveLds];
   __shared__ float mws[kAttnWaves][16 * QB], sws[kAttnWaves][16 * QB];
@@ -60,25 +61,22 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
   const int tid = threadIdx.x, wid = uniform(tid >> 6), lane = tid & 63;
   const int lr = lane & 15, lg = lane >> 4;
   const int w = worker_of(a);
-  int64_t total, share = 0, pos = 0;
+  int64_t share, end;
+  bool padded;
   LineTile at;
   if (tid == 0) a.shared[w] = make_int4(0, 0, -1, 0);
-  if (!find_tile(a, sc, total, [&](int64_t all) {
-        share = share_of(a, all);
-        pos = share * w;
-        return pos;
-      }, at))
-    return;
-  const int64_t end = min(pos + share, total);
+  if (!find_piece<true>(a, sc, w, share, end, padded, at)) return;
+  int64_t pos = share * w;
   char* stage = lds[wid];
 
-  while (pos < end && at.seg < a.S) {
-    const PagedSeg g = paged_seg(a, at.seg);
-    if (at.tile >= g.tiles) {  // the next segment
-      ++at.seg;
+  while (pos < end) {
+    if (at.tile >= at.g.tiles) {  // the next segment
+      if (++at.seg >= a.S) return;
       at.tile = 0;
+      at.g = paged_seg(a, at.seg);
       continue;
     }
+    const PagedSeg& g = at.g;
     const int limit = uniform(tile_rows(a, g, at.tile));
     const int nkt = max((limit + kTile - 1) / kTile, 1);
     const int j0 = (int)((pos - at.start + kTile - 1) / kTile);
@@ -229,7 +227,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
         }
 #pragma unroll
         for (int d = 0; d < ND; ++d)
-          *reinterpret_cast<f32x4*>(stage + ((16 * qb + lr) * D + 16 * d + 4 * lg) * 4) = o[qb][d];
+          *reinterpret_cast<f32x4*>(stage + ((16 * qb + lr) * OP + 16 * d + 4 * lg) * 4) = o[qb][d];
       }
       __syncthreads();
       const bool whole = j0 == 0 && j1 == nkt;
@@ -247,7 +245,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
         for (int x = 0; x < kAttnWaves; ++x) {
           const float f = fast_exp2(mws[x][r] - ref);
           sum = fmaf(sws[x][r], f, sum);
-          acc += f * *reinterpret_cast<const f32x4*>(lds[x] + (r * D + col) * 4);
+          acc += f * *reinterpret_cast<const f32x4*>(lds[x] + (r * OP + col) * 4);
         }
         if (whole) {
           const int tok = r / a.G, hd = r - tok * a.G;
@@ -265,7 +263,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
       }
       __syncthreads();
     }
-    const int64_t next = at.start + max(limit, 1);
+    const int64_t next = padded ? end : at.start + max(limit, 1);
     if (next >= end) leave_shared(a, w, share, at, nkt);
     at.start = pos = next;
     ++at.tile;

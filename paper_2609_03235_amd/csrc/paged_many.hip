@@ -37,24 +37,21 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
   const int tid = threadIdx.x, wid = uniform(tid >> 6), lane = tid & 63;
   const int lq = lane & 31, half = lane >> 5;
   const int w = worker_of(a);
-  int64_t total, share = 0, pos = 0;
+  int64_t share, end;
+  bool padded;
   LineTile at;
   if (tid == 0) a.shared[w] = make_int4(0, 0, -1, 0);
-  if (!find_tile(a, sc, total, [&](int64_t all) {
-        share = share_of(a, all);
-        pos = share * w;
-        return pos;
-      }, at))
-    return;
-  const int64_t end = min(pos + share, total);
+  if (!find_piece<false>(a, sc, w, share, end, padded, at)) return;
+  int64_t pos = share * w;
 
-  while (pos < end && at.seg < a.S) {
-    const PagedSeg g = paged_seg(a, at.seg);
-    if (at.tile >= g.tiles) {
-      ++at.seg;
+  while (pos < end) {
+    if (at.tile >= at.g.tiles) {  // the next segment
+      if (++at.seg >= a.S) return;
       at.tile = 0;
+      at.g = paged_seg(a, at.seg);
       continue;
     }
+    const PagedSeg& g = at.g;
     const int limit = uniform(tile_rows(a, g, at.tile));
     const int nkt = max((limit + KT - 1) / KT, 1);
     const int j0 = (int)((pos - at.start + KT - 1) / KT);
