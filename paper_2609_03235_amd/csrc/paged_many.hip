@@ -1,37 +1,100 @@
 // Paged attention for many query rows per KV head (chunks of new tokens). See paged_attention.h.
 //
 // A workgroup holds 128 query rows, 32 per wave, and walks the keys of its piece of the line in tiles that
-// all four waves share through LDS (two buffers, one barrier per tile; the tile after the next is in flight
-// in registers). Products are 32x32 MFMAs. Every row keeps a reference for its exponentials that only moves
-// when a tile's sum shows that it fell too far behind, so a logit costs one fma, one exp2 and one add.
+// all four waves share through LDS: two buffers, one barrier per tile, and the next tile on its way from memory
+// straight into LDS while one is computed (no registers, no LDS writes). Products are 32x32 MFMAs. Every row
+// keeps a reference for its exponentials that only moves when a tile's sum shows that it fell too far behind,
+// so a logit costs one fma, one exp2 and one add.
+#include <type_traits>
+
 #include "paged_attention.h"
 
 namespace sgdkv {
 
 namespace {
 
+// Rows in LDS have no padding (a load writes its lanes' 16 bytes one after the other); the 16-byte pieces of a
+// row change places instead, piece c of row r lying at place c ^ key_swizzle(r) (value_swizzle): reads of one
+// piece of 16 rows, or of four pieces of four rows, touch every bank once.
 template <typename T, int D>
 struct ManyShape {
   static constexpr int EB = sizeof(T), RB = D * EB;
   static constexpr int KT = EB == 2 ? 64 : 32;    // keys per tile
   static constexpr int RPW = KT / kAttnWaves;     // rows a wave loads
   static constexpr int VPR = RB / 16, RPL = 64 / VPR, NL = RPW / RPL;  // rows per load, loads per wave
-  static constexpr int KP = RB + 16;                   // pitch of a key row in LDS
-  static constexpr int VP = EB == 2 ? RB + 64 : RB + 16;  // pitch of a value row
   static constexpr int NK = KT / 32, ND = D / 32;
   static constexpr int NC = EB == 2 ? D / 16 : D / 8;  // 16-byte operand pieces of a row per lane half
-  static constexpr int LDS = KT * (KP + VP);
+  static constexpr int TILE = KT * RB;
+  static __device__ __forceinline__ int key_swizzle(int r) { return RB == 128 ? (r >> 1) & 7 : r & 15; }
+  static __device__ __forceinline__ int value_swizzle(int r) {
+    return EB == 4 ? ((r >> 2) & 1) << 3 : (RB == 128 ? ((r >> 1) & 1) << 2 : (r & 3) << 2);
+  }
 };
+
+// 64 x 16 bytes from a buffer into LDS at lds + 16 * lane; out-of-range lanes write zeros. The compiler does not
+// see this load: wait_loads() before the barrier after which other waves read.
+__device__ __forceinline__ void load_to_lds(u32x4 rsrc, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rsrc)
+               : "memory");
+}
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// The buffer of group_rsrc as four scalar words.
+__device__ __forceinline__ u32x4 group_words(const PagedAttnArgs& a, const void* pool, int page, int r0, int valid,
+                                             int rows, int row_bytes) {
+  const bool ok = page >= 0 && page < a.num_pages && valid > 0;
+  const int64_t row = ok ? ((int64_t)page << a.page_shift) + (r0 & ((1 << a.page_shift) - 1)) : 0;
+  const uint64_t p = reinterpret_cast<uint64_t>(pool) + row * row_bytes;
+  return u32x4{(uint32_t)uniform((int)p), (uint32_t)uniform((int)(p >> 32)),
+               (uint32_t)uniform(ok ? min(valid, rows) * row_bytes : 0), (uint32_t)kRsrcWord3};
+}
 
 // Reference kept while a tile's sum of exponentials stays below this.
 constexpr float kFar = 1024.f;
+
+// A tile's probabilities of one lane, as the operand of the product with the values.
+template <typename T, bool FINE, int NK>
+struct Probs;
+template <int NK>
+struct Probs<float, false, NK> {
+  float v[NK][16];
+  __device__ __forceinline__ void set(int n, int i, float x, float y) {
+    v[n][i] = x;
+    v[n][i + 1] = y;
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int n = 0; n < NK; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[n][i] = 0.f;
+  }
+};
+template <bool FINE, int NK>
+struct Probs<__bf16, FINE, NK> {
+  u32x4 hi[2 * NK], lo[FINE ? 2 * NK : 1];  // piece t: keys 16t .. 16t + 15 in the accumulator's order
+  __device__ __forceinline__ void set(int n, int i, float x, float y) {
+    const uint32_t w = pack_bf16(x, y);
+    hi[2 * n + i / 8][(i % 8) / 2] = w;
+    if (FINE) lo[2 * n + i / 8][(i % 8) / 2] = pack_bf16_rest(x, y, w);
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int t = 0; t < 2 * NK; ++t) hi[t] = u32x4{0, 0, 0, 0};
+    if (FINE) {
+#pragma unroll
+      for (int t = 0; t < 2 * NK; ++t) lo[t] = u32x4{0, 0, 0, 0};
+    }
+  }
+  __device__ __forceinline__ bf16x8 piece(int t) const { return __builtin_bit_cast(bf16x8, hi[t]); }
+  __device__ __forceinline__ bf16x8 rest(int t) const { return __builtin_bit_cast(bf16x8, lo[FINE ? t : 0]); }
+};
 
 template <typename T, int D, bool FINE>
 __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs a) {
   using S = ManyShape<T, D>;
   constexpr int EB = S::EB, RB = S::RB, KT = S::KT, NC = S::NC, NK = S::NK, ND = S::ND, NL = S::NL;
-  constexpr int KP = S::KP, VP = S::VP, M = 128;
-  __shared__ __attribute__((aligned(16))) char lds[2][S::LDS];
+  constexpr int M = 128;
+  __shared__ __attribute__((aligned(16))) char lds[2][2][S::TILE];  // two buffers of keys and values
   __shared__ LineScratch sc;
 
   const int tid = threadIdx.x, wid = uniform(tid >> 6), lane = tid & 63;
@@ -43,6 +106,17 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
   if (tid == 0) a.shared[w] = make_int4(0, 0, -1, 0);
   if (!find_piece<false>(a, sc, w, share, end, padded, at)) return;
   int64_t pos = share * w;
+
+  // where this lane's 16 bytes of each load come from, within the wave's rows
+  const int my_row = wid * S::RPW;
+  uint32_t koff[NL], voff[NL];
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    const int r = i * S::RPL + lane / S::VPR, c = lane % S::VPR;
+    koff[i] = r * RB + (c ^ S::key_swizzle(my_row + r)) * 16;
+    voff[i] = r * RB + (c ^ S::value_swizzle(my_row + r)) * 16;
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)&lds[0][0][0];
 
   while (pos < end) {
     if (at.tile >= at.g.tiles) {  // the next segment
@@ -56,8 +130,8 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
     const int nkt = max((limit + KT - 1) / KT, 1);
     const int j0 = (int)((pos - at.start + KT - 1) / KT);
     const int j1 = (int)min((int64_t)nkt, (end - at.start + KT - 1) / KT);
-    const int h = at.seg % a.Hkv;
     if (j0 < j1) {
+      const int h = at.seg % a.Hkv;
       const int tok0 = at.tile * a.tokens, ntok = min(a.tokens, g.n - tok0);
       const int nrow = ntok * a.G;
       const int r = wid * 32 + lq, tok = r / a.G, hd = r - tok * a.G;
@@ -66,7 +140,20 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
       // the rows of this wave see between lo and hi keys
       const bool any_row = wid * 32 < nrow;
       const int lo = any_row ? uniform(seen) : 0;
-      const int hi = any_row ? seen_by(a, g, tok0 + (min(nrow, wid * 32 + 32) - 1) / a.G) : 0;
+      const int hi = any_row ? uniform(seen_by(a, g, tok0 + (min(nrow, wid * 32 + 32) - 1) / a.G)) : 0;
+
+      const int32_t* table = a.tables + (int64_t)at.seg * a.max_pages;
+      int page = uniform(group_page(a, table, j0 * KT + my_row, limit));
+      auto load = [&](int j) {
+        const int r0 = j * KT + my_row;
+        const u32x4 kr = group_words(a, a.k_pages, page, r0, limit - r0, S::RPW, RB);
+        const u32x4 vr = group_words(a, a.v_pages, page, r0, limit - r0, S::RPW, RB);
+        const uint32_t to = uniform((int)(lds0 + (j & 1) * 2 * S::TILE + my_row * RB));
+#pragma unroll
+        for (int i = 0; i < NL; ++i) load_to_lds(kr, koff[i], to + i * 1024);
+#pragma unroll
+        for (int i = 0; i < NL; ++i) load_to_lds(vr, voff[i], to + S::TILE + i * 1024);
+      };
       u32x4 q[NC];
       {
         const rsrc_t qr = make_rsrc(static_cast<const char*>(a.q) + ((int64_t)(g.t0 + tok0) * a.Hq + h * a.G) * RB,
@@ -82,158 +169,125 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
-      const int32_t* table = a.tables + (int64_t)at.seg * a.max_pages;
-      u32x4 kreg[NL], vreg[NL];
-      int page;
-      const int my_row = wid * S::RPW;
-      auto find_page = [&](int j) { page = uniform(group_page(a, table, j * KT + my_row, limit)); };
-      auto load = [&](int j) {
-        const int r0 = j * KT + my_row, valid = min(limit - r0, S::RPW);
-        const rsrc_t kr = group_rsrc(a, a.k_pages, page, r0, valid, RB);
-        const rsrc_t vr = group_rsrc(a, a.v_pages, page, r0, valid, RB);
+      // One tile of keys from LDS. EDGE: some row does not see all of it; `left` is how many of the keys from
+      // 4 * half on this lane's row sees.
+      auto attend = [&](const char* kb, auto edge, int left) {
+        constexpr bool EDGE = decltype(edge)::value;
+        const char* vb = kb + S::TILE;
+        f32x16 y[NK];
+        const int ksw = S::key_swizzle(lq);  // of every block's row: 32 rows on it repeats
 #pragma unroll
-        for (int i = 0; i < NL; ++i) kreg[i] = ld128(kr, (uint32_t)(i * 1024 + lane * 16));
+        for (int n = 0; n < NK; ++n) {
 #pragma unroll
-        for (int i = 0; i < NL; ++i) vreg[i] = ld128(vr, (uint32_t)(i * 1024 + lane * 16));
-      };
-      auto stage = [&](char* buf) {
-        const int row = my_row + lane / S::VPR, col = (lane % S::VPR) * 16;
+          for (int i = 0; i < 16; ++i) y[n][i] = 0.f;
 #pragma unroll
-        for (int i = 0; i < NL; ++i) *reinterpret_cast<u32x4*>(buf + (row + i * S::RPL) * KP + col) = kreg[i];
+          for (int c = 0; c < NC; ++c) {
+            const u32x4 kf =
+                *reinterpret_cast<const u32x4*>(kb + (32 * n + lq) * RB + (((2 * c + half) ^ ksw) * 16));
+            if constexpr (EB == 2) {
+              y[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
+                                                             __builtin_bit_cast(bf16x8, q[c]), y[n], 0, 0, 0);
+            } else {
 #pragma unroll
-        for (int i = 0; i < NL; ++i)
-          *reinterpret_cast<u32x4*>(buf + KT * KP + (row + i * S::RPL) * VP + col) = vreg[i];
+              for (int e = 0; e < 4; ++e)
+                y[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(q[c][e]), y[n], 0,
+                                                            0, 0);
+            }
+          }
+        }
+        // lane: query row lq; register i of block n: key 32n + 8(i / 4) + 4 half + i % 4
+        auto sees = [&](int n, int i) { return !EDGE || 32 * n + 8 * (i / 4) + i % 4 < left; };
+        float sum;
+        Probs<T, FINE, NK> p;
+        auto exps = [&]() {
+          float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+              const float e0 = fast_exp2(fmaf(y[n][i], a.c2, -m)), e1 = fast_exp2(fmaf(y[n][i + 1], a.c2, -m));
+              const float p0 = sees(n, i) ? e0 : 0.f, p1 = sees(n, i + 1) ? e1 : 0.f;
+              part[(i / 2) & 3] += p0;
+              part[(i / 2) & 3] += p1;
+              p.set(n, i, p0, p1);
+            }
+          sum = (part[0] + part[1]) + (part[2] + part[3]);
+        };
+        exps();
+        if (__any(!(sum <= kFar) || m == -INFINITY)) {
+          float mx = -INFINITY;
+#pragma unroll
+          for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (sees(n, i)) mx = fmaxf(mx, y[n][i] * a.c2);
+          mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+          const float mn = fmaxf(m, mx);
+          if (mn != m) {
+            const float alpha = m == -INFINITY ? 1.f : fast_exp2(m - mn);
+            s *= alpha;
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+            m = mn;
+          }
+          if (m == -INFINITY) {  // nothing seen so far
+            sum = 0.f;
+            p.clear();
+          } else {
+            exps();
+          }
+        }
+        s += sum;
+        if constexpr (EB == 2) {
+          const int l16 = lane & 15;
+          const int row = 4 * half + l16 / 4;                        // and 8, 16, ... further on: the same swizzle
+          const int piece = 2 * ((lane >> 4) & 1) + (l16 & 3) / 2;  // of a block's four
+          const char* vp = vb + row * RB + (l16 & 1) * 8;
+#pragma unroll
+          for (int d = 0; d < ND; ++d) {
+            const char* vd = vp + (((4 * d + piece) ^ S::value_swizzle(row)) * 16);
+#pragma unroll
+            for (int t = 0; t < KT / 16; ++t) {
+              const u32x2 v0 = lds_transposed(vd + 16 * t * RB), v1 = lds_transposed(vd + (16 * t + 8) * RB);
+              const u32x4 vt = {v0.x, v0.y, v1.x, v1.y};
+              o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt), p.piece(t), o[d], 0, 0, 0);
+              if (FINE)
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt), p.rest(t), o[d], 0, 0, 0);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int row = 32 * n + 8 * (i / 4) + 4 * half + i % 4;
+#pragma unroll
+              for (int d = 0; d < ND; ++d) {
+                const float v = *reinterpret_cast<const float*>(
+                    vb + row * RB + (((8 * d + lq / 4) ^ S::value_swizzle(4 * half)) * 16) + (lq & 3) * 4);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p.v[n][i], o[d], 0, 0, 0);
+              }
+            }
+        }
       };
 
       __syncthreads();  // the buffers of the tile before are done with
-      find_page(j0);
       load(j0);
-      find_page(j0 + 1);
-      stage(lds[j0 & 1]);
-      load(j0 + 1);
-      find_page(j0 + 2);
+      page = uniform(group_page(a, table, (j0 + 1) * KT + my_row, limit));
+      wait_loads();
       __syncthreads();
       for (int j = j0; j < j1; ++j) {
-        const char* kb = lds[j & 1];
-        const char* vb = kb + KT * KP;
-        if (j + 1 < j1) {
-          stage(lds[(j + 1) & 1]);
-          load(j + 2);
-          find_page(j + 3);
-        }
+        // the page of the tile after the next, asked for before the next tile's loads and used after them
+        const int page2 = group_page(a, table, (j + 2) * KT + my_row, limit);
+        if (j + 1 < j1) load(j + 1);
         const int key0 = j * KT;
-        if (key0 < hi) {
-          f32x16 y[NK];
-#pragma unroll
-          for (int n = 0; n < NK; ++n) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) y[n][i] = 0.f;
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-              const u32x4 kf = *reinterpret_cast<const u32x4*>(kb + (32 * n + lq) * KP + 32 * c + 16 * half);
-              if constexpr (EB == 2) {
-                y[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
-                                                               __builtin_bit_cast(bf16x8, q[c]), y[n], 0, 0, 0);
-              } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  y[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(q[c][e]), y[n],
-                                                              0, 0, 0);
-              }
-            }
-          }
-          // lane: query row lq; register i of block n: key 32n + 8(i / 4) + 4 half + i % 4
-          const bool edge = key0 + KT > lo;
-          const int left = seen - key0 - 4 * half;
-          float p[NK][16];
-          float sum = 0.f;
-          auto exps = [&]() {
-            sum = 0.f;
-#pragma unroll
-            for (int n = 0; n < NK; ++n)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) p[n][i] = fast_exp2(fmaf(y[n][i], a.c2, -m));
-            if (edge) {
-#pragma unroll
-              for (int n = 0; n < NK; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                  if (32 * n + 8 * (i / 4) + i % 4 >= left) p[n][i] = 0.f;
-            }
-#pragma unroll
-            for (int n = 0; n < NK; ++n)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) sum += p[n][i];
-          };
-          exps();
-          if (__any(!(sum <= kFar) || m == -INFINITY)) {
-            float mx = -INFINITY;
-#pragma unroll
-            for (int n = 0; n < NK; ++n)
-#pragma unroll
-              for (int i = 0; i < 16; ++i)
-                if (32 * n + 8 * (i / 4) + i % 4 < left) mx = fmaxf(mx, y[n][i] * a.c2);
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            const float mn = fmaxf(m, mx);
-            if (mn != m) {
-              const float alpha = m == -INFINITY ? 1.f : fast_exp2(m - mn);
-              s *= alpha;
-#pragma unroll
-              for (int d = 0; d < ND; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
-              m = mn;
-            }
-            if (m == -INFINITY) {
-              // nothing seen so far
-              sum = 0.f;
-#pragma unroll
-              for (int n = 0; n < NK; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) p[n][i] = 0.f;
-            } else {
-              exps();
-            }
-          }
-          s += sum;
-          if constexpr (EB == 2) {
-            const int g16 = lane >> 4, l16 = lane & 15;
-            const char* vp = vb + (4 * half + l16 / 4) * VP + (16 * (g16 & 1) + 4 * (l16 & 3)) * 2;
-#pragma unroll
-            for (int t = 0; t < KT / 16; ++t) {
-              const int n = t / 2, i0 = 8 * (t % 2);
-              u32x4 ph, pl;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) ph[e] = pack_bf16(p[n][i0 + 2 * e], p[n][i0 + 2 * e + 1]);
-              if (FINE) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) pl[e] = pack_bf16_rest(p[n][i0 + 2 * e], p[n][i0 + 2 * e + 1], ph[e]);
-              }
-#pragma unroll
-              for (int d = 0; d < ND; ++d) {
-                const u32x2 v0 = lds_transposed(vp + 16 * t * VP + 64 * d);
-                const u32x2 v1 = lds_transposed(vp + (16 * t + 8) * VP + 64 * d);
-                const u32x4 vt = {v0.x, v0.y, v1.x, v1.y};
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt),
-                                                               __builtin_bit_cast(bf16x8, ph), o[d], 0, 0, 0);
-                if (FINE)
-                  o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt),
-                                                                 __builtin_bit_cast(bf16x8, pl), o[d], 0, 0, 0);
-              }
-            }
-          } else {
-#pragma unroll
-            for (int n = 0; n < NK; ++n)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const char* vp = vb + (32 * n + 8 * (i / 4) + 4 * half + i % 4) * VP + lq * 4;
-#pragma unroll
-                for (int d = 0; d < ND; ++d)
-                  o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(vp + 128 * d), p[n][i],
-                                                              o[d], 0, 0, 0);
-              }
-          }
-        }
+        const char* kb = lds[j & 1][0];
+        if (key0 + KT <= lo) attend(kb, std::false_type{}, 0);
+        else if (key0 < hi) attend(kb, std::true_type{}, seen - key0 - 4 * half);
+        wait_loads();
+        page = uniform(page2);
         __syncthreads();
       }
       s += __shfl_xor(s, 32, 64);
