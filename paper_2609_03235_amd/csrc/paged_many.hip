@@ -137,10 +137,8 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
       const int r = wid * 32 + lq, tok = r / a.G, hd = r - tok * a.G;
       const bool on = r < nrow;
       const int seen = on ? seen_by(a, g, tok0 + tok) : 0;
-      // the rows of this wave see between lo and hi keys
-      const bool any_row = wid * 32 < nrow;
-      const int lo = any_row ? uniform(seen) : 0;
-      const int hi = any_row ? uniform(seen_by(a, g, tok0 + (min(nrow, wid * 32 + 32) - 1) / a.G)) : 0;
+      // the rows of this wave see at most hi keys
+      const int hi = wid * 32 < nrow ? uniform(seen_by(a, g, tok0 + (min(nrow, wid * 32 + 32) - 1) / a.G)) : 0;
 
       const int32_t* table = a.tables + (int64_t)at.seg * a.max_pages;
       int page = uniform(group_page(a, table, j0 * KT + my_row, limit));
@@ -199,13 +197,13 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
         auto sees = [&](int n, int i) { return !EDGE || 32 * n + 8 * (i / 4) + i % 4 < left; };
         float sum;
         Probs<T, FINE, NK> p;
-        auto exps = [&]() {
+        auto exps = [&](float ref) {
           float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int n = 0; n < NK; ++n)
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
-              const float e0 = fast_exp2(fmaf(y[n][i], a.c2, -m)), e1 = fast_exp2(fmaf(y[n][i + 1], a.c2, -m));
+              const float e0 = fast_exp2(fmaf(y[n][i], a.c2, -ref)), e1 = fast_exp2(fmaf(y[n][i + 1], a.c2, -ref));
               const float p0 = sees(n, i) ? e0 : 0.f, p1 = sees(n, i + 1) ? e1 : 0.f;
               part[(i / 2) & 3] += p0;
               part[(i / 2) & 3] += p1;
@@ -213,31 +211,24 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
             }
           sum = (part[0] + part[1]) + (part[2] + part[3]);
         };
-        exps();
+        exps(m);
+        // Without a lane of its own accord in the branch: the compiler then keeps o in place.
         if (__any(!(sum <= kFar) || m == -INFINITY)) {
           float mx = -INFINITY;
 #pragma unroll
           for (int n = 0; n < NK; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (sees(n, i)) mx = fmaxf(mx, y[n][i] * a.c2);
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sees(n, i) ? y[n][i] * a.c2 : -INFINITY);
           mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
           const float mn = fmaxf(m, mx);
-          if (mn != m) {
-            const float alpha = m == -INFINITY ? 1.f : fast_exp2(m - mn);
-            s *= alpha;
+          const float alpha = m == mn ? 1.f : fast_exp2(m - mn);  // before the first key s and o are 0
+          s *= alpha;
 #pragma unroll
-            for (int d = 0; d < ND; ++d)
+          for (int d = 0; d < ND; ++d)
 #pragma unroll
-              for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
-            m = mn;
-          }
-          if (m == -INFINITY) {  // nothing seen so far
-            sum = 0.f;
-            p.clear();
-          } else {
-            exps();
-          }
+            for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+          m = mn;
+          exps(m == -INFINITY ? 0.f : m);  // nothing seen so far: all are 0
         }
         s += sum;
         if constexpr (EB == 2) {
@@ -278,18 +269,21 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
       page = uniform(group_page(a, table, (j0 + 1) * KT + my_row, limit));
       wait_loads();
       __syncthreads();
-      for (int j = j0; j < j1; ++j) {
-        // the page of the tile after the next, asked for before the next tile's loads and used after them
-        const int page2 = group_page(a, table, (j + 2) * KT + my_row, limit);
-        if (j + 1 < j1) load(j + 1);
-        const int key0 = j * KT;
-        const char* kb = lds[j & 1][0];
-        if (key0 + KT <= lo) attend(kb, std::false_type{}, 0);
-        else if (key0 < hi) attend(kb, std::true_type{}, seen - key0 - 4 * half);
-        wait_loads();
-        page = uniform(page2);
-        __syncthreads();
-      }
+      // the tiles that every row sees whole, then the others
+      int j = j0;
+      auto tiles = [&](int to, auto edge) {
+        for (; j < to; ++j) {
+          // the page of the tile after the next, asked for before the next tile's loads and used after them
+          const int page2 = group_page(a, table, (j + 2) * KT + my_row, limit);
+          if (j + 1 < j1) load(j + 1);
+          if (j * KT < hi) attend(lds[j & 1][0], edge, seen - j * KT - 4 * half);
+          wait_loads();
+          page = uniform(page2);
+          __syncthreads();
+        }
+      };
+      tiles(min(j1, seen_by(a, g, tok0) / KT), std::false_type{});
+      tiles(j1, std::true_type{});
       s += __shfl_xor(s, 32, 64);
       if (on) {
         const bool whole = j0 == 0 && j1 == nkt;
