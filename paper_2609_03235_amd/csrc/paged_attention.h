@@ -29,6 +29,9 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kAttnBlock = 256;
 constexpr int kAttnWaves = kAttnBlock / 64;
+// Most query rows per KV head of the instances for few: what leaves room for two workgroups in a compute unit's
+// registers and LDS.
+constexpr int kFewRowsBf16 = 48, kFewRowsF32 = 32;
 
 // A segment as a workgroup sees it. Lengths that do not fit the buffers are cut to them.
 struct PagedSeg {
@@ -205,6 +208,33 @@ __device__ __forceinline__ rsrc_t group_rsrc(const PagedAttnArgs& a, const void*
   return make_rsrc(static_cast<const char*>(pool) + row * row_bytes, (uint64_t)(n * row_bytes));
 }
 
+// The same buffer, of at most `rows` rows, as four scalar words.
+__device__ __forceinline__ u32x4 group_words(const PagedAttnArgs& a, const void* pool, int page, int r0, int valid,
+                                             int rows, int row_bytes) {
+  const bool ok = page >= 0 && page < a.num_pages && valid > 0;
+  const int64_t row = ok ? ((int64_t)page << a.page_shift) + (r0 & ((1 << a.page_shift) - 1)) : 0;
+  const uint64_t p = reinterpret_cast<uint64_t>(pool) + row * row_bytes;
+  return u32x4{(uint32_t)uniform((int)p), (uint32_t)uniform((int)(p >> 32)),
+               (uint32_t)uniform(ok ? min(valid, rows) * row_bytes : 0), (uint32_t)kRsrcWord3};
+}
+
+// 64 x 16 bytes from a buffer into LDS at lds + 16 * lane; out-of-range lanes write zeros. The compiler does not
+// see that these loads are under way: wait_loads() before the data is read (and a barrier, if by other waves).
+// There is no destination register that could be reused too early; m0 is no allocatable register.
+__device__ __forceinline__ uint32_t lds_address(const char* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
+__device__ __forceinline__ void load_to_lds(u32x4 rsrc, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rsrc)
+               : "memory");
+}
+__device__ __forceinline__ void load_to_lds_nt(u32x4 rsrc, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(lds), "v"(off),
+               "s"(rsrc)
+               : "memory");
+}
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 __device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
   f32x2 v = {x, y};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
@@ -236,7 +266,7 @@ __device__ __forceinline__ float lse_of(float m, float s) {
   return s > 0.f ? (m + fast_log2(s)) * kLn2 : (s == 0.f ? -INFINITY : s);
 }
 
-hipError_t launch_paged_few(const PagedAttnArgs& a, int rows, hipStream_t stream);
+hipError_t launch_paged_few(const PagedAttnArgs& a, hipStream_t stream);
 hipError_t launch_paged_many(const PagedAttnArgs& a, hipStream_t stream);
 
 }  // namespace sgdkv

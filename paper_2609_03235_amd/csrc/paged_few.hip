@@ -1,10 +1,11 @@
 // Paged attention for few query rows per KV head (single tokens, drafted tokens), and the merge of the
 // partial results of every instance. See paged_attention.h.
 //
-// Bound by HBM: a key and value row is read once and used by at most 32 query rows. Each wave takes 32 of
-// the workgroup's 128 key rows per step on its own (no barrier in the loop): keys go from memory straight
-// into the MFMA's A layout, values through 32 rows of LDS that only this wave uses, for the transposing
-// read. The next step's rows are in flight while a step is computed.
+// Bound by HBM: a key and value row is read once and used by at most 48 query rows. Each wave takes its own
+// rows of the workgroup's key tile (no barrier in the loop): keys go from memory into registers in the MFMA's A
+// layout, values straight into LDS that only this wave uses (two buffers), for the transposing read. The next
+// step's loads start as soon as the step's keys are used up, so that all but the logits of a step runs beside
+// them: 8 waves of a compute unit have 128 KB under way.
 #include <algorithm>
 
 #include "paged_attention.h"
@@ -13,50 +14,35 @@ namespace sgdkv {
 
 namespace {
 
-constexpr int kStep = 32;                    // key rows per wave and step
-constexpr int kTile = kStep * kAttnWaves;    // key rows per workgroup and step
-
-// A step's rows of one wave: the keys as two 16-key A operands, the values as they lie in memory.
+// Rows of values in LDS have no padding (a load writes its lanes' 16 bytes one after the other); piece c of row r
+// lies at place c ^ swizzle(r), which spreads the pieces that a read takes from several rows over the banks.
 template <typename T, int D>
-struct FewStep {
-  static constexpr int EB = sizeof(T), RB = D * EB, NC = D / 32;
-  static constexpr int VPR = RB / 16, RPL = 64 / VPR, NV = 16 / RPL;  // value rows per load, loads per 16 rows
-  Frag<T> k[2][NC];
-  u32x4 v[2][NV];
-  __device__ __forceinline__ void load(const PagedAttnArgs& a, const int (&page)[2], int r0, int limit, int lane) {
-    const int lr = lane & 15, lg = lane >> 4;
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const rsrc_t kr = group_rsrc(a, a.k_pages, page[g], r0 + 16 * g, limit - r0 - 16 * g, RB);
-      const rsrc_t vr = group_rsrc(a, a.v_pages, page[g], r0 + 16 * g, limit - r0 - 16 * g, RB);
-#pragma unroll
-      for (int c = 0; c < NC; ++c) k[g][c] = gload_frag_nt<T>(kr, (uint32_t)(lr * RB + (32 * c + 8 * lg) * EB));
-#pragma unroll
-      for (int i = 0; i < NV; ++i) v[g][i] = ld128_nt(vr, (uint32_t)(i * 1024 + lane * 16));
-    }
+struct FewShape {
+  static constexpr int EB = sizeof(T), RB = D * EB, NC = D / 32, ND = D / 16;
+  static constexpr int U = EB == 2 ? 2 : 1;              // 16-row groups per wave and step
+  static constexpr int STEP = 16 * U, KT = STEP * kAttnWaves;
+  static constexpr int VPR = RB / 16, RPL = 64 / VPR, NV = 16 / RPL;  // rows per load, loads per group
+  static constexpr int STAGE = STEP * RB;
+  static __device__ __forceinline__ int swizzle(int r) {
+    return EB == 4 ? ((r >> 2) & 3) << 2 : (RB == 128 ? ((r >> 1) & 3) << 1 : (r & 7) << 1);
   }
 };
-
-__device__ __forceinline__ void few_wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
 
 // QB: 16-row query blocks. FINE: probabilities as two bf16 terms (fp32 output of bf16 inputs).
 template <typename T, int D, int QB, bool FINE>
 __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs a) {
-  using S = FewStep<T, D>;
-  constexpr int EB = S::EB, RB = S::RB, NC = S::NC, ND = D / 16;
-  constexpr int VP = EB == 2 ? RB + 16 : RB + 16;  // pitch of a value row in LDS
-  constexpr int kStage = kStep * VP;
-  constexpr int OP = D + 4;  // pitch of a row of o in LDS, in floats: the rows' writes spread over the banks
-  constexpr int kMerge = 16 * QB * OP * 4;
-  constexpr int kWaveLds = kStage > kMerge ? kStage : kMerge;
-  __shared__ __attribute__((aligned(16))) char lds[kAttnWaves][kWaveLds];
-  __shared__ float mws[kAttnWaves][16 * QB], sws[kAttnWaves][16 * QB];
-  __shared__ LineScratch sc;
+  using S = FewShape<T, D>;
+  constexpr int EB = S::EB, RB = S::RB, NC = S::NC, ND = S::ND, U = S::U, STEP = S::STEP, KT = S::KT, NV = S::NV;
   constexpr int M = 16 * QB;
+  constexpr bool QLDS = QB > 2;    // query operands read from LDS at each use: no registers for them
+  constexpr int QP = RB + 16;      // their pitch
+  constexpr int OP = D + 4;        // pitch of a row of o in LDS, in floats: the rows' writes spread over the banks
+  constexpr int kMerge = 16 * OP * 4;
+  constexpr int kWaveLds = 2 * S::STAGE > kMerge ? 2 * S::STAGE : kMerge;
+  __shared__ __attribute__((aligned(16))) char lds[kAttnWaves][kWaveLds];
+  __shared__ __attribute__((aligned(16))) char qlds[QLDS ? M * QP : 16];
+  __shared__ float mws[kAttnWaves][M], sws[kAttnWaves][M];
+  __shared__ LineScratch sc;
 
   const int tid = threadIdx.x, wid = uniform(tid >> 6), lane = tid & 63;
   const int lr = lane & 15, lg = lane >> 4;
@@ -68,6 +54,13 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
   if (!find_piece<true>(a, sc, w, share, end, padded, at)) return;
   int64_t pos = share * w;
   char* stage = lds[wid];
+  const uint32_t stage0 = lds_address(stage);
+  uint32_t voff[NV];  // where this lane's 16 bytes of each load of a group come from
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int r = i * S::RPL + lane / S::VPR;
+    voff[i] = r * RB + ((lane % S::VPR) ^ S::swizzle(r)) * 16;
+  }
 
   while (pos < end) {
     if (at.tile >= at.g.tiles) {  // the next segment
@@ -78,27 +71,50 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
     }
     const PagedSeg& g = at.g;
     const int limit = uniform(tile_rows(a, g, at.tile));
-    const int nkt = max((limit + kTile - 1) / kTile, 1);
-    const int j0 = (int)((pos - at.start + kTile - 1) / kTile);
-    const int j1 = (int)min((int64_t)nkt, (end - at.start + kTile - 1) / kTile);
-    const int h = at.seg % a.Hkv;
+    const int nkt = max((limit + KT - 1) / KT, 1);
+    const int j0 = (int)((pos - at.start + KT - 1) / KT);
+    const int j1 = (int)min((int64_t)nkt, (end - at.start + KT - 1) / KT);
     if (j0 < j1) {
+      const int h = at.seg % a.Hkv;
       const int tok0 = at.tile * a.tokens, ntok = min(a.tokens, g.n - tok0);
       const int nrow = ntok * a.G;
+      const int32_t* table = a.tables + (int64_t)at.seg * a.max_pages;
+      auto first_row = [&](int j) { return j * KT + wid * STEP; };
+      int page[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) page[u] = group_page(a, table, first_row(j0) + 16 * u, limit);
+
       // query rows as B operands: row lr of block qb is head row % G of token row / G
-      Frag<T> q[QB][NC];
+      Frag<T> q[QLDS ? 1 : QB][NC];
       int seen[QB];
+      const rsrc_t qr = make_rsrc(static_cast<const char*>(a.q) + ((int64_t)(g.t0 + tok0) * a.Hq + h * a.G) * RB,
+                                  ((uint64_t)(ntok - 1) * a.Hq + a.G) * RB);
+      auto query_off = [&](int r) -> uint32_t {
+        const int tok = r / a.G, hd = r - tok * a.G;
+        return r < nrow ? (uint32_t)((tok * a.Hq + hd) * RB) : 0xFFFF0000u;
+      };
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
-        const int r = 16 * qb + lr, tok = r / a.G, hd = r - tok * a.G;
-        const bool on = r < nrow;
-        seen[qb] = on ? seen_by(a, g, tok0 + tok) : 0;
-        const rsrc_t qr = make_rsrc(static_cast<const char*>(a.q) + ((int64_t)(g.t0 + tok0) * a.Hq + h * a.G) * RB,
-                                    ((uint64_t)(ntok - 1) * a.Hq + a.G) * RB);
+        const int r = 16 * qb + lr;
+        seen[qb] = r < nrow ? seen_by(a, g, tok0 + r / a.G) : 0;
+        if constexpr (!QLDS) {
+          const uint32_t off = query_off(r);
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
-          q[qb][c] = gload_frag<T>(qr, on ? (uint32_t)((tok * a.Hq + hd) * RB + (32 * c + 8 * lg) * EB) : 0xFFFFFF00u);
+          for (int c = 0; c < NC; ++c) q[qb][c] = gload_frag<T>(qr, off + (32 * c + 8 * lg) * EB);
+        }
       }
+      if constexpr (QLDS) {
+        __syncthreads();  // the tile before is done with its queries
+        for (int i = tid; i < M * S::VPR; i += kAttnBlock) {
+          const int r = i / S::VPR, c = i % S::VPR;
+          *reinterpret_cast<u32x4*>(qlds + r * QP + c * 16) = ld128(qr, query_off(r) + c * 16);
+        }
+        __syncthreads();
+      }
+      auto query = [&](int qb, int c) {
+        if constexpr (QLDS) return lds_frag<T>(qlds, (16 * qb + lr) * QP + (32 * c + 8 * lg) * EB);
+        else return q[qb][c];
+      };
       float m[QB], s[QB];
       f32x4 o[QB][ND];
 #pragma unroll
@@ -108,51 +124,55 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
 #pragma unroll
         for (int d = 0; d < ND; ++d) o[qb][d] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
-      const int32_t* table = a.tables + (int64_t)at.seg * a.max_pages;
-      auto first_row = [&](int j) { return j * kTile + wid * kStep; };
-      S cur, next;
-      int page[2];
-      auto pages = [&](int j) {
-        page[0] = uniform(group_page(a, table, first_row(j), limit));
-        page[1] = uniform(group_page(a, table, first_row(j) + 16, limit));
-      };
-      pages(j0);
-      next.load(a, page, first_row(j0), limit, lane);
-      if (j0 + 1 < j1) pages(j0 + 1);
-      for (int j = j0; j < j1; ++j) {
-        cur = next;
+
+      Frag<T> k[U][NC];
+      auto load = [&](int j) {
         const int r0 = first_row(j);
-        if (j + 1 < j1) {
-          next.load(a, page, first_row(j + 1), limit, lane);
-          pages(j + 2);
+        const uint32_t to = uniform((int)(stage0 + (j & 1) * S::STAGE));
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const u32x4 vr = group_words(a, a.v_pages, uniform(page[u]), r0 + 16 * u, limit - r0 - 16 * u, 16, RB);
+#pragma unroll
+          for (int i = 0; i < NV; ++i) load_to_lds_nt(vr, voff[i], to + u * 16 * RB + i * 1024);
         }
-        if (r0 >= limit) continue;
-        // values to LDS
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < U; ++u) {
+          const rsrc_t kr = group_rsrc(a, a.k_pages, uniform(page[u]), r0 + 16 * u, limit - r0 - 16 * u, RB);
 #pragma unroll
-          for (int i = 0; i < S::NV; ++i) {
-            const int row = 16 * u + i * S::RPL + lane / S::VPR;
-            *reinterpret_cast<u32x4*>(stage + row * VP + (lane % S::VPR) * 16) = cur.v[u][i];
+          for (int c = 0; c < NC; ++c) k[u][c] = gload_frag_nt<T>(kr, (uint32_t)(lr * RB + (32 * c + 8 * lg) * EB));
+        }
+      };
+      load(j0);
+      for (int j = j0; j < j1; ++j) {
+        const int r0 = first_row(j);
+#pragma unroll
+        for (int u = 0; u < U; ++u) page[u] = group_page(a, table, first_row(j + 1) + 16 * u, limit);
+        wait_loads();  // this step's keys and values, the next one's pages
+        f32x4 y[QB][U];
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+          for (int u = 0; u < U; ++u) y[qb][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) {
+            const Frag<T> qf = query(qb, c);
+#pragma unroll
+            for (int u = 0; u < U; ++u) y[qb][u] = mma(k[u][c], qf, y[qb][u]);
           }
-        few_wave_sync();
-        float p[QB][2][4];
+        if (j + 1 < j1) load(j + 1);
+        const char* vals = stage + (j & 1) * S::STAGE;
+        float p[QB][U][4];
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
-          f32x4 y[2];
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            y[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < NC; ++c) y[u] = mma(cur.k[u][c], q[qb][c], y[u]);
-          }
           // lane: query row lr; keys 16u + 4lg + i
+          const int left = seen[qb] - r0 - 4 * lg;
           float mx = -INFINITY;
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
+          for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (r0 + 16 * u + 4 * lg + i < seen[qb]) mx = fmaxf(mx, y[u][i] * a.c2);
+            for (int i = 0; i < 4; ++i) mx = fmaxf(mx, 16 * u + i < left ? y[qb][u][i] * a.c2 : -INFINITY);
           mx = max_lane_groups(mx);
           const float mn = fmaxf(m[qb], mx);
           const float ref = mn == -INFINITY ? 0.f : mn;
@@ -160,11 +180,11 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
           m[qb] = mn;
           float sum = 0.f;
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
+          for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const float e = fast_exp2(fmaf(y[u][i], a.c2, -ref));
-              p[qb][u][i] = r0 + 16 * u + 4 * lg + i < seen[qb] ? e : 0.f;
+              const float e = fast_exp2(fmaf(y[qb][u][i], a.c2, -ref));
+              p[qb][u][i] = 16 * u + i < left ? e : 0.f;
               sum += p[qb][u][i];
             }
           s[qb] = fmaf(s[qb], alpha, sum);
@@ -187,10 +207,12 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
               }
             }
           }
-          const char* vp = stage + (4 * lg + lr / 4) * VP + (lr % 4) * 8;
+          const int row = 4 * lg + lr / 4;  // and 16 further on: the same swizzle
+          const char* vp = vals + row * RB + (lr & 1) * 8;
 #pragma unroll
           for (int d = 0; d < ND; ++d) {
-            const u32x2 v0 = lds_transposed(vp + d * 32), v1 = lds_transposed(vp + 16 * VP + d * 32);
+            const char* vd = vp + (((2 * d + (lr & 3) / 2) ^ S::swizzle(row)) * 16);
+            const u32x2 v0 = lds_transposed(vd), v1 = lds_transposed(vd + 16 * RB);
             Frag<__bf16> vt;
             vt.v = u32x4{v0.x, v0.y, v1.x, v1.y};
 #pragma unroll
@@ -201,63 +223,63 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
           }
         } else {
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
+          for (int i = 0; i < 4; ++i) {
+            const char* vp = vals + (4 * lg + i) * RB + (lr & 3) * 4;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const char* vp = stage + (16 * u + 4 * lg + i) * VP + lr * 4;
+            for (int d = 0; d < ND; ++d) {
+              const float v = *reinterpret_cast<const float*>(vp + (((4 * d + lr / 4) ^ S::swizzle(4 * lg)) * 16));
 #pragma unroll
-              for (int d = 0; d < ND; ++d) {
-                const float v = *reinterpret_cast<const float*>(vp + d * 64);
-#pragma unroll
-                for (int qb = 0; qb < QB; ++qb)
-                  o[qb][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[qb][u][i], o[qb][d], 0, 0, 0);
-              }
+              for (int qb = 0; qb < QB; ++qb)
+                o[qb][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[qb][0][i], o[qb][d], 0, 0, 0);
             }
+          }
         }
-        few_wave_sync();
       }
-      // merge the waves' parts, in wave order
-      __syncthreads();
-#pragma unroll
-      for (int qb = 0; qb < QB; ++qb) {
-        s[qb] = sum_lane_groups(s[qb]);
-        if (lg == 0) {
-          mws[wid][16 * qb + lr] = m[qb];
-          sws[wid][16 * qb + lr] = s[qb];
-        }
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-          *reinterpret_cast<f32x4*>(stage + ((16 * qb + lr) * OP + 16 * d + 4 * lg) * 4) = o[qb][d];
-      }
-      __syncthreads();
+      // merge the waves' parts in wave order, 16 rows at a time
       const bool whole = j0 == 0 && j1 == nkt;
       const int64_t slot = 2 * (int64_t)w + (at.start > share * w ? 1 : 0);
-      for (int idx = tid; idx < M * (D / 4); idx += kAttnBlock) {
-        const int r = idx / (D / 4), col = 4 * (idx % (D / 4));
-        if (r >= nrow) break;
-        float mm = -INFINITY;
 #pragma unroll
-        for (int x = 0; x < kAttnWaves; ++x) mm = fmaxf(mm, mws[x][r]);
-        const float ref = mm == -INFINITY ? 0.f : mm;
-        float sum = 0.f;
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int x = 0; x < kAttnWaves; ++x) {
-          const float f = fast_exp2(mws[x][r] - ref);
-          sum = fmaf(sws[x][r], f, sum);
-          acc += f * *reinterpret_cast<const f32x4*>(lds[x] + (r * OP + col) * 4);
+      for (int qb = 0; qb < QB; ++qb) {
+        const float total = sum_lane_groups(s[qb]);
+        if (lg == 0) {
+          mws[wid][16 * qb + lr] = m[qb];
+          sws[wid][16 * qb + lr] = total;
         }
-        if (whole) {
-          const int tok = r / a.G, hd = r - tok * a.G;
-          const int64_t row = (int64_t)(g.t0 + tok0 + tok) * a.Hq + h * a.G + hd;
-          const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-          store_out4(a, row, D, col, acc * inv);
-          if (a.lse && col == 0) a.lse[row] = lse_of(mm, sum);
-        } else {
-          *reinterpret_cast<f32x4*>(a.part + (slot * M + r) * D + col) = acc;
-          if (col == 0) {
-            a.part_ms[(slot * M + r) * 2] = mm;
-            a.part_ms[(slot * M + r) * 2 + 1] = sum;
+      }
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        if (16 * qb >= nrow) break;
+        __syncthreads();
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+          *reinterpret_cast<f32x4*>(stage + (lr * OP + 16 * d + 4 * lg) * 4) = o[qb][d];
+        __syncthreads();
+        for (int idx = tid; idx < 16 * (D / 4); idx += kAttnBlock) {
+          const int lrow = idx / (D / 4), r = 16 * qb + lrow, col = 4 * (idx % (D / 4));
+          if (r >= nrow) break;
+          float mm = -INFINITY;
+#pragma unroll
+          for (int x = 0; x < kAttnWaves; ++x) mm = fmaxf(mm, mws[x][r]);
+          const float ref = mm == -INFINITY ? 0.f : mm;
+          float sum = 0.f;
+          f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int x = 0; x < kAttnWaves; ++x) {
+            const float f = fast_exp2(mws[x][r] - ref);
+            sum = fmaf(sws[x][r], f, sum);
+            acc += f * *reinterpret_cast<const f32x4*>(lds[x] + (lrow * OP + col) * 4);
+          }
+          if (whole) {
+            const int tok = r / a.G, hd = r - tok * a.G;
+            const int64_t row = (int64_t)(g.t0 + tok0 + tok) * a.Hq + h * a.G + hd;
+            store_out4(a, row, D, col, acc * (sum == 0.f ? 0.f : 1.0f / sum));
+            if (a.lse && col == 0) a.lse[row] = lse_of(mm, sum);
+          } else {
+            *reinterpret_cast<f32x4*>(a.part + (slot * M + r) * D + col) = acc;
+            if (col == 0) {
+              a.part_ms[(slot * M + r) * 2] = mm;
+              a.part_ms[(slot * M + r) * 2 + 1] = sum;
+            }
           }
         }
       }
@@ -340,38 +362,44 @@ void launch_few(const PagedAttnArgs& a, hipStream_t stream) {
   paged_few_kernel<T, D, QB, false><<<dim3(a.workers), dim3(kAttnBlock), 0, stream>>>(a);
 }
 
+template <typename T, int D>
+void launch_few_rows(const PagedAttnArgs& a, hipStream_t stream) {
+  switch (a.tile_rows) {
+    case 16: return launch_few<T, D, 1>(a, stream);
+    case 32: return launch_few<T, D, 2>(a, stream);
+    default:
+      if constexpr (sizeof(T) == 2) launch_few<T, D, 3>(a, stream);
+  }
+}
+
 }  // namespace
 
 PagedAttnShape paged_attn_shape(int dtype, int G, int max_new) {
-  if ((int64_t)max_new * G <= 16) return {16, kTile};
-  if ((int64_t)max_new * G <= 32) return {32, kTile};
+  const int64_t rows = (int64_t)max_new * G;
+  if (rows <= (dtype ? kFewRowsBf16 : kFewRowsF32)) return {16 * (int)((rows + 15) / 16), dtype ? 128 : 64};
   return {128, dtype ? 64 : 32};
 }
 
-hipError_t launch_paged_few(const PagedAttnArgs& a, int rows, hipStream_t stream) {
-  if (a.dtype) {
-    if (a.D == 128) rows == 16 ? launch_few<__bf16, 128, 1>(a, stream) : launch_few<__bf16, 128, 2>(a, stream);
-    else rows == 16 ? launch_few<__bf16, 64, 1>(a, stream) : launch_few<__bf16, 64, 2>(a, stream);
-  } else {
-    if (a.D == 128) rows == 16 ? launch_few<float, 128, 1>(a, stream) : launch_few<float, 128, 2>(a, stream);
-    else rows == 16 ? launch_few<float, 64, 1>(a, stream) : launch_few<float, 64, 2>(a, stream);
-  }
+hipError_t launch_paged_few(const PagedAttnArgs& a, hipStream_t stream) {
+  if (a.dtype) a.D == 128 ? launch_few_rows<__bf16, 128>(a, stream) : launch_few_rows<__bf16, 64>(a, stream);
+  else a.D == 128 ? launch_few_rows<float, 128>(a, stream) : launch_few_rows<float, 64>(a, stream);
   return hipGetLastError();
 }
 
 hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream) {
+  const bool few = a.tile_rows < 128;
   prof_begin("paged_attention", stream);
-  hipError_t e = a.tile_rows <= 32 ? launch_paged_few(a, a.tile_rows, stream) : launch_paged_many(a, stream);
+  hipError_t e = few ? launch_paged_few(a, stream) : launch_paged_many(a, stream);
   prof_end(stream);
-  if (e != hipSuccess || a.workers == 1) return e;  // one worker shares no tile
+  if (e != hipSuccess) return e;
   prof_begin("paged_merge", stream);
-  if (a.tile_rows <= 32) {
-    const dim3 grid(a.workers, std::min(a.max_new, a.tokens) * a.G);
+  const int rows = std::min(a.max_new, a.tokens) * a.G;
+  const int per = few ? 1 : kAttnBlock / (a.D / 4);  // rows of a workgroup
+  const dim3 grid(a.workers, (rows + per - 1) / per);
+  if (few) {
     if (a.D == 128) paged_merge_kernel<128, false><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
     else paged_merge_kernel<64, false><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
   } else {
-    const int per = kAttnBlock / (a.D / 4);  // rows of a workgroup
-    const dim3 grid(a.workers, (std::min(a.max_new, a.tokens) * a.G + per - 1) / per);
     if (a.D == 128) paged_merge_kernel<128, true><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
     else paged_merge_kernel<64, true><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
   }

@@ -132,7 +132,7 @@ sgdkv_status plan_paged(const sgdkv_page_pool* pool, const sgdkv_paged_desc* d, 
   a.key_tile = shape.key_tile;
   a.tokens = shape.rows / G;
   a.workers = kPagedWorkers;
-  a.min_cost = shape.rows <= 32 ? shape.key_tile : 2 * shape.key_tile;
+  a.min_cost = shape.rows < 128 ? 128 : 2 * shape.key_tile;  // a power of two and whole key tiles
   // The workspace follows the bound the caller gave, whatever the tokens of this call.
   const int most_rows = sgdkv::paged_attn_shape(a.dtype, G, d->max_new).rows;
   bytes = (size_t)kPagedWorkers * (sizeof(int4) + 2 * (size_t)most_rows * (a.D + 2) * sizeof(float));

@@ -31,24 +31,6 @@ struct ManyShape {
   }
 };
 
-// 64 x 16 bytes from a buffer into LDS at lds + 16 * lane; out-of-range lanes write zeros. The compiler does not
-// see this load: wait_loads() before the barrier after which other waves read.
-__device__ __forceinline__ void load_to_lds(u32x4 rsrc, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rsrc)
-               : "memory");
-}
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-
-// The buffer of group_rsrc as four scalar words.
-__device__ __forceinline__ u32x4 group_words(const PagedAttnArgs& a, const void* pool, int page, int r0, int valid,
-                                             int rows, int row_bytes) {
-  const bool ok = page >= 0 && page < a.num_pages && valid > 0;
-  const int64_t row = ok ? ((int64_t)page << a.page_shift) + (r0 & ((1 << a.page_shift) - 1)) : 0;
-  const uint64_t p = reinterpret_cast<uint64_t>(pool) + row * row_bytes;
-  return u32x4{(uint32_t)uniform((int)p), (uint32_t)uniform((int)(p >> 32)),
-               (uint32_t)uniform(ok ? min(valid, rows) * row_bytes : 0), (uint32_t)kRsrcWord3};
-}
-
 // Reference kept while a tile's sum of exponentials stays below this.
 constexpr float kFar = 1024.f;
 
@@ -116,7 +98,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
     koff[i] = r * RB + (c ^ S::key_swizzle(my_row + r)) * 16;
     voff[i] = r * RB + (c ^ S::value_swizzle(my_row + r)) * 16;
   }
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)&lds[0][0][0];
+  const uint32_t lds0 = lds_address(&lds[0][0][0]);
 
   while (pos < end) {
     if (at.tile >= at.g.tiles) {  // the next segment
@@ -172,6 +154,8 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
       auto attend = [&](const char* kb, auto edge, int left) {
         constexpr bool EDGE = decltype(edge)::value;
         const char* vb = kb + S::TILE;
+        // products first where waves compete: the other waves' exponentials fill in
+        __builtin_amdgcn_s_setprio(1);
         f32x16 y[NK];
         const int ksw = S::key_swizzle(lq);  // of every block's row: 32 rows on it repeats
 #pragma unroll
@@ -193,6 +177,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
             }
           }
         }
+        __builtin_amdgcn_s_setprio(0);
         // lane: query row lq; register i of block n: key 32n + 8(i / 4) + 4 half + i % 4
         auto sees = [&](int n, int i) { return !EDGE || 32 * n + 8 * (i / 4) + i % 4 < left; };
         float sum;
@@ -231,16 +216,17 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
           exps(m == -INFINITY ? 0.f : m);  // nothing seen so far: all are 0
         }
         s += sum;
+        __builtin_amdgcn_s_setprio(1);
         if constexpr (EB == 2) {
           const int l16 = lane & 15;
           const int row = 4 * half + l16 / 4;                        // and 8, 16, ... further on: the same swizzle
           const int piece = 2 * ((lane >> 4) & 1) + (l16 & 3) / 2;  // of a block's four
           const char* vp = vb + row * RB + (l16 & 1) * 8;
 #pragma unroll
-          for (int d = 0; d < ND; ++d) {
-            const char* vd = vp + (((4 * d + piece) ^ S::value_swizzle(row)) * 16);
+          for (int t = 0; t < KT / 16; ++t) {
 #pragma unroll
-            for (int t = 0; t < KT / 16; ++t) {
+            for (int d = 0; d < ND; ++d) {
+              const char* vd = vp + (((4 * d + piece) ^ S::value_swizzle(row)) * 16);
               const u32x2 v0 = lds_transposed(vd + 16 * t * RB), v1 = lds_transposed(vd + (16 * t + 8) * RB);
               const u32x4 vt = {v0.x, v0.y, v1.x, v1.y};
               o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt), p.piece(t), o[d], 0, 0, 0);
@@ -262,6 +248,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
               }
             }
         }
+        __builtin_amdgcn_s_setprio(0);
       };
 
       __syncthreads();  // the buffers of the tile before are done with
