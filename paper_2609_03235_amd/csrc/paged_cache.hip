@@ -196,18 +196,30 @@ __global__ __launch_bounds__(kPageBlock) void page_update_kernel(PageArgs a, int
 }
 
 // ------------------------------------------------------------------ rows to their slots
+// A workgroup takes kStoreVecs * 256 consecutive 16-byte pieces; a thread has all its loads under way before it
+// stores. The rows are streamed once, in and out: non-temporal. Bound by HBM.
+constexpr int kStoreVecs = 4;
 __global__ __launch_bounds__(kPageBlock) void paged_store_kernel(PagedStoreArgs a) {
-  const int64_t total = a.n * a.row_vecs;
-  const int64_t i = (int64_t)blockIdx.x * kPageBlock + threadIdx.x;
-  if (i >= total) return;
-  const int64_t row = i / a.row_vecs;
-  const int64_t slot = a.slots[row];
-  if (slot < 0 || slot >= a.total_slots) return;
-  const int64_t to = slot * a.row_vecs + (i - row * a.row_vecs);
-  const u32x4 k = static_cast<const u32x4*>(a.k)[i];
-  const u32x4 v = static_cast<const u32x4*>(a.v)[i];
-  static_cast<u32x4*>(a.k_pages)[to] = k;
-  static_cast<u32x4*>(a.v_pages)[to] = v;
+  const int64_t total = a.n << a.row_shift;
+  const int64_t first = (int64_t)blockIdx.x * (kStoreVecs * kPageBlock) + threadIdx.x;
+  int64_t to[kStoreVecs];
+  u32x4 k[kStoreVecs], v[kStoreVecs];
+#pragma unroll
+  for (int u = 0; u < kStoreVecs; ++u) {
+    const int64_t i = first + u * kPageBlock;
+    to[u] = -1;
+    if (i >= total) continue;
+    const int64_t slot = a.slots[i >> a.row_shift];
+    if (slot >= 0 && slot < a.total_slots) to[u] = (slot << a.row_shift) + (i & ((1 << a.row_shift) - 1));
+    k[u] = __builtin_nontemporal_load(static_cast<const u32x4*>(a.k) + i);
+    v[u] = __builtin_nontemporal_load(static_cast<const u32x4*>(a.v) + i);
+  }
+#pragma unroll
+  for (int u = 0; u < kStoreVecs; ++u) {
+    if (to[u] < 0) continue;
+    __builtin_nontemporal_store(k[u], static_cast<u32x4*>(a.k_pages) + to[u]);
+    __builtin_nontemporal_store(v[u], static_cast<u32x4*>(a.v_pages) + to[u]);
+  }
 }
 
 // ------------------------------------------------------------------ norm, rotation, store
@@ -267,6 +279,16 @@ struct RowPiece<float> {
   }
 };
 
+// Sum over the LPR lanes of a row, the same in each.
+template <int LPR>
+__device__ __forceinline__ float row_sum(float x) {
+  if constexpr (LPR == 32) x += __shfl_xor(x, 16, 64);
+  if constexpr (LPR >= 16) return row16_sum(x);
+  x += __shfl_xor(x, 4, 64);
+  x += __shfl_xor(x, 2, 64);
+  return x + __shfl_xor(x, 1, 64);
+}
+
 // A wave takes one token (or 1/parts of its heads): LPR lanes hold a head's row, 16 bytes each, so 64/LPR
 // heads go at once. Lane l computes the token's angle l; the sines and cosines go through LDS once and stay
 // in registers, where every head uses them. Sum of squares, norm and rotation are in 32 bits, rounded once
@@ -312,44 +334,54 @@ __global__ __launch_bounds__(kPageBlock) void norm_rope_kernel(NormRopeArgs a) {
   const char* krow = static_cast<const char*>(a.k) + token * a.k_stride + (int64_t)(lane % LPR) * 16;
   const char* vrow = static_cast<const char*>(a.v) + token * a.v_stride + (int64_t)(lane % LPR) * 16;
   constexpr int RB = D * (int)sizeof(T);
-  for (int h0 = part * HPW; h0 < heads; h0 += a.parts * HPW) {
-    const int h = h0 + lane / LPR;
-    const bool on = h < heads;
-    const bool is_q = h < a.Hq, is_k = !is_q && h < a.Hq + a.Hkv;
-    const int kv = is_k ? h - a.Hq : h - a.Hq - a.Hkv;
-    u32x4 w{};
-    if (on) w = *reinterpret_cast<const u32x4*>(is_q ? qrow + h * RB : (is_k ? krow : vrow) + kv * RB);
-    u32x4 y = w;
-    float x[N];
-    P::widen(w, x);
-    if (is_q ? a.q_weight != nullptr : is_k && a.k_weight != nullptr) {
-      // every lane of a row takes this branch together
-      float ss = 0.f;
+  // kAhead steps' rows are loaded before the first of them is used
+  constexpr int kAhead = 4;
+  const int step = a.parts * HPW;
+  for (int h0 = part * HPW; h0 < heads; h0 += kAhead * step) {
+    u32x4 w[kAhead];
+    int64_t slot[kAhead];
 #pragma unroll
-      for (int e = 0; e < N; ++e) ss = fmaf(x[e], x[e], ss);
-#pragma unroll
-      for (int o = LPR / 2; o >= 1; o >>= 1) ss += __shfl_xor(ss, o, 64);
-      const float r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
-#pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = x[e] * r * (is_q ? qw[e] : kw[e]);
+    for (int u = 0; u < kAhead; ++u) {
+      const int h = h0 + u * step + lane / LPR;
+      slot[u] = -1;
+      if (h >= heads) continue;
+      const int kv = h < a.Hq + a.Hkv ? h - a.Hq : h - a.Hq - a.Hkv;
+      w[u] = *reinterpret_cast<const u32x4*>(h < a.Hq ? qrow + h * RB : (h < a.Hq + a.Hkv ? krow : vrow) + kv * RB);
+      if (h >= a.Hq) slot[u] = a.slots[token * a.Hkv + kv];
     }
-    if (a.rot) {
-      float p[N];
 #pragma unroll
-      for (int e = 0; e < N; ++e) p[e] = a.interleaved ? x[e ^ 1] : __shfl(x[e], partner, 64);
-      if (is_q || is_k) {
+    for (int u = 0; u < kAhead; ++u) {
+      const int h = h0 + u * step + lane / LPR;
+      if (h0 + u * step >= heads) break;
+      const bool is_q = h < a.Hq, is_k = !is_q && h < a.Hq + a.Hkv;
+      u32x4 y = w[u];
+      float x[N];
+      P::widen(y, x);
+      if (is_q ? a.q_weight != nullptr : is_k && a.k_weight != nullptr) {
+        // every lane of a row takes this branch together
+        float ss = 0.f;
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = fmaf(p[e], sn[e], x[e] * cs[e]);
+        for (int e = 0; e < N; ++e) ss = fmaf(x[e], x[e], ss);
+        ss = row_sum<LPR>(ss);
+        const float r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = x[e] * r * (is_q ? qw[e] : kw[e]);
       }
-    }
-    if (is_q || is_k) y = P::narrow(x);
-    if (!on) continue;
-    if (is_q) {
-      reinterpret_cast<u32x4*>(a.q_out)[(token * a.Hq + h) * LPR + lane % LPR] = y;
-    } else {
-      const int64_t slot = a.slots[token * a.Hkv + kv];
-      if (slot >= 0 && slot < a.total_slots)
-        reinterpret_cast<u32x4*>(is_k ? a.k_pages : a.v_pages)[slot * LPR + lane % LPR] = y;
+      if (a.rot) {
+        float p[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) p[e] = a.interleaved ? x[e ^ 1] : __shfl(x[e], partner, 64);
+        if (is_q || is_k) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) x[e] = fmaf(p[e], sn[e], x[e] * cs[e]);
+        }
+      }
+      if (is_q || is_k) y = P::narrow(x);
+      if (is_q) {
+        reinterpret_cast<u32x4*>(a.q_out)[(token * a.Hq + h) * LPR + lane % LPR] = y;
+      } else if (slot[u] >= 0 && slot[u] < a.total_slots) {
+        reinterpret_cast<u32x4*>(is_k ? a.k_pages : a.v_pages)[slot[u] * LPR + lane % LPR] = y;
+      }
     }
   }
 }
@@ -373,10 +405,9 @@ hipError_t launch_page_update(const PageArgs& a, int cus, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_paged_store(const PagedStoreArgs& a, int cus, hipStream_t stream) {
-  (void)cus;
+hipError_t launch_paged_store(const PagedStoreArgs& a, hipStream_t stream) {
   if (a.n == 0) return hipSuccess;
-  const int64_t blocks = (a.n * a.row_vecs + kPageBlock - 1) / kPageBlock;
+  const int64_t per = kStoreVecs * kPageBlock, blocks = ((a.n << a.row_shift) + per - 1) / per;
   prof_begin("paged_store", stream);
   paged_store_kernel<<<dim3((unsigned)blocks), dim3(kPageBlock), 0, stream>>>(a);
   prof_end(stream);

@@ -209,10 +209,9 @@ sgdkv_status sgdkv_paged_store(const sgdkv_page_pool* pool, const void* k_rows, 
     return fail(SGDKV_ERR_INVALID_ARG, "n = %lld rows out of range", (long long)n);
   if (n > 0)
     if (sgdkv_status st = check_ptrs({{k_rows, "k_rows"}, {v_rows, "v_rows"}, {slots, "slots"}})) return st;
-  int cus = 0;
-  if (sgdkv_status st = host_check_device(&cus)) return st;
+  if (sgdkv_status st = host_check_device(nullptr)) return st;
   sgdkv::PagedStoreArgs a{};
-  a.row_vecs = pool->head_dim * elt_bytes(pool->dtype) / 16;
+  a.row_shift = log2_of(pool->head_dim * elt_bytes(pool->dtype) / 16);
   a.n = n;
   a.total_slots = pool->num_pages * pool->page_size;
   a.k = k_rows;
@@ -221,7 +220,7 @@ sgdkv_status sgdkv_paged_store(const sgdkv_page_pool* pool, const void* k_rows, 
   a.k_pages = pool->k_pages;
   a.v_pages = pool->v_pages;
   (void)hipGetLastError();
-  return launched(sgdkv::launch_paged_store(a, cus, stream_of(stream)), "paged store");
+  return launched(sgdkv::launch_paged_store(a, stream_of(stream)), "paged store");
 }
 
 sgdkv_status sgdkv_norm_rope_store(const sgdkv_page_pool* pool, const sgdkv_norm_rope_desc* desc, const void* q,

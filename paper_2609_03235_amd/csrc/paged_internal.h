@@ -36,7 +36,7 @@ hipError_t launch_page_update(const PageArgs& a, int cus, hipStream_t stream);
 
 // ------------------------------------------------------------- rows into pages
 struct PagedStoreArgs {
-  int row_vecs;         // 16-byte vectors per row
+  int row_shift;        // log2 of a row's 16-byte pieces
   int64_t n;            // rows
   int64_t total_slots;  // rows of the pool
   const void* k;
@@ -45,7 +45,7 @@ struct PagedStoreArgs {
   void* k_pages;
   void* v_pages;
 };
-hipError_t launch_paged_store(const PagedStoreArgs& a, int cus, hipStream_t stream);
+hipError_t launch_paged_store(const PagedStoreArgs& a, hipStream_t stream);
 
 struct NormRopeArgs {
   int T, Hq, Hkv, D, dtype;
