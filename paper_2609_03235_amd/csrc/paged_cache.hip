@@ -292,7 +292,9 @@ __device__ __forceinline__ float row_sum(float x) {
 // A wave takes one token (or 1/parts of its heads): LPR lanes hold a head's row, 16 bytes each, so 64/LPR
 // heads go at once. Lane l computes the token's angle l; the sines and cosines go through LDS once and stay
 // in registers, where every head uses them. Sum of squares, norm and rotation are in 32 bits, rounded once
-// at the store.
+// at the store. Bound by HBM: four heads' loads ahead of their use and stores that do not displace the inputs from
+// the caches (80 heads of 8191 tokens, 168 MB in and out: 95 us without either, 80 and 73 with the first, 60 to 70
+// with both; the stores make no difference up to 4096 tokens).
 template <typename T, int D>
 __global__ __launch_bounds__(kPageBlock) void norm_rope_kernel(NormRopeArgs a) {
   using P = RowPiece<T>;
@@ -378,9 +380,10 @@ __global__ __launch_bounds__(kPageBlock) void norm_rope_kernel(NormRopeArgs a) {
       }
       if (is_q || is_k) y = P::narrow(x);
       if (is_q) {
-        reinterpret_cast<u32x4*>(a.q_out)[(token * a.Hq + h) * LPR + lane % LPR] = y;
+        __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(a.q_out) + (token * a.Hq + h) * LPR + lane % LPR);
       } else if (slot[u] >= 0 && slot[u] < a.total_slots) {
-        reinterpret_cast<u32x4*>(is_k ? a.k_pages : a.v_pages)[slot[u] * LPR + lane % LPR] = y;
+        __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(is_k ? a.k_pages : a.v_pages) + slot[u] * LPR +
+                                           lane % LPR);
       }
     }
   }
