@@ -251,6 +251,45 @@ __device__ __forceinline__ u32x2 lds_transposed(const char* p) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)(p)));
 }
 
+// Masked keys have probability zero, and zero times a value that is not finite is NaN. Keys past every row's last
+// one are loaded as zeros. In a tile with keys that some rows see and others do not, clean_values sets values that
+// are not finite to zero in LDS, and notes the first such key of each column: as a row sees the keys up to some
+// key, it sees such a value exactly if it sees the first, and its output is then NaN. (The same in registers, where
+// the products are made, cost the tiles without masks up to a third of their time.)
+// ROWS rows from key0 on, whose 16-byte pieces lie where `swizzle` says; by every wave that uses them.
+template <int EB, int RB, int ROWS, typename F>
+__device__ __forceinline__ void clean_values(char* vals, int key0, int* first_odd, F swizzle) {
+  constexpr int VPR = RB / 16;
+  constexpr uint32_t kOdd = 0x7F800000u;  // the exponent of infinities and NaN; bf16 in each half
+#pragma unroll 1
+  for (int i = threadIdx.x & 63; i < ROWS * VPR; i += 64) {
+    const int r = i / VPR, col = ((i % VPR) ^ swizzle(r)) * (16 / EB);
+    u32x4* at = reinterpret_cast<u32x4*>(vals + i * 16);
+    u32x4 v = *at;
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = max(top, EB == 2 ? max(v[e] & kOdd, v[e] << 16 & kOdd) : v[e] & kOdd);
+    if (top != kOdd) continue;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if ((v[e] & kOdd) == kOdd) {
+        atomicMin(&first_odd[col + (EB == 2 ? 2 * e + 1 : e)], key0 + r);
+        v[e] &= EB == 2 ? 0xFFFFu : 0u;
+      }
+      if (EB == 2 && (v[e] << 16 & kOdd) == kOdd) {
+        atomicMin(&first_odd[col + 2 * e], key0 + r);
+        v[e] &= 0xFFFF0000u;
+      }
+    }
+    *at = v;
+  }
+}
+// Columns col .. col + 3 of a row that sees `seen` keys.
+__device__ __forceinline__ f32x4 lose_odd(f32x4 o, const int* first_odd, int col, int seen) {
+  const int4 odd = *reinterpret_cast<const int4*>(first_odd + col);
+  return f32x4{odd.x < seen ? NAN : o[0], odd.y < seen ? NAN : o[1], odd.z < seen ? NAN : o[2], odd.w < seen ? NAN : o[3]};
+}
+
 // Four consecutive columns of an output row.
 __device__ __forceinline__ void store_out4(const PagedAttnArgs& a, int64_t row, int D, int col, f32x4 v) {
   if (a.out_dtype) {

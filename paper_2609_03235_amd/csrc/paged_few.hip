@@ -42,6 +42,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
   __shared__ __attribute__((aligned(16))) char lds[kAttnWaves][kWaveLds];
   __shared__ __attribute__((aligned(16))) char qlds[QLDS ? M * QP : 16];
   __shared__ float mws[kAttnWaves][M], sws[kAttnWaves][M];
+  __shared__ __attribute__((aligned(16))) int first_odd[D];
   __shared__ LineScratch sc;
 
   const int tid = threadIdx.x, wid = uniform(tid >> 6), lane = tid & 63;
@@ -79,6 +80,9 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
       const int tok0 = at.tile * a.tokens, ntok = min(a.tokens, g.n - tok0);
       const int nrow = ntok * a.G;
       const int32_t* table = a.tables + (int64_t)at.seg * a.max_pages;
+      const int first_seen = seen_by(a, g, tok0);
+      if (tid < D) first_odd[tid] = 0x7FFFFFFF;
+      __syncthreads();  // and the tile before is done with LDS
       auto first_row = [&](int j) { return j * KT + wid * STEP; };
       int page[U];
 #pragma unroll
@@ -104,7 +108,6 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
         }
       }
       if constexpr (QLDS) {
-        __syncthreads();  // the tile before is done with its queries
         for (int i = tid; i < M * S::VPR; i += kAttnBlock) {
           const int r = i / S::VPR, c = i % S::VPR;
           *reinterpret_cast<u32x4*>(qlds + r * QP + c * 16) = ld128(qr, query_off(r) + c * 16);
@@ -162,7 +165,8 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
             for (int u = 0; u < U; ++u) y[qb][u] = mma(k[u][c], qf, y[qb][u]);
           }
         if (j + 1 < j1) load(j + 1);
-        const char* vals = stage + (j & 1) * S::STAGE;
+        char* vals = stage + (j & 1) * S::STAGE;
+        if (r0 + STEP > first_seen && r0 < limit) clean_values<EB, RB, STEP>(vals, r0, first_odd, S::swizzle);
         float p[QB][U][4];
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
@@ -269,6 +273,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
             sum = fmaf(sws[x][r], f, sum);
             acc += f * *reinterpret_cast<const f32x4*>(lds[x] + (lrow * OP + col) * 4);
           }
+          acc = lose_odd(acc, first_odd, col, seen_by(a, g, tok0 + r / a.G));
           if (whole) {
             const int tok = r / a.G, hd = r - tok * a.G;
             const int64_t row = (int64_t)(g.t0 + tok0 + tok) * a.Hq + h * a.G + hd;

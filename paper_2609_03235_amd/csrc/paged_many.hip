@@ -77,6 +77,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
   constexpr int EB = S::EB, RB = S::RB, KT = S::KT, NC = S::NC, NK = S::NK, ND = S::ND, NL = S::NL;
   constexpr int M = 128;
   __shared__ __attribute__((aligned(16))) char lds[2][2][S::TILE];  // two buffers of keys and values
+  __shared__ __attribute__((aligned(16))) int first_odd[D];
   __shared__ LineScratch sc;
 
   const int tid = threadIdx.x, wid = uniform(tid >> 6), lane = tid & 63;
@@ -149,11 +150,12 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
-      // One tile of keys from LDS. EDGE: some row does not see all of it; `left` is how many of the keys from
-      // 4 * half on this lane's row sees.
-      auto attend = [&](const char* kb, auto edge, int left) {
+      // One tile of keys, from key0 on, out of LDS. EDGE: some row does not see all of it; `left` is how many of the
+      // keys from 4 * half on this lane's row sees.
+      auto attend = [&](char* kb, auto edge, int key0) {
+        const int left = seen - key0 - 4 * half;
         constexpr bool EDGE = decltype(edge)::value;
-        const char* vb = kb + S::TILE;
+        char* vb = kb + S::TILE;
         // products first where waves compete: the other waves' exponentials fill in
         __builtin_amdgcn_s_setprio(1);
         f32x16 y[NK];
@@ -216,42 +218,46 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
           exps(m == -INFINITY ? 0.f : m);  // nothing seen so far: all are 0
         }
         s += sum;
+        if constexpr (EDGE) clean_values<EB, RB, KT>(vb, key0, first_odd, S::value_swizzle);
         __builtin_amdgcn_s_setprio(1);
         if constexpr (EB == 2) {
           const int l16 = lane & 15;
           const int row = 4 * half + l16 / 4;                        // and 8, 16, ... further on: the same swizzle
           const int piece = 2 * ((lane >> 4) & 1) + (l16 & 3) / 2;  // of a block's four
           const char* vp = vb + row * RB + (l16 & 1) * 8;
+          auto values = [&](int t, int d) {
+            const char* vd = vp + (((4 * d + piece) ^ S::value_swizzle(row)) * 16);
+            const u32x2 v0 = lds_transposed(vd + 16 * t * RB), v1 = lds_transposed(vd + (16 * t + 8) * RB);
+            return u32x4{v0.x, v0.y, v1.x, v1.y};
+          };
 #pragma unroll
-          for (int t = 0; t < KT / 16; ++t) {
+          for (int t = 0; t < KT / 16; ++t)
 #pragma unroll
             for (int d = 0; d < ND; ++d) {
-              const char* vd = vp + (((4 * d + piece) ^ S::value_swizzle(row)) * 16);
-              const u32x2 v0 = lds_transposed(vd + 16 * t * RB), v1 = lds_transposed(vd + (16 * t + 8) * RB);
-              const u32x4 vt = {v0.x, v0.y, v1.x, v1.y};
-              o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt), p.piece(t), o[d], 0, 0, 0);
-              if (FINE)
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt), p.rest(t), o[d], 0, 0, 0);
+              const bf16x8 vt = __builtin_bit_cast(bf16x8, values(t, d));
+              o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, p.piece(t), o[d], 0, 0, 0);
+              if (FINE) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, p.rest(t), o[d], 0, 0, 0);
             }
-          }
         } else {
+          auto value = [&](int n, int i, int d) {
+            const int row = 32 * n + 8 * (i / 4) + 4 * half + i % 4;
+            return *reinterpret_cast<const float*>(vb + row * RB +
+                                                   (((8 * d + lq / 4) ^ S::value_swizzle(4 * half)) * 16) + (lq & 3) * 4);
+          };
 #pragma unroll
           for (int n = 0; n < NK; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int row = 32 * n + 8 * (i / 4) + 4 * half + i % 4;
+            for (int i = 0; i < 16; ++i)
 #pragma unroll
               for (int d = 0; d < ND; ++d) {
-                const float v = *reinterpret_cast<const float*>(
-                    vb + row * RB + (((8 * d + lq / 4) ^ S::value_swizzle(4 * half)) * 16) + (lq & 3) * 4);
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p.v[n][i], o[d], 0, 0, 0);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(n, i, d), p.v[n][i], o[d], 0, 0, 0);
               }
-            }
         }
         __builtin_amdgcn_s_setprio(0);
       };
 
       __syncthreads();  // the buffers of the tile before are done with
+      if (tid < D) first_odd[tid] = 0x7FFFFFFF;
       load(j0);
       page = uniform(group_page(a, table, (j0 + 1) * KT + my_row, limit));
       wait_loads();
@@ -263,7 +269,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
           // the page of the tile after the next, asked for before the next tile's loads and used after them
           const int page2 = group_page(a, table, (j + 2) * KT + my_row, limit);
           if (j + 1 < j1) load(j + 1);
-          if (j * KT < hi) attend(lds[j & 1][0], edge, seen - j * KT - 4 * half);
+          if (j * KT < hi) attend(lds[j & 1][0], edge, j * KT);
           wait_loads();
           page = uniform(page2);
           __syncthreads();
@@ -272,6 +278,10 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
       tiles(min(j1, seen_by(a, g, tok0) / KT), std::false_type{});
       tiles(j1, std::true_type{});
       s += __shfl_xor(s, 32, 64);
+      auto result = [&](int d, int i) {
+        return lose_odd(f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]}, first_odd,
+                        32 * d + 8 * i + 4 * half, seen);
+      };
       if (on) {
         const bool whole = j0 == 0 && j1 == nkt;
         if (whole) {
@@ -282,7 +292,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               store_out4(a, row, D, 32 * d + 8 * i + 4 * half,
-                         f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]} * inv);
+                         result(d, i) * inv);
           if (a.lse && half == 0) a.lse[row] = lse_of(m, s);
         } else {
           const int64_t slot = 2 * (int64_t)w + (at.start > share * w ? 1 : 0);
@@ -291,7 +301,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               *reinterpret_cast<f32x4*>(a.part + (slot * M + r) * D + 32 * d + 8 * i + 4 * half) =
-                  f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+                  result(d, i);
           if (half == 0) {
             a.part_ms[(slot * M + r) * 2] = m;
             a.part_ms[(slot * M + r) * 2 + 1] = s;
