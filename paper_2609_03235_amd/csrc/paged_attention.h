@@ -239,9 +239,15 @@ __device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
   f32x2 v = {x, y};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
-// What packing rounded away.
-__device__ __forceinline__ uint32_t pack_bf16_rest(float x, float y, uint32_t hi) {
-  return pack_bf16(x - bf16_lo(hi), y - bf16_hi(hi));
+// x and y as sums of three bf16 terms each, which hold all 24 bits: word e of each term.
+__device__ __forceinline__ void split_bf16(float x, float y, u32x4 (&to)[3], int e) {
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const uint32_t w = pack_bf16(x, y);
+    to[k][e] = w;
+    x -= bf16_lo(w);
+    y -= bf16_hi(w);
+  }
 }
 
 // Four keys (rows) by the wave's 16-lane groups' columns, transposed: lane i of a group receives column i of

@@ -28,7 +28,8 @@ struct FewShape {
   }
 };
 
-// QB: 16-row query blocks. FINE: probabilities as two bf16 terms (fp32 output of bf16 inputs).
+// QB: 16-row query blocks. FINE: probabilities as three bf16 terms, all their 24 bits (fp32 output of
+// bf16 inputs).
 template <typename T, int D, int QB, bool FINE>
 __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs a) {
   using S = FewShape<T, D>;
@@ -198,19 +199,15 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
           }
         }
         if constexpr (EB == 2) {
-          u32x4 ph[QB], pl[QB];
+          u32x4 piece[QB][FINE ? 3 : 1];
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb) {
+          for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              ph[qb][2 * u] = pack_bf16(p[qb][u][0], p[qb][u][1]);
-              ph[qb][2 * u + 1] = pack_bf16(p[qb][u][2], p[qb][u][3]);
-              if (FINE) {
-                pl[qb][2 * u] = pack_bf16_rest(p[qb][u][0], p[qb][u][1], ph[qb][2 * u]);
-                pl[qb][2 * u + 1] = pack_bf16_rest(p[qb][u][2], p[qb][u][3], ph[qb][2 * u + 1]);
-              }
+            for (int e = 0; e < 4; ++e) {
+              const float x = p[qb][e / 2][2 * (e % 2)], y = p[qb][e / 2][2 * (e % 2) + 1];
+              if constexpr (FINE) split_bf16(x, y, piece[qb], e);
+              else piece[qb][0][e] = pack_bf16(x, y);
             }
-          }
           const int row = 4 * lg + lr / 4;  // and 16 further on: the same swizzle
           const char* vp = vals + row * RB + (lr & 1) * 8;
 #pragma unroll
@@ -220,10 +217,9 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
             Frag<__bf16> vt;
             vt.v = u32x4{v0.x, v0.y, v1.x, v1.y};
 #pragma unroll
-            for (int qb = 0; qb < QB; ++qb) {
-              o[qb][d] = mma(vt, Frag<__bf16>{ph[qb]}, o[qb][d]);
-              if (FINE) o[qb][d] = mma(vt, Frag<__bf16>{pl[qb]}, o[qb][d]);
-            }
+            for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+              for (int k = 0; k < (FINE ? 3 : 1); ++k) o[qb][d] = mma(vt, Frag<__bf16>{piece[qb][k]}, o[qb][d]);
           }
         } else {
 #pragma unroll

@@ -44,31 +44,21 @@ struct Probs<float, false, NK> {
     v[n][i] = x;
     v[n][i + 1] = y;
   }
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int n = 0; n < NK; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[n][i] = 0.f;
-  }
 };
-template <bool FINE, int NK>
-struct Probs<__bf16, FINE, NK> {
-  u32x4 hi[2 * NK], lo[FINE ? 2 * NK : 1];  // piece t: keys 16t .. 16t + 15 in the accumulator's order
+template <int NK>
+struct Probs<__bf16, false, NK> {
+  u32x4 hi[2 * NK];  // piece t: keys 16t .. 16t + 15 in the accumulator's order
   __device__ __forceinline__ void set(int n, int i, float x, float y) {
-    const uint32_t w = pack_bf16(x, y);
-    hi[2 * n + i / 8][(i % 8) / 2] = w;
-    if (FINE) lo[2 * n + i / 8][(i % 8) / 2] = pack_bf16_rest(x, y, w);
+    hi[2 * n + i / 8][(i % 8) / 2] = pack_bf16(x, y);
   }
-  __device__ __forceinline__ void clear() {
+  __device__ __forceinline__ void pieces(int t, u32x4 (&to)[1]) const { to[0] = hi[t]; }
+};
+template <int NK>
+struct Probs<__bf16, true, NK> : Probs<float, false, NK> {
+  __device__ __forceinline__ void pieces(int t, u32x4 (&to)[3]) const {
 #pragma unroll
-    for (int t = 0; t < 2 * NK; ++t) hi[t] = u32x4{0, 0, 0, 0};
-    if (FINE) {
-#pragma unroll
-      for (int t = 0; t < 2 * NK; ++t) lo[t] = u32x4{0, 0, 0, 0};
-    }
+    for (int e = 0; e < 4; ++e) split_bf16(this->v[t / 2][8 * (t % 2) + 2 * e], this->v[t / 2][8 * (t % 2) + 2 * e + 1], to, e);
   }
-  __device__ __forceinline__ bf16x8 piece(int t) const { return __builtin_bit_cast(bf16x8, hi[t]); }
-  __device__ __forceinline__ bf16x8 rest(int t) const { return __builtin_bit_cast(bf16x8, lo[FINE ? t : 0]); }
 };
 
 template <typename T, int D, bool FINE>
@@ -223,21 +213,25 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
         if constexpr (EB == 2) {
           const int l16 = lane & 15;
           const int row = 4 * half + l16 / 4;                        // and 8, 16, ... further on: the same swizzle
-          const int piece = 2 * ((lane >> 4) & 1) + (l16 & 3) / 2;  // of a block's four
+          const int place = 2 * ((lane >> 4) & 1) + (l16 & 3) / 2;  // of a block's four pieces
           const char* vp = vb + row * RB + (l16 & 1) * 8;
           auto values = [&](int t, int d) {
-            const char* vd = vp + (((4 * d + piece) ^ S::value_swizzle(row)) * 16);
+            const char* vd = vp + (((4 * d + place) ^ S::value_swizzle(row)) * 16);
             const u32x2 v0 = lds_transposed(vd + 16 * t * RB), v1 = lds_transposed(vd + (16 * t + 8) * RB);
             return u32x4{v0.x, v0.y, v1.x, v1.y};
           };
 #pragma unroll
-          for (int t = 0; t < KT / 16; ++t)
+          for (int t = 0; t < KT / 16; ++t) {
+            u32x4 piece[FINE ? 3 : 1];
+            p.pieces(t, piece);
 #pragma unroll
             for (int d = 0; d < ND; ++d) {
               const bf16x8 vt = __builtin_bit_cast(bf16x8, values(t, d));
-              o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, p.piece(t), o[d], 0, 0, 0);
-              if (FINE) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, p.rest(t), o[d], 0, 0, 0);
+#pragma unroll
+              for (int k = 0; k < (FINE ? 3 : 1); ++k)
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, __builtin_bit_cast(bf16x8, piece[k]), o[d], 0, 0, 0);
             }
+          }
         } else {
           auto value = [&](int n, int i, int d) {
             const int row = 32 * n + 8 * (i / 4) + 4 * half + i % 4;
