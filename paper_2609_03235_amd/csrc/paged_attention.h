@@ -92,7 +92,7 @@ struct LineTile {
 };
 
 struct LineScratch {
-  int64_t wave_sum[kAttnWaves][2];
+  int64_t wave_sum[kAttnWaves];
   int64_t start;
   int seg;
   PagedSeg g;
@@ -102,60 +102,73 @@ __device__ __forceinline__ PagedSeg uniform(const PagedSeg& g) {
   return PagedSeg{uniform(g.t0), uniform(g.n), uniform(g.rows), uniform(g.base), uniform(g.tiles)};
 }
 
-// The whole workgroup adds the segments up and finds worker w's piece of the line, [at.., end): false if there
-// is none. share receives the pieces' length: an equal part, at least min_cost.
+// Exclusive prefix sum over the workgroup; total = the sum. Two barriers where it is used twice in a row.
+template <typename I>
+__device__ __forceinline__ I block_prefix(I mine, int64_t* wave_sum, I& total) {
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+  I x = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const I y = sizeof(I) == 8 ? (I)__shfl_up((long long)x, o, 64) : (I)__shfl_up((int)x, o, 64);
+    if (lane >= o) x += y;
+  }
+  if (lane == 63) wave_sum[wid] = x;
+  __syncthreads();
+  I before = x - mine;
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < kAttnWaves; ++i) {
+    const I y = (I)wave_sum[i];
+    if (i < wid) before += y;
+    total += y;
+  }
+  return before;
+}
+
+// The whole workgroup adds the segments up and finds worker w's piece of the line, [share * w, end): false if
+// there is none. share receives the pieces' length: an equal part, at least 2^min_shift.
 // PAD (segments of one tile): where all workers' least pieces cover the segments rounded up to whole pieces,
 // the line is that, and no worker has parts of two tiles. Short calls are bound by latency: one token over four
-// segments of 8K rows took 14.9 us with, 9 without the three workers that had two.
+// segments of 8K rows took 14.9 us with, 10.4 without the three workers that had two.
 template <bool PAD>
 __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, LineScratch& sc, int w, int64_t& share,
                                            int64_t& end, bool& padded, LineTile& at) {
-  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+  const int tid = threadIdx.x;
   const int per = (a.S + kAttnBlock - 1) / kAttnBlock;
   const int s0 = min(tid * per, a.S), s1 = min(s0 + per, a.S);
-  int64_t mine[2] = {0, 0};
+  const int64_t least = (int64_t)1 << a.min_shift;
+  int64_t mine = 0;
+  int pieces = 0;  // of the least length, cut off where there are too many for all workers
   PagedSeg g{};
-  auto pad = [&](int64_t c) { return (c + a.min_cost - 1) & ~(a.min_cost - 1); };  // min_cost is a power of two
+  auto pieces_of = [&](int64_t c) { return (int)min((c + least - 1) >> a.min_shift, (int64_t)kPagedWorkers + 1); };
   for (int s = s0; s < s1; ++s) {
     g = paged_seg(a, s);
     const int64_t c = cost_of(a, g, g.tiles);
-    mine[0] += c;
-    if (PAD) mine[1] += pad(c);
+    mine += c;
+    if (PAD) pieces += pieces_of(c);
   }
-  int64_t before[2], total[2] = {0, 0};
-#pragma unroll
-  for (int k = 0; k < (PAD ? 2 : 1); ++k) {
-    int64_t x = mine[k];
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t y = __shfl_up((long long)x, o, 64);
-      if (lane >= o) x += y;
-    }
-    if (lane == 63) sc.wave_sum[wid][k] = x;
-    before[k] = x - mine[k];
+  padded = false;
+  int64_t run = 0, all = 0;
+  if constexpr (PAD) {
+    int n;
+    run = (int64_t)block_prefix(pieces, sc.wave_sum, n) << a.min_shift;
+    padded = uniform(n) <= kPagedWorkers;
+    all = (int64_t)uniform(n) << a.min_shift;
+    if (!padded) __syncthreads();
   }
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < (PAD ? 2 : 1); ++k)
-#pragma unroll
-    for (int i = 0; i < kAttnWaves; ++i) {
-      const int64_t y = sc.wave_sum[i][k];
-      if (i < wid) before[k] += y;
-      total[k] += y;
-    }
-  padded = PAD && total[1] <= a.workers * a.min_cost;
-  const int64_t all = uniform(padded ? total[1] : total[0]);
-  share = uniform((all + a.workers - 1) / a.workers);
-  if (share < a.min_cost) share = a.min_cost;
+  if (!padded) {
+    run = block_prefix(mine, sc.wave_sum, all);
+    all = uniform(all);
+  }
+  share = padded ? least : max((all + kPagedWorkers - 1) / kPagedWorkers, least);
   const int64_t want = share * w;
   if (want >= all) return false;
   end = min(want + share, all);
-  int64_t run = padded ? before[1] : before[0];
-  if (want >= run && want < run + (padded ? mine[1] : mine[0])) {
+  if (want >= run && want < run + (padded ? (int64_t)pieces << a.min_shift : mine)) {
     for (int s = s0; s < s1; ++s) {
       if (per > 1) g = paged_seg(a, s);
       int64_t c = cost_of(a, g, g.tiles);
-      if (padded) c = pad(c);
+      if (padded) c = (int64_t)pieces_of(c) << a.min_shift;
       if (want < run + c) {
         sc.seg = s;
         sc.start = run;
@@ -180,19 +193,21 @@ __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, LineScratch& 
   return true;
 }
 
-// What a worker leaves for the merge (see PagedAttnArgs::shared). `at` is its last tile, of nkt key tiles.
+// What a worker leaves for the merge (see PagedAttnArgs::shared) about a tile of nkt key tiles.
 __device__ __forceinline__ void leave_shared(const PagedAttnArgs& a, int w, int64_t share, const LineTile& at, int nkt) {
   const int64_t own = share * w;
-  const int last = (int)((at.start + (int64_t)(nkt - 1) * a.key_tile) / share);
-  const bool left = at.start >= own && last > w;
-  if (threadIdx.x == 0) a.shared[w] = make_int4(at.seg, at.tile, left ? last : -1, at.start > own ? 1 : 0);
+  if (threadIdx.x != 0 || at.start < own) return;  // begun by a worker before
+  const int64_t last_key = at.start + (int64_t)(nkt - 1) * a.key_tile;
+  const int last = last_key < own + share ? -1 : (int)(last_key / share);
+  if (a.by_tile) a.shared[at.seg * a.max_tiles + at.tile] = make_int4(at.seg, at.tile, 2 * w + (at.start > own), last);
+  else if (last >= 0) a.shared[w] = make_int4(at.seg, at.tile, 2 * w + (at.start > own), last);
 }
 
 // Neighbouring workers on one XCD (workgroups go to the eight XCDs in turn): they read the same segment's
 // rows, from one L2.
-__device__ __forceinline__ int worker_of(const PagedAttnArgs& a) {
-  const int bid = blockIdx.x;
-  return a.workers % 8 == 0 ? (bid & 7) * (a.workers >> 3) + (bid >> 3) : bid;
+__device__ __forceinline__ int worker_of() {
+  static_assert(kPagedWorkers % 8 == 0, "workers per XCD");
+  return (blockIdx.x & 7) * (kPagedWorkers / 8) + (blockIdx.x >> 3);
 }
 
 // Buffer over the 16-row group of a segment that starts at row r0, `valid` rows of it (0 or fewer: none).

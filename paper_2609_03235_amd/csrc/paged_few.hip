@@ -48,11 +48,11 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
 
   const int tid = threadIdx.x, wid = uniform(tid >> 6), lane = tid & 63;
   const int lr = lane & 15, lg = lane >> 4;
-  const int w = worker_of(a);
+  const int w = worker_of();
   int64_t share, end;
   bool padded;
   LineTile at;
-  if (tid == 0) a.shared[w] = make_int4(0, 0, -1, 0);
+  if (!a.by_tile && tid == 0) a.shared[w] = make_int4(0, 0, 0, -1);
   if (!find_piece<true>(a, sc, w, share, end, padded, at)) return;
   int64_t pos = share * w;
   char* stage = lds[wid];
@@ -287,14 +287,14 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
       __syncthreads();
     }
     const int64_t next = padded ? end : at.start + max(limit, 1);
-    if (next >= end) leave_shared(a, w, share, at, nkt);
+    leave_shared(a, w, share, at, nkt);
     at.start = pos = next;
     ++at.tile;
   }
 }
 
-// Joins the parts of the query tiles that several workers shared: workgroup (w, y) looks at the tile that
-// worker w began and left to the next ones, if any. Lanes in groups of D / 4 hold a row, four columns each.
+// Joins the parts of the query tiles that several workers shared: workgroup (x, y) looks at entry x of `shared`.
+// Lanes in groups of D / 4 hold a row, four columns each.
 //   MANY = false: tiles of few rows and up to hundreds of parts. A workgroup takes one row; the groups take its
 //     parts in turn with a running maximum and are then joined in order.
 //   MANY = true: tiles of many rows and seldom more than three parts. A group takes a row of its own (the rows
@@ -305,25 +305,47 @@ __global__ __launch_bounds__(kAttnBlock) void paged_merge_kernel(PagedAttnArgs a
   __shared__ float ms[NG], ss[NG];
   __shared__ __attribute__((aligned(16))) float os[NG][D];
   const int tid = threadIdx.x, grp = tid / LPS, col = 4 * (tid % LPS);
-  const int w = blockIdx.x;
-  const int4 left = a.shared[w];
-  if (left.z < 0) return;
-  const PagedSeg g = paged_seg(a, left.x);
-  const int M = a.tile_rows, h = left.x % a.Hkv, tok0 = left.y * a.tokens;
-  const int nrow = min(a.tokens, g.n - tok0) * a.G, parts = left.z - w + 1;
+  // The reads come from other XCDs' writes, a microsecond each where one waits for the other: the entry and the
+  // segment's lengths are asked for together.
+  const int4 left = a.shared[blockIdx.x];
+  const int seg = a.by_tile ? blockIdx.x / a.max_tiles : (left.w < 0 ? 0 : left.x);
+  const PagedSeg g = paged_seg(a, seg);
+  if (a.by_tile && (int)blockIdx.x - seg * a.max_tiles >= g.tiles) return;  // no such tile: the entry holds anything
+  if (left.w < 0) return;
+  const int w = left.z >> 1;
+  const int M = a.tile_rows, h = seg % a.Hkv, tok0 = left.y * a.tokens;
+  const int nrow = min(a.tokens, g.n - tok0) * a.G, parts = left.w - w + 1;
   const int r = MANY ? blockIdx.y * NG + grp : blockIdx.y;
   if (r >= nrow) return;
   float m = -INFINITY, s = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int i = MANY ? 0 : grp; i < parts; i += MANY ? 1 : NG) {
-    const int64_t at = (2 * (int64_t)(w + i) + (i == 0 ? left.w : 0)) * M + r;
-    const float pm = a.part_ms[at * 2], ps = a.part_ms[at * 2 + 1];
-    const f32x4 po = *reinterpret_cast<const f32x4*>(a.part + at * D + col);
-    const float mn = fmaxf(m, pm), ref = mn == -INFINITY ? 0.f : mn;
-    const float fo = fast_exp2(m - ref), fn = fast_exp2(pm - ref);
+  // kBatch parts' loads are under way together; a part past the last repeats it with weight zero
+  constexpr int kBatch = 8, STRIDE = MANY ? 1 : NG;
+  for (int i0 = MANY ? 0 : grp; i0 < parts; i0 += kBatch * STRIDE) {
+    float pm[kBatch], ps[kBatch];
+    f32x4 po[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int i = min(i0 + u * STRIDE, parts - 1);
+      const int64_t at = (2 * (int64_t)(w + i) + (i == 0 ? left.z & 1 : 0)) * M + r;
+      pm[u] = a.part_ms[at * 2];
+      ps[u] = a.part_ms[at * 2 + 1];
+      po[u] = *reinterpret_cast<const f32x4*>(a.part + at * D + col);
+    }
+    float mn = m;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, pm[u]);
+    const float ref = mn == -INFINITY ? 0.f : mn, fo = fast_exp2(m - ref);
     m = mn;
-    s = s * fo + ps * fn;
-    o = o * fo + po * fn;
+    s *= fo;
+    o *= fo;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      if (i0 + u * STRIDE >= parts) break;
+      const float fn = fast_exp2(pm[u] - ref);
+      s += ps[u] * fn;
+      o += po[u] * fn;
+    }
   }
   if (!MANY) {
     if (col == 0) {
@@ -356,11 +378,11 @@ template <typename T, int D, int QB>
 void launch_few(const PagedAttnArgs& a, hipStream_t stream) {
   if constexpr (sizeof(T) == 2) {
     if (a.out_dtype == 0) {
-      paged_few_kernel<T, D, QB, true><<<dim3(a.workers), dim3(kAttnBlock), 0, stream>>>(a);
+      paged_few_kernel<T, D, QB, true><<<dim3(kPagedWorkers), dim3(kAttnBlock), 0, stream>>>(a);
       return;
     }
   }
-  paged_few_kernel<T, D, QB, false><<<dim3(a.workers), dim3(kAttnBlock), 0, stream>>>(a);
+  paged_few_kernel<T, D, QB, false><<<dim3(kPagedWorkers), dim3(kAttnBlock), 0, stream>>>(a);
 }
 
 template <typename T, int D>
@@ -396,7 +418,7 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream) {
   prof_begin("paged_merge", stream);
   const int rows = std::min(a.max_new, a.tokens) * a.G;
   const int per = few ? 1 : kAttnBlock / (a.D / 4);  // rows of a workgroup
-  const dim3 grid(a.workers, (rows + per - 1) / per);
+  const dim3 grid(a.by_tile ? a.S * a.max_tiles : kPagedWorkers, (rows + per - 1) / per);
   if (few) {
     if (a.D == 128) paged_merge_kernel<128, false><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
     else paged_merge_kernel<64, false><<<grid, dim3(kAttnBlock), 0, stream>>>(a);

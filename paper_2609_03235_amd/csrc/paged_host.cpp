@@ -84,10 +84,6 @@ sgdkv_status launched(hipError_t e, const char* what) {
 }
 
 // ------------------------------------------------------------- attention plan
-// Workgroups that share the work: two per compute unit of the MI355X. A constant, so that results do not
-// depend on the device.
-constexpr int kPagedWorkers = 512;
-
 sgdkv_status plan_paged(const sgdkv_page_pool* pool, const sgdkv_paged_desc* d, sgdkv::PagedAttnArgs& a,
                         size_t& bytes) {
   if (sgdkv_status st = check_pool_shape(pool)) return st;
@@ -131,11 +127,12 @@ sgdkv_status plan_paged(const sgdkv_page_pool* pool, const sgdkv_paged_desc* d, 
   a.tile_rows = shape.rows;
   a.key_tile = shape.key_tile;
   a.tokens = shape.rows / G;
-  a.workers = kPagedWorkers;
-  a.min_cost = shape.rows < 128 ? 128 : 2 * shape.key_tile;  // a power of two and whole key tiles
+  a.max_tiles = (a.max_new + a.tokens - 1) / a.tokens;
+  a.by_tile = nseg * a.max_tiles <= sgdkv::kPagedWorkers;
+  a.min_shift = log2_of(shape.rows < 128 ? 128 : 2 * shape.key_tile);
   // The workspace follows the bound the caller gave, whatever the tokens of this call.
   const int most_rows = sgdkv::paged_attn_shape(a.dtype, G, d->max_new).rows;
-  bytes = (size_t)kPagedWorkers * (sizeof(int4) + 2 * (size_t)most_rows * (a.D + 2) * sizeof(float));
+  bytes = (size_t)sgdkv::kPagedWorkers * (sizeof(int4) + 2 * (size_t)most_rows * (a.D + 2) * sizeof(float));
   return SGDKV_OK;
 }
 
@@ -342,8 +339,8 @@ sgdkv_status sgdkv_paged_attention(const sgdkv_page_pool* pool, const sgdkv_page
   a.out = out;
   a.lse = lse_out;
   a.shared = static_cast<int4*>(workspace);
-  a.part = reinterpret_cast<float*>(a.shared + a.workers);
-  a.part_ms = a.part + 2 * (size_t)a.workers * a.tile_rows * a.D;
+  a.part = reinterpret_cast<float*>(a.shared + sgdkv::kPagedWorkers);
+  a.part_ms = a.part + 2 * (size_t)sgdkv::kPagedWorkers * a.tile_rows * a.D;
   (void)hipGetLastError();
   return launched(sgdkv::launch_paged_attention(a, stream_of(stream)), "paged attention");
 }

@@ -12,6 +12,9 @@ constexpr int kPageBlock = 256;       // threads per workgroup of the page and r
 constexpr int kMaxPageSegs = 4096;    // segments of one page update (their lengths and prefix sums fill 64 KB of LDS)
 constexpr int kMinPage = 16;          // rows per page: every 16-row group of a segment lies in one page
 constexpr int kMaxPage = 1024;
+// Workgroups that share an attention call: two per compute unit of the MI355X. A constant, so that results do not
+// depend on the device.
+constexpr int kPagedWorkers = 512;
 constexpr int kMaxPagedGroup = 16;    // query heads per KV head
 
 // ------------------------------------------------------------- page update
@@ -80,8 +83,9 @@ struct PagedAttnArgs {
   int tile_rows;     // query rows per tile (M)
   int key_tile;      // key rows per step of a workgroup (KT)
   int tokens;        // new tokens per query tile
-  int workers;       // workgroups that share the work
-  int64_t min_cost;  // key rows a worker takes at least (a multiple of the key tile)
+  int max_tiles;     // query tiles of a segment with max_new tokens
+  int by_tile;
+  int min_shift;     // log2 of the key rows a worker takes at least (whole key tiles)
   const void* q;
   const void* k_pages;
   const void* v_pages;
@@ -91,10 +95,12 @@ struct PagedAttnArgs {
   void* out;
   float* lse;        // optional
   // workspace
-  int4* shared;      // [workers]: the query tile that a worker began and left to the next ones: segment, tile,
-                     // the last worker (-1: none) and 1 if the tile starts after the worker's share does
-  float* part;       // [2 * workers][M][D]: o of a query tile that several workers share
-  float* part_ms;    // [2 * workers][M][2]
+  // Query tiles that a worker began: segment, tile, 2 * that worker (+ 1 if the tile starts after the worker's
+  // share does), and the last worker that has a part of it (-1: no other). [S * max_tiles], an entry per tile, where
+  // that is at most kPagedWorkers (by_tile); otherwise [kPagedWorkers], the tile each worker left to the next ones.
+  int4* shared;
+  float* part;       // [2 * kPagedWorkers][M][D]: o of a query tile that several workers share
+  float* part_ms;    // [2 * kPagedWorkers][M][2]
 };
 // The kernel instance for a shape: query rows per tile and key rows per step.
 struct PagedAttnShape {

@@ -72,11 +72,11 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
 
   const int tid = threadIdx.x, wid = uniform(tid >> 6), lane = tid & 63;
   const int lq = lane & 31, half = lane >> 5;
-  const int w = worker_of(a);
+  const int w = worker_of();
   int64_t share, end;
   bool padded;
   LineTile at;
-  if (tid == 0) a.shared[w] = make_int4(0, 0, -1, 0);
+  if (!a.by_tile && tid == 0) a.shared[w] = make_int4(0, 0, 0, -1);
   if (!find_piece<false>(a, sc, w, share, end, padded, at)) return;
   int64_t pos = share * w;
 
@@ -304,7 +304,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
       }
     }
     const int64_t next = at.start + max(limit, 1);
-    if (next >= end) leave_shared(a, w, share, at, nkt);
+    leave_shared(a, w, share, at, nkt);
     at.start = pos = next;
     ++at.tile;
   }
@@ -314,11 +314,11 @@ template <typename T, int D>
 void launch_many(const PagedAttnArgs& a, hipStream_t stream) {
   if constexpr (sizeof(T) == 2) {
     if (a.out_dtype == 0) {
-      paged_many_kernel<T, D, true><<<dim3(a.workers), dim3(kAttnBlock), 0, stream>>>(a);
+      paged_many_kernel<T, D, true><<<dim3(kPagedWorkers), dim3(kAttnBlock), 0, stream>>>(a);
       return;
     }
   }
-  paged_many_kernel<T, D, false><<<dim3(a.workers), dim3(kAttnBlock), 0, stream>>>(a);
+  paged_many_kernel<T, D, false><<<dim3(kPagedWorkers), dim3(kAttnBlock), 0, stream>>>(a);
 }
 
 }  // namespace
