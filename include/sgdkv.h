@@ -457,7 +457,7 @@ typedef struct sgdkv_norm_rope_desc {
  * slots. Per head, in fp32 and rounded once at the end:
  *   x <- x * weight / sqrt(mean(x^2) + eps)          (with a weight)
  *   (a, b) <- (a cos t - b sin t, b cos t + a sin t)  t = position * inv_freq[i]
- * for the pairs i < rot_dim/2; t is exact to 2^-31 turns whatever the position.
+ * for the pairs i < rot_dim/2; t is good to 2^-31 turns whatever the position.
  * Values are copied.
  * q [T][Hq][d], k and v [T][Hkv][d]: device, the pool's dtype, strides above.
  * positions: device [T] int32. slots: device [T][Hkv] int32; a slot outside
@@ -478,7 +478,7 @@ typedef struct sgdkv_paged_desc {
   int32_t num_q_heads;   /* Hq */
   int32_t num_kv_heads;  /* Hkv, Hq % Hkv == 0, at most 16 query heads per KV head */
   int32_t out_dtype;     /* dtype of out */
-  int64_t num_tokens;    /* T >= 0: tokens of q, out and lse_out */
+  int64_t num_tokens;    /* T >= 0: tokens of q, out and lse_out; T*Hq <= 2^31 - 129 */
   int32_t max_new;       /* >= 1: at least the longest sequence's new tokens */
   int32_t max_pages;     /* columns of tables, >= 1 */
   int32_t causal;        /* 1: a token sees the rows up to its own; 0: all of its segment's */

@@ -54,7 +54,7 @@ __device__ __forceinline__ PagedSeg paged_seg(const PagedAttnArgs& a, int seg) {
   s.t0 = c0;
   s.n = min(c1 - c0, a.max_new);
   s.base = s.rows - (c1 - c0);
-  s.tiles = (int)((uint32_t)(s.n + a.tokens - 1) / (uint32_t)a.tokens);
+  s.tiles = (int)(((uint32_t)s.n + a.tokens - 1) / (uint32_t)a.tokens);
   return s;
 }
 
@@ -194,7 +194,8 @@ __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, LineScratch& 
 }
 
 // What a worker leaves for the merge (see PagedAttnArgs::shared) about a tile of nkt key tiles.
-__device__ __forceinline__ void leave_shared(const PagedAttnArgs& a, int w, int64_t share, const LineTile& at, int nkt) {
+__device__ __forceinline__ void leave_shared(const PagedAttnArgs& a, int w, int64_t share, const LineTile& at,
+                                             int nkt) {
   const int64_t own = share * w;
   if (threadIdx.x != 0 || at.start < own) return;  // begun by a worker before
   const int64_t last_key = at.start + (int64_t)(nkt - 1) * a.key_tile;
@@ -308,7 +309,8 @@ __device__ __forceinline__ void clean_values(char* vals, int key0, int* first_od
 // Columns col .. col + 3 of a row that sees `seen` keys.
 __device__ __forceinline__ f32x4 lose_odd(f32x4 o, const int* first_odd, int col, int seen) {
   const int4 odd = *reinterpret_cast<const int4*>(first_odd + col);
-  return f32x4{odd.x < seen ? NAN : o[0], odd.y < seen ? NAN : o[1], odd.z < seen ? NAN : o[2], odd.w < seen ? NAN : o[3]};
+  return f32x4{odd.x < seen ? NAN : o[0], odd.y < seen ? NAN : o[1], odd.z < seen ? NAN : o[2],
+               odd.w < seen ? NAN : o[3]};
 }
 
 // Four consecutive columns of an output row.

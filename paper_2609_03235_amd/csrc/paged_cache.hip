@@ -223,12 +223,16 @@ __global__ __launch_bounds__(kPageBlock) void paged_store_kernel(PagedStoreArgs 
 }
 
 // ------------------------------------------------------------------ norm, rotation, store
-// sin and cos of 2 pi t: the quarter turn nearest t is taken off in 64 bits, which leaves an angle x in
-// [-pi/4, pi/4] for the Taylor sums (the first terms left out are below 2e-9 and 2e-10), so the angle of a
-// position of millions is as good as that of a small one.
-__device__ __forceinline__ void sincos_turns(double t, float& sin_t, float& cos_t) {
+// sin and cos of position * freq. In turns the angle is position * freq / (2 pi): both products are carried with
+// their rounding errors, and the nearest quarter turn is taken off in 64 bits, which leaves an angle x in
+// [-pi/4, pi/4] for the Taylor sums (the first terms left out are below 2e-9 and 2e-10). So the angle of a position
+// of 2^31 is as good as that of a small one.
+__device__ __forceinline__ void sincos_at(double position, double freq, float& sin_t, float& cos_t) {
+  constexpr double kHi = 0.15915494309189535, kLo = -9.839338337591243e-18;  // 1 / (2 pi)
+  const double a0 = position * freq, a1 = fma(position, freq, -a0);
+  const double t = a0 * kHi, t1 = fma(a0, kHi, -t) + fma(a0, kLo, a1 * kHi);
   const double n = rint(4.0 * t);
-  const float x = (float)((t - 0.25 * n) * 6.283185307179586476925);
+  const float x = (float)((fma(-0.25, n, t) + t1) * 6.283185307179586476925);
   const float z = x * x;
   float s = fmaf(z, 2.7557319e-6f, -1.9841270e-4f);
   s = fmaf(z, s, 8.3333333e-3f);
@@ -308,9 +312,8 @@ __global__ __launch_bounds__(kPageBlock) void norm_rope_kernel(NormRopeArgs a) {
   const int col = (lane % LPR) * N, half = a.rot / 2;
 
   if (live && lane < half) {
-    const double turns = (double)a.positions[token] * ((double)a.inv_freq[lane] * 0.159154943091895335769);
     float s, c;
-    sincos_turns(turns, s, c);
+    sincos_at(a.positions[token], a.inv_freq[lane], s, c);
     sines[wid][lane] = s;
     cosines[wid][lane] = c;
   }

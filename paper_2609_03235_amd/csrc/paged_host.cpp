@@ -101,8 +101,8 @@ sgdkv_status plan_paged(const sgdkv_page_pool* pool, const sgdkv_paged_desc* d, 
   if (nseg > 65535) return fail(SGDKV_ERR_UNSUPPORTED, "batch * num_kv_heads = %lld > 65535", (long long)nseg);
   if (d->out_dtype != SGDKV_DTYPE_F32 && d->out_dtype != SGDKV_DTYPE_BF16)
     return fail(SGDKV_ERR_INVALID_ARG, "out_dtype %d", d->out_dtype);
-  if (d->num_tokens < 0 || d->num_tokens > kMaxInt / d->num_q_heads)
-    return fail(SGDKV_ERR_INVALID_ARG, "num_tokens %lld outside [0, (2^31 - 1) / num_q_heads]",
+  if (d->num_tokens < 0 || d->num_tokens > (kMaxInt - 128) / d->num_q_heads)  // a tile past the end still counts
+    return fail(SGDKV_ERR_INVALID_ARG, "num_tokens %lld outside [0, (2^31 - 129) / num_q_heads]",
                 (long long)d->num_tokens);
   if (d->max_new < 1) return fail(SGDKV_ERR_INVALID_ARG, "max_new %d < 1", d->max_new);
   if (d->causal != 0 && d->causal != 1) return fail(SGDKV_ERR_INVALID_ARG, "causal %d is not 0 or 1", d->causal);

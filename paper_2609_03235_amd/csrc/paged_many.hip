@@ -57,7 +57,10 @@ template <int NK>
 struct Probs<__bf16, true, NK> : Probs<float, false, NK> {
   __device__ __forceinline__ void pieces(int t, u32x4 (&to)[3]) const {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) split_bf16(this->v[t / 2][8 * (t % 2) + 2 * e], this->v[t / 2][8 * (t % 2) + 2 * e + 1], to, e);
+    for (int e = 0; e < 4; ++e) {
+      const float* x = &this->v[t / 2][8 * (t % 2) + 2 * e];
+      split_bf16(x[0], x[1], to, e);
+    }
   }
 };
 
@@ -229,14 +232,15 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
               const bf16x8 vt = __builtin_bit_cast(bf16x8, values(t, d));
 #pragma unroll
               for (int k = 0; k < (FINE ? 3 : 1); ++k)
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, __builtin_bit_cast(bf16x8, piece[k]), o[d], 0, 0, 0);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, __builtin_bit_cast(bf16x8, piece[k]), o[d], 0, 0,
+                                                               0);
             }
           }
         } else {
           auto value = [&](int n, int i, int d) {
             const int row = 32 * n + 8 * (i / 4) + 4 * half + i % 4;
-            return *reinterpret_cast<const float*>(vb + row * RB +
-                                                   (((8 * d + lq / 4) ^ S::value_swizzle(4 * half)) * 16) + (lq & 3) * 4);
+            const int at = ((8 * d + lq / 4) ^ S::value_swizzle(4 * half)) * 16 + (lq & 3) * 4;
+            return *reinterpret_cast<const float*>(vb + row * RB + at);
           };
 #pragma unroll
           for (int n = 0; n < NK; ++n)

@@ -225,6 +225,7 @@ ROPE_CASES = [
     (3, 8, 8, 64, 32, False, True, F32, 2**31 - 4),
     (65, 16, 2, 128, 96, True, False, F32, 77),
     (2, 3, 3, 64, 16, True, False, BF, 5),
+    (5, 4, 2, 128, 128, False, False, F32, -100003),
     (9, 2, 1, 128, 0, True, False, BF, 0),
     (4000, 4, 2, 128, 128, True, False, BF, 3),
 ]
@@ -672,3 +673,91 @@ def test_page_update_of_the_most_segments():
     add = [(i * 29) % 50 - 12 for i in range(4096)]
     tables, free, head = _start(rows, 16, 6, 20000, 2)
     _update_both(rows, add, tables, free, head, 16, sum(max(x, 0) for x in add) + 3, 1, True)
+
+
+def test_pools_beyond_4_gib():
+    """Pages whose bytes and rows lie past 2^32 bytes of the pool: stores, rotation and both attention kernels."""
+    _say("pools beyond 4 GiB")
+    d, page, hq, hkv = 128, 256, 8, 2
+    n_pages = (5 << 30) // (page * d * 2)
+    kp, vp = (torch.empty(n_pages, page, d, dtype=BF, device=DEV) for _ in range(2))
+    for new in ([1, 2], [40, 9]):
+        c = Case(new, [300, 700, 257, 512], hq, hkv, d, page, BF, seed=21)
+        far = c.tables.clone()
+        used = c.tables >= 0
+        far[used] = n_pages - 1 - c.tables[used]
+        slot = lambda s: (far[s].long()[:, None] * page + torch.arange(page, device=DEV)).flatten()[:c.rows_host[s]]
+        for s in range(4):
+            sg.paged_store(c.k[s], c.v[s], slot(s).to(torch.int32), kp, vp)
+            assert torch.equal(kp.view(-1, d)[slot(s)], c.k[s])
+        c.k_pages, c.v_pages, c.tables = kp, vp, far
+        out, lse = c.call(out_dtype=F32)
+        c.check(out, lse)
+    k = torch.randn(3, hkv, d, device=DEV).to(BF)
+    slots = (n_pages * page - 1 - torch.arange(6, device=DEV)).to(torch.int32).view(3, hkv)
+    sg.norm_rope_store(None, k, k, _i32([0, 0, 0]), slots, kp, vp)
+    assert torch.equal(kp.view(-1, d)[slots.flatten().long()], k.view(-1, d))
+
+
+def test_two_calls_at_once():
+    """Calls on two streams with a workspace each, overlapping, against the same calls one after the other."""
+    _say("two at once")
+    cases = [Case([1, 1], [30000, 20000, 3000, 50], 14, 2, 128, 64, BF, seed=31),
+             Case([300, 77], [3000, 5000, 300, 77], 14, 2, 128, 16, BF, seed=32)]
+    want = [c.call() for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    ws = [sg.alloc_workspace(sg.paged_attention_workspace_size(c.q, c.hkv, 2, max_new=max(c.new)), DEV) for c in cases]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = [c.call(workspace=w, stream=s) for c, w, s in zip(cases, ws, streams)]
+        torch.cuda.synchronize()
+        for (o, l), (wo, wl) in zip(got, want):
+            assert torch.equal(o, wo) and torch.equal(l, wl)
+
+
+def test_two_captured_calls_share_a_workspace():
+    """Two captured graphs with one workspace, replayed in turn on one stream, with eager calls between."""
+    _say("two graphs, one workspace")
+    cases = [Case([1, 1], [9000, 20000, 3000, 50], 14, 2, 128, 64, BF, seed=41),
+             Case([130, 7], [3000, 500, 300, 77], 14, 2, 128, 16, BF, seed=42)]
+    want = [c.call() for c in cases]
+    ws = sg.alloc_workspace(max(sg.paged_attention_workspace_size(c.q, c.hkv, 2, max_new=max(c.new)) for c in cases),
+                            DEV)
+    graphs, outs = [], []
+    for c in cases:
+        g = torch.cuda.CUDAGraph()
+        out, lse = torch.zeros_like(c.q), torch.zeros(c.T, c.hq, device=DEV)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            c.call(workspace=ws, out=out, lse=lse)
+        graphs.append(g)
+        outs.append((out, lse))
+    for _ in range(4):
+        for g, c, (out, lse), (wo, wl) in zip(graphs, cases, outs, want):
+            out.zero_()
+            g.replay()
+            eager = c.call()
+            torch.cuda.synchronize()
+            assert torch.equal(out, wo) and torch.equal(lse, wl) and torch.equal(eager[0], wo)
+
+
+def test_shared_pages():
+    """Two sequences whose tables name the same pages (a common prompt) read the same rows."""
+    _say("shared pages")
+    c = Case([1, 3], [500, 90, 500, 90], 8, 2, 128, 16, BF, seed=51)
+    c.tables[2:] = c.tables[:2]
+    c.k[2:], c.v[2:] = c.k[:2], c.v[:2]
+    out, lse = c.call(out_dtype=F32)
+    c.check(out, lse)
+
+
+@pytest.mark.parametrize("hq,new", [(2, [3]), (4, [40])])
+def test_many_segments(hq, new):
+    """600 sequences: more tiles than workers, most of a token, one of many."""
+    _say(f"many segments {new}")
+    n = [1 if i % 7 else 0 for i in range(600)]
+    n[300] = new[0]
+    c = Case(n, [(i * 53) % 70 + n[i // 2] for i in range(1200)], hq, 2, 64, 16, BF, seed=61)
+    out, lse = c.call(out_dtype=F32)
+    c.check(out, lse)
