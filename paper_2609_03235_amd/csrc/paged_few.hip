@@ -286,7 +286,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
       }
       __syncthreads();
     }
-    const int64_t next = padded ? end : at.start + max(limit, 1);
+    const int64_t next = padded ? end : at.start + max(limit, 1) + (1 << a.min_shift);
     leave_shared(a, w, share, at, nkt);
     at.start = pos = next;
     ++at.tile;

@@ -307,7 +307,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
         }
       }
     }
-    const int64_t next = at.start + max(limit, 1);
+    const int64_t next = at.start + max(limit, 1) + (1 << a.min_shift);
     leave_shared(a, w, share, at, nkt);
     at.start = pos = next;
     ++at.tile;
