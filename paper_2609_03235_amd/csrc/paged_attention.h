@@ -188,11 +188,14 @@ __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, LineScratch& 
   at.seg = uniform(sc.seg);
   at.g = uniform(sc.g);
   const int64_t seg_start = uniform(sc.start);
-  int lo = 0, hi = at.g.tiles;  // the last tile that starts at or before `want`
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (seg_start + places_of(a, at.g, mid) <= want) lo = mid;
-    else hi = mid;
+  // The last tile that starts at or before `want`: every lane looks at one place in 64.
+  const int lane = tid & 63;
+  int lo = 0;
+  for (int n = at.g.tiles; n > 1;) {
+    const int step = (n + 63) >> 6, m = lo + lane * step;
+    const int upto = __popcll(__ballot(lane * step < n && seg_start + places_of(a, at.g, m) <= want));
+    lo += (upto - 1) * step;
+    n = min(step, n - (upto - 1) * step);
   }
   at.tile = uniform(lo);
   at.start = uniform(seg_start + places_of(a, at.g, lo));
@@ -201,11 +204,11 @@ __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, LineScratch& 
 
 // What a worker leaves for the merge (see PagedAttnArgs::shared) about a tile of nkt key tiles.
 __device__ __forceinline__ void leave_shared(const PagedAttnArgs& a, int w, int64_t share, const LineTile& at,
-                                             int nkt) {
+                                             int nkt, bool unshared) {
   const int64_t own = share * w;
   if (threadIdx.x != 0 || at.start < own) return;  // begun by a worker before
   const int64_t last_key = at.start + (int64_t)(nkt - 1) * a.key_tile;
-  const int last = last_key < own + share ? -1 : (int)(last_key / share);
+  const int last = unshared || last_key < own + share ? -1 : (int)(last_key / share);
   if (a.by_tile) a.shared[at.seg * a.max_tiles + at.tile] = make_int4(at.seg, at.tile, 2 * w + (at.start > own), last);
   else if (last >= 0) a.shared[w] = make_int4(at.seg, at.tile, 2 * w + (at.start > own), last);
 }
@@ -284,13 +287,14 @@ __device__ __forceinline__ u32x2 lds_transposed(const char* p) {
 // are not finite to zero in LDS, and notes the first such key of each column: as a row sees the keys up to some
 // key, it sees such a value exactly if it sees the first, and its output is then NaN. (The same in registers, where
 // the products are made, cost the tiles without masks up to a third of their time.)
-// ROWS rows from key0 on, whose 16-byte pieces lie where `swizzle` says; by every wave that uses them.
-template <int EB, int RB, int ROWS, typename F>
-__device__ __forceinline__ void clean_values(char* vals, int key0, int* first_odd, F swizzle) {
+// Rows [r0, r1) of those from key0 on, the ones that not all see, whose 16-byte pieces lie where `swizzle` says; by
+// every wave that uses them.
+template <int EB, int RB, typename F>
+__device__ __forceinline__ void clean_values(char* vals, int key0, int r0, int r1, int* first_odd, F swizzle) {
   constexpr int VPR = RB / 16;
   constexpr uint32_t kOdd = 0x7F800000u;  // the exponent of infinities and NaN; bf16 in each half
-#pragma unroll 1
-  for (int i = threadIdx.x & 63; i < ROWS * VPR; i += 64) {
+#pragma unroll 2
+  for (int i = r0 * VPR + (threadIdx.x & 63); i < r1 * VPR; i += 64) {
     const int r = i / VPR, col = ((i % VPR) ^ swizzle(r)) * (16 / EB);
     u32x4* at = reinterpret_cast<u32x4*>(vals + i * 16);
     u32x4 v = *at;

@@ -167,7 +167,8 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
           }
         if (j + 1 < j1) load(j + 1);
         char* vals = stage + (j & 1) * S::STAGE;
-        if (r0 + STEP > first_seen && r0 < limit) clean_values<EB, RB, STEP>(vals, r0, first_odd, S::swizzle);
+        if (r0 + STEP > first_seen && r0 < limit)
+          clean_values<EB, RB>(vals, r0, max(first_seen - r0, 0), min(limit - r0, STEP), first_odd, S::swizzle);
         float p[QB][U][4];
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
@@ -287,7 +288,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
       __syncthreads();
     }
     const int64_t next = padded ? end : at.start + max(limit, 1) + (1 << a.min_shift);
-    leave_shared(a, w, share, at, nkt);
+    leave_shared(a, w, share, at, nkt, false);
     at.start = pos = next;
     ++at.tile;
   }

@@ -31,6 +31,13 @@ struct ManyShape {
   }
 };
 
+// A query tile of at most so many keys is one worker's alone where that is at most twice a worker's share: a part
+// of a tile costs 64 KB of partial results, as much time as about 400 keys, written and read again (8 sequences of
+// 512 tokens with 28 / 4 heads 65 us shared, 59 so; 3 of 128 over 600 rows, whose tiles the second half leaves
+// shared, 32 and 36).
+template <typename T>
+constexpr int kUnshared = sizeof(T) == 2 ? 512 : 128;
+
 // Reference kept while a tile's sum of exponentials stays below this.
 constexpr float kFar = 1024.f;
 
@@ -104,8 +111,10 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
     const PagedSeg& g = at.g;
     const int limit = uniform(tile_rows(a, g, at.tile));
     const int nkt = max((limit + KT - 1) / KT, 1);
-    const int j0 = (int)((pos - at.start + KT - 1) / KT);
-    const int j1 = (int)min((int64_t)nkt, (end - at.start + KT - 1) / KT);
+    // A tile of few keys is not shared: the worker that it starts with does all of it.
+    const bool own = limit <= kUnshared<T> && limit + (1 << a.min_shift) <= 2 * share;
+    const int j0 = own ? (at.start < share * w ? nkt : 0) : (int)((pos - at.start + KT - 1) / KT);
+    const int j1 = own ? nkt : (int)min((int64_t)nkt, (end - at.start + KT - 1) / KT);
     if (j0 < j1) {
       const int h = at.seg % a.Hkv;
       const int tok0 = at.tile * a.tokens, ntok = min(a.tokens, g.n - tok0);
@@ -113,6 +122,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
       const int r = wid * 32 + lq, tok = r / a.G, hd = r - tok * a.G;
       const bool on = r < nrow;
       const int seen = on ? seen_by(a, g, tok0 + tok) : 0;
+      const int first_seen = seen_by(a, g, tok0);
       // the rows of this wave see at most hi keys
       const int hi = wid * 32 < nrow ? uniform(seen_by(a, g, tok0 + (min(nrow, wid * 32 + 32) - 1) / a.G)) : 0;
 
@@ -211,7 +221,8 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
           exps(m == -INFINITY ? 0.f : m);  // nothing seen so far: all are 0
         }
         s += sum;
-        if constexpr (EDGE) clean_values<EB, RB, KT>(vb, key0, first_odd, S::value_swizzle);
+        if constexpr (EDGE) clean_values<EB, RB>(vb, key0, max(first_seen - key0, 0), min(limit - key0, KT), first_odd,
+                                               S::value_swizzle);
         __builtin_amdgcn_s_setprio(1);
         if constexpr (EB == 2) {
           const int l16 = lane & 15;
@@ -273,7 +284,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
           __syncthreads();
         }
       };
-      tiles(min(j1, seen_by(a, g, tok0) / KT), std::false_type{});
+      tiles(min(j1, first_seen / KT), std::false_type{});
       tiles(j1, std::true_type{});
       s += __shfl_xor(s, 32, 64);
       auto result = [&](int d, int i) {
@@ -308,7 +319,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
       }
     }
     const int64_t next = at.start + max(limit, 1) + (1 << a.min_shift);
-    leave_shared(a, w, share, at, nkt);
+    leave_shared(a, w, share, at, nkt, own);
     at.start = pos = next;
     ++at.tile;
   }
