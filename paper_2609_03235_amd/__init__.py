@@ -377,36 +377,29 @@ class PagedDesc(ctypes.Structure):
 PAGES_OK, PAGES_SHORT, PAGES_ROWS, PAGES_STACK, PAGES_SLOTS = range(5)
 
 
-class _on_stream:
-    """Makes GPU `index` current and `stream` (None: that GPU's current stream) torch's current stream, so that
-    what a call allocates belongs to the stream it is used on. Enters as the raw handle. Where both are current
-    already, the usual call, nothing is switched (a serving step makes several calls of a few us each)."""
-    __slots__ = ("guards", "index")
+def _raw_stream(index):
+    """The raw handle of GPU `index`'s current stream where that GPU is current, else None. The handle alone:
+    building a torch.cuda.Stream for it takes 2.8 us, a third of a small call."""
+    import torch
+    if torch.cuda.current_device() != index:
+        return None
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return torch.cuda.current_stream().cuda_stream if raw is None else raw(index)
 
-    def __init__(self, index, stream):
-        import torch
-        self.guards, self.index = (), index
-        if stream is not None or torch.cuda.current_device() != index:
-            guards = [torch.cuda.device(index)]
-            if stream is not None:
-                if not hasattr(stream, "cuda_stream"):
-                    stream = torch.cuda.ExternalStream(int(stream), device=torch.device("cuda", index))
-                if stream.device.index != index:
-                    _refuse(f"the stream is on {stream.device}, the tensors on cuda:{index}")
-                guards.append(torch.cuda.stream(stream))
-            self.guards = guards
 
-    def __enter__(self):
-        import torch
-        for g in self.guards:
-            g.__enter__()
-        # the handle alone: building a torch.cuda.Stream for it takes 2.8 us, a third of a small call
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        return torch.cuda.current_stream().cuda_stream if raw is None else raw(self.index)
-
-    def __exit__(self, *exc):
-        for g in reversed(self.guards):
-            g.__exit__(*exc)
+def _switched(fn, index, stream, args, kw):
+    """fn(*args, **kw) with GPU `index` current and `stream` (None: that GPU's current one) torch's current stream, so
+    that what the call allocates belongs to the stream it is used on."""
+    import torch
+    with torch.cuda.device(index):
+        if stream is None:
+            return fn(*args, **kw)
+        if not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream), device=torch.device("cuda", index))
+        if stream.device.index != index:
+            _refuse(f"the stream is on {stream.device}, the tensors on cuda:{index}")
+        with torch.cuda.stream(stream):
+            return fn(*args, **kw)
 
 
 def _refuse(message: str):
@@ -474,23 +467,28 @@ def page_update(rows, add, tables, free_pages, head, *, page_size: int, n_slots:
                           (slots, "slots", shape)):
         if t is not None:
             _check_int32(t, name, want)
-    with _on_stream(index, stream) as s:
-        if slots is None or rows_out is None or cu is None or head_out is None or status is None:
-            # each at a multiple of 16 bytes
-            n = n_slots if by_segment else n_slots * Hkv
-            sizes = (n, -n % 4, S, -S % 4, n_add + 1, (3 - n_add) % 4, 1, 3, 1)
-            parts = torch.empty(sum(sizes), dtype=torch.int32, device=rows.device).split_with_sizes(sizes)
-            if slots is None:
-                slots = parts[0] if by_segment else parts[0].view(shape)
-            rows_out = parts[2] if rows_out is None else rows_out
-            cu = parts[4] if cu is None else cu
-            head_out = parts[6] if head_out is None else head_out
-            status = parts[8] if status is None else status
-        desc = PageDesc(B, Hkv, page_size, tables.shape[1], 1 if by_segment else 0, 0, free_pages.shape[0], n_slots)
-        _check(load_library().sgdkv_page_update(
-            ctypes.byref(desc), rows.data_ptr(), add.data_ptr(), tables.data_ptr(), free_pages.data_ptr(),
-            head.data_ptr(), rows_out.data_ptr(), head_out.data_ptr(), cu.data_ptr(), slots.data_ptr(),
-            status.data_ptr(), s))
+    handle = _raw_stream(index) if stream is None else None
+    if handle is None:
+        return _switched(page_update, index, stream, (rows, add, tables, free_pages, head),
+                         dict(page_size=page_size, n_slots=n_slots, by_segment=by_segment, rows_out=rows_out,
+                              head_out=head_out, slots=slots, cu=cu, status=status))
+    if slots is None or rows_out is None or cu is None or head_out is None or status is None:
+        # each at a multiple of 16 bytes
+        n = n_slots if by_segment else n_slots * Hkv
+        sizes = (n, -n % 4, S, -S % 4, n_add + 1, (3 - n_add) % 4, 1, 3, 1)
+        parts = torch.empty(sum(sizes), dtype=torch.int32, device=rows.device).split_with_sizes(sizes)
+        if slots is None:
+            slots = parts[0] if by_segment else parts[0].view(shape)
+        rows_out = parts[2] if rows_out is None else rows_out
+        cu = parts[4] if cu is None else cu
+        head_out = parts[6] if head_out is None else head_out
+        status = parts[8] if status is None else status
+    desc = PageDesc(B, Hkv, page_size, tables.shape[1], 1 if by_segment else 0, 0, free_pages.shape[0], n_slots)
+    st = load_library().sgdkv_page_update(
+        ctypes.byref(desc), rows.data_ptr(), add.data_ptr(), tables.data_ptr(), free_pages.data_ptr(), head.data_ptr(),
+        rows_out.data_ptr(), head_out.data_ptr(), cu.data_ptr(), slots.data_ptr(), status.data_ptr(), handle)
+    if st:
+        _check(st)
     return dict(slots=slots, rows=rows_out, head=head_out, cu=cu, status=status, tables=tables, free_pages=free_pages)
 
 
@@ -504,9 +502,13 @@ def paged_store(k_rows, v_rows, slots, k_pages, v_pages, *, stream=None):
     _check_dense(k_rows, "k_rows", shape, k_pages.dtype)
     _check_dense(v_rows, "v_rows", shape, k_pages.dtype)
     _check_int32(slots, "slots", shape[:1])
-    with _on_stream(index, stream) as s:
-        _check(load_library().sgdkv_paged_store(ctypes.byref(pool), k_rows.data_ptr(), v_rows.data_ptr(),
-                                                slots.data_ptr(), shape[0], s))
+    handle = _raw_stream(index) if stream is None else None
+    if handle is None:
+        return _switched(paged_store, index, stream, (k_rows, v_rows, slots, k_pages, v_pages), {})
+    st = load_library().sgdkv_paged_store(ctypes.byref(pool), k_rows.data_ptr(), v_rows.data_ptr(), slots.data_ptr(),
+                                          shape[0], handle)
+    if st:
+        _check(st)
 
 
 def _token_stride(t, name, d):
@@ -548,14 +550,20 @@ def norm_rope_store(q, k, v, positions, slots, k_pages, v_pages, *, inv_freq=Non
     _check_int32(slots, "slots", (T, Hkv))
     desc = NormRopeDesc(T, Hq, Hkv, q_stride, _token_stride(k, "k", d), _token_stride(v, "v", d),
                         0 if inv_freq is None else 2 * inv_freq.shape[0], 1 if interleaved else 0, eps, 0)
-    with _on_stream(index, stream) as s:
-        if Hq and q_out is None:
-            q_out = torch.empty((T, Hq, d), dtype=dt, device=q.device)
-        _check(load_library().sgdkv_norm_rope_store(
-            ctypes.byref(pool), ctypes.byref(desc), q.data_ptr() if Hq else None, k.data_ptr(), v.data_ptr(),
-            positions.data_ptr(), slots.data_ptr(), None if inv_freq is None else inv_freq.data_ptr(),
-            None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
-            q_out.data_ptr() if Hq else None, s))
+    handle = _raw_stream(index) if stream is None else None
+    if handle is None:
+        return _switched(norm_rope_store, index, stream, (q, k, v, positions, slots, k_pages, v_pages),
+                         dict(inv_freq=inv_freq, q_weight=q_weight, k_weight=k_weight, eps=eps,
+                              interleaved=interleaved, q_out=q_out))
+    if Hq and q_out is None:
+        q_out = torch.empty((T, Hq, d), dtype=dt, device=q.device)
+    st = load_library().sgdkv_norm_rope_store(
+        ctypes.byref(pool), ctypes.byref(desc), q.data_ptr() if Hq else None, k.data_ptr(), v.data_ptr(),
+        positions.data_ptr(), slots.data_ptr(), None if inv_freq is None else inv_freq.data_ptr(),
+        None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+        q_out.data_ptr() if Hq else None, handle)
+    if st:
+        _check(st)
     return q_out
 
 
@@ -604,17 +612,23 @@ def paged_attention(q, k_pages, v_pages, tables, rows, cu_new, num_kv_heads: int
         _refuse("workspace must be contiguous")
     if with_lse and lse is not None:
         _check_dense(lse, "lse", shape[:2], torch.float32)
-    with _on_stream(index, stream) as s:
-        if out is None:
-            out = torch.empty(shape, dtype=od, device=q.device)
-        if with_lse and lse is None:
-            lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device)
-        if workspace is None:
-            workspace = alloc_workspace(paged_attention_workspace_size(q, num_kv_heads, B, max_new=max_new), q.device)
-        _check(load_library().sgdkv_paged_attention(
-            ctypes.byref(pool), ctypes.byref(desc), q.data_ptr(), tables.data_ptr(), rows.data_ptr(),
-            cu_new.data_ptr(), out.data_ptr(), lse.data_ptr() if with_lse else None, workspace.data_ptr(),
-            workspace.numel() * workspace.element_size(), s))
+    handle = _raw_stream(index) if stream is None else None
+    if handle is None:
+        return _switched(paged_attention, index, stream, (q, k_pages, v_pages, tables, rows, cu_new, num_kv_heads),
+                         dict(max_new=max_new, causal=causal, scale=scale, out_dtype=out_dtype, with_lse=with_lse,
+                              out=out, lse=lse, workspace=workspace))
+    if out is None:
+        out = torch.empty(shape, dtype=od, device=q.device)
+    if with_lse and lse is None:
+        lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device)
+    if workspace is None:
+        workspace = alloc_workspace(paged_attention_workspace_size(q, num_kv_heads, B, max_new=max_new), q.device)
+    st = load_library().sgdkv_paged_attention(
+        ctypes.byref(pool), ctypes.byref(desc), q.data_ptr(), tables.data_ptr(), rows.data_ptr(), cu_new.data_ptr(),
+        out.data_ptr(), lse.data_ptr() if with_lse else None, workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), handle)
+    if st:
+        _check(st)
     return out, (lse if with_lse else None)
 
 
