@@ -12,6 +12,7 @@
 // All three are bound by latency or by HBM. The pools may pass 4 GiB, so their rows are addressed with
 // 64-bit pointers; every slot is compared with the pool's size first.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.h"
 #include "paged_internal.h"
@@ -74,8 +75,9 @@ __device__ __forceinline__ int piece_of(const int32_t* p, int n, int i) {
 
 // Every workgroup reads the segments' lengths and computes the same prefix sums into LDS (they are few
 // beside the slots), then does its share of the table entries and slots: one launch, no scan before it. Bound
-// by latency: about four dependent memory reads and the scan; 512 segments and slots take 7 us, 524288 slots 11
-// (one workgroup with the lengths read again at every use took 22 and more).
+// by latency: about four dependent memory reads and the scan; one more token for 512 segments takes 6 us, the 2.1 M
+// slots of 64 segments 13 (the first with one workgroup and the lengths read again at every use 24, with the first
+// workgroup's threads at four slots each 10).
 // Nothing that one workgroup writes is read by another: table entries past a segment's old pages are written
 // and those within them read; the stack is written below its head (the pages given back, looked up in their
 // tables by those who take them in the same call) and read from its head on. rows_out and head_out may be the
@@ -145,54 +147,99 @@ __global__ __launch_bounds__(kPageBlock) void page_update_kernel(PageArgs a, int
     for (int i = tid; i <= pieces; i += kPageBlock) a.cu_out[i] = status ? 0 : cu[i];
     if (tid == 0) a.status[0] = status;
   }
-  // the page at stack index i: given back in this call below the old head, else the stack's
-  auto page_at = [&](int64_t i) -> int32_t {
-    if (i >= head) return a.free_pages[i];
+  // where the page at stack index i is found: given back in this call below the old head, else on the stack
+  auto page_at = [&](int64_t i) -> const int32_t* {
+    if (i >= head) return a.free_pages + i;
     const int at = (int)(i - base), g = piece_of(given, a.S, at);
     const int left = pages_of(a, rows[g]) - (given[g + 1] - given[g]);  // its pages afterwards
-    return a.tables[(int64_t)g * a.max_pages + left + (at - given[g])];
+    return a.tables + (int64_t)g * a.max_pages + left + (at - given[g]);
   };
   if (status == 0) {
-    for (int64_t i = first; i < all.taken; i += stride) {
+    // from the last workgroup on: the first ones have the slots
+    const int64_t from = (int64_t)(gridDim.x - 1 - blockIdx.x) * kPageBlock + tid;
+    for (int64_t i = from; i < all.taken; i += stride) {
       const int s = piece_of(taken, a.S, (int)i);
-      a.tables[(int64_t)s * a.max_pages + pages_of(a, rows[s]) + ((int)i - taken[s])] = page_at(base + i);
+      a.tables[(int64_t)s * a.max_pages + pages_of(a, rows[s]) + ((int)i - taken[s])] = *page_at(base + i);
     }
-    for (int64_t i = first; i < all.given; i += stride) a.free_pages[base + i] = page_at(base + i);
+    for (int64_t i = from; i < all.given; i += stride) a.free_pages[base + i] = *page_at(base + i);
   }
-  // slots: a thread takes four consecutive ones
+  // slots: a thread takes one, or four consecutive ones where there are more than threads
   const uint32_t per_row = a.by_segment ? 1 : a.Hkv;
   const int64_t n = a.num_slots * per_row;
   const int in_page = (1 << a.page_shift) - 1;
-  for (int64_t at = first * 4; at < n; at += stride * 4) {
-    int32_t out[4] = {-1, -1, -1, -1};
-    uint32_t item = (uint32_t)at / per_row, h = (uint32_t)at - item * per_row;
-    int piece = -1, seg = -1, entry = -1, page = 0;  // neighbours mostly share these
+  auto slots = [&](auto count, auto by_segment) {
+    constexpr int N = decltype(count)::value;
+    constexpr bool BY_SEGMENT = decltype(by_segment)::value;
+    for (int64_t at = first * N; at < n; at += stride * N) {
+      if (BY_SEGMENT && N == 4 && status == 0 && at + 4 <= all.fresh) {
+        const int s = piece_of(cu, pieces, (int)at);
+        if (at + 4 <= cu[s + 1]) {  // mostly: four rows of one segment, in one page or two
+          const int p0 = rows[s] + ((int)at - cu[s]), had = pages_of(a, rows[s]);
+          const int j0 = p0 >> a.page_shift, j3 = (p0 + 3) >> a.page_shift;
+          const int32_t* table = a.tables + (int64_t)s * a.max_pages;
+          const int64_t base_s = base + taken[s] - had;
+          const int32_t* first_page = j0 < had ? table + j0 : page_at(base_s + j0);
+          const int32_t* last_page = j3 == j0 ? first_page : j3 < had ? table + j3 : page_at(base_s + j3);
+          const int64_t pages[2] = {*first_page, *last_page};
+          int slot[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (status == 0 && item < (uint32_t)all.fresh) {
-        if (piece < 0 || (int)item >= cu[piece + 1]) piece = piece_of(cu, pieces, (int)item);
-        const int s = a.by_segment ? piece : piece * a.Hkv + (int)h;
-        const int pos = rows[s] + ((int)item - cu[piece]), j = pos >> a.page_shift;
-        if (s != seg || j != entry) {
-          const int had = pages_of(a, rows[s]);
-          page = j < had ? a.tables[(int64_t)s * a.max_pages + j] : page_at(base + taken[s] + (j - had));
-          seg = s;
-          entry = j;
+          for (int e = 0; e < 4; ++e) {
+            const int p = p0 + e;
+            const int64_t x = ((p >> a.page_shift == j0 ? pages[0] : pages[1]) << a.page_shift) + (p & in_page);
+            slot[e] = x < 0 || x > 0x7FFFFFFF ? -1 : (int)x;
+          }
+          *reinterpret_cast<int4*>(a.slots + at) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+          continue;
         }
-        const int64_t slot = ((int64_t)page << a.page_shift) + (pos & in_page);
-        out[e] = slot < 0 || slot > 0x7FFFFFFF ? -1 : (int32_t)slot;
       }
-      if (++h == per_row) {
-        h = 0;
-        ++item;
+      // all places are worked out before the first page is read
+      const int32_t* page[N];
+      int pos[N];
+      uint32_t item = (uint32_t)at / per_row, h = (uint32_t)at - item * per_row;
+      int piece = -1, seg = -1, entry = -1;  // neighbours mostly share these
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        page[e] = nullptr;
+        pos[e] = 0;
+        if (status == 0 && item < (uint32_t)all.fresh) {
+          if (piece < 0 || (int)item >= cu[piece + 1]) piece = piece_of(cu, pieces, (int)item);
+          const int s = BY_SEGMENT ? piece : piece * a.Hkv + (int)h;
+          pos[e] = rows[s] + ((int)item - cu[piece]);
+          const int j = pos[e] >> a.page_shift;
+          if (e > 0 && s == seg && j == entry) {
+            page[e] = page[e - 1];
+          } else {
+            const int had = pages_of(a, rows[s]);
+            page[e] = j < had ? a.tables + (int64_t)s * a.max_pages + j : page_at(base + taken[s] + (j - had));
+            seg = s;
+            entry = j;
+          }
+        }
+        if (++h == per_row) {
+          h = 0;
+          ++item;
+        }
+      }
+      int64_t out[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) out[e] = page[e] ? *page[e] : -1;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const int64_t slot = (out[e] << a.page_shift) + (pos[e] & in_page);
+        out[e] = slot < 0 || slot > 0x7FFFFFFF ? -1 : slot;
+      }
+      if (N == 4 && at + 4 <= n) {
+        *reinterpret_cast<int4*>(a.slots + at) =
+            make_int4((int)out[0], (int)out[N / 4], (int)out[N / 2], (int)out[N - 1]);
+      } else {
+        for (int e = 0; e < N && at + e < n; ++e) a.slots[at + e] = (int32_t)out[e];
       }
     }
-    if (at + 4 <= n) {
-      *reinterpret_cast<int4*>(a.slots + at) = make_int4(out[0], out[1], out[2], out[3]);
-    } else {
-      for (int e = 0; e < 4 && at + e < n; ++e) a.slots[at + e] = out[e];
-    }
-  }
+  };
+  using One = std::integral_constant<int, 1>;
+  using Four = std::integral_constant<int, 4>;
+  if (a.by_segment) n <= stride ? slots(One{}, std::true_type{}) : slots(Four{}, std::true_type{});
+  else n <= stride ? slots(One{}, std::false_type{}) : slots(Four{}, std::false_type{});
 }
 
 // ------------------------------------------------------------------ rows to their slots
