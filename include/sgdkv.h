@@ -394,7 +394,7 @@ typedef struct sgdkv_page_desc {
   int32_t batch;         /* B >= 1 sequences */
   int32_t num_kv_heads;  /* Hkv >= 1; B*Hkv <= 4096 */
   int32_t page_size;     /* P: a power of two, 16 to 1024 */
-  int32_t max_pages;     /* columns of tables, >= 1; max_pages * P <= 2^31 - 1 */
+  int32_t max_pages;     /* columns of tables, >= 1; max_pages * P <= 2^31 - 2049 */
   int32_t by_segment;    /* 0: add and slots per sequence and token; 1: per segment */
   int32_t reserved;      /* must be 0 */
   int64_t num_free;      /* entries of free_pages, 1 to 2^31 - 1 */
@@ -480,7 +480,7 @@ typedef struct sgdkv_paged_desc {
   int32_t out_dtype;     /* dtype of out */
   int64_t num_tokens;    /* T >= 0: tokens of q, out and lse_out; T*Hq <= 2^31 - 129 */
   int32_t max_new;       /* >= 1: at least the longest sequence's new tokens */
-  int32_t max_pages;     /* columns of tables, >= 1 */
+  int32_t max_pages;     /* columns of tables, >= 1; max_pages * page_size <= 2^31 - 2049 */
   int32_t causal;        /* 1: a token sees the rows up to its own; 0: all of its segment's */
   float scale;           /* logit scale; 0 selects 1/sqrt(head_dim) */
 } sgdkv_paged_desc;
@@ -512,8 +512,7 @@ sgdkv_status sgdkv_paged_attention_workspace_size(const sgdkv_page_pool* pool, c
  * column, of the tokens that see its row, not finite, and no others.
  * Errors (nothing enqueued): a bad pool; sizes out of range; Hq % Hkv; more
  * than 16 query heads per KV head, 8192 query heads or 65535 segments
- * (UNSUPPORTED); max_pages * page_size beyond 2^31 - 1; missing or misaligned
- * pointers; small workspace (WORKSPACE). */
+ * (UNSUPPORTED); missing or misaligned pointers; small workspace (WORKSPACE). */
 sgdkv_status sgdkv_paged_attention(const sgdkv_page_pool* pool, const sgdkv_paged_desc* desc, const void* q,
                                    const int32_t* tables, const int32_t* rows, const int32_t* cu_new, void* out,
                                    float* lse_out, void* workspace, size_t workspace_bytes, void* stream);

@@ -389,7 +389,8 @@ def _raw_stream(index):
 
 def _switched(fn, index, stream, args, kw):
     """fn(*args, **kw) with GPU `index` current and `stream` (None: that GPU's current one) torch's current stream, so
-    that what the call allocates belongs to the stream it is used on."""
+    that what the call allocates belongs to the stream it is used on; the tensors it is given are marked as in use
+    there, so that the allocator does not hand their memory to other work before the call is done."""
     import torch
     with torch.cuda.device(index):
         if stream is None:
@@ -399,7 +400,11 @@ def _switched(fn, index, stream, args, kw):
         if stream.device.index != index:
             _refuse(f"the stream is on {stream.device}, the tensors on cuda:{index}")
         with torch.cuda.stream(stream):
-            return fn(*args, **kw)
+            result = fn(*args, **kw)
+        for t in (*args, *kw.values()):
+            if isinstance(t, torch.Tensor):
+                t.record_stream(stream)
+        return result
 
 
 def _refuse(message: str):

@@ -17,6 +17,8 @@ using sgdkv::host_check_device;
 using sgdkv::host_ok;
 
 constexpr int64_t kMaxInt = 0x7FFFFFFF;
+// Rows of a segment: the kernels' row numbers may run a few tiles past the last one.
+constexpr int64_t kMaxRows = kMaxInt - 2048;
 
 sgdkv_status fail(sgdkv_status code, const char* fmt, ...) {
   char buf[512];
@@ -151,8 +153,8 @@ sgdkv_status sgdkv_page_update(const sgdkv_page_desc* desc, const int32_t* rows,
   if (nseg > sgdkv::kMaxPageSegs)
     return fail(SGDKV_ERR_UNSUPPORTED, "batch * num_kv_heads = %lld > %d", (long long)nseg, sgdkv::kMaxPageSegs);
   if (sgdkv_status st = check_page_size(desc->page_size)) return st;
-  if (desc->max_pages < 1 || desc->max_pages > kMaxInt / desc->page_size)
-    return fail(SGDKV_ERR_INVALID_ARG, "max_pages %d outside [1, (2^31 - 1) / page_size]", desc->max_pages);
+  if (desc->max_pages < 1 || desc->max_pages > kMaxRows / desc->page_size)
+    return fail(SGDKV_ERR_INVALID_ARG, "max_pages %d outside [1, (2^31 - 2049) / page_size]", desc->max_pages);
   if (nseg * desc->max_pages > kMaxInt)
     return fail(SGDKV_ERR_UNSUPPORTED, "%lld segments of %d table columns", (long long)nseg, desc->max_pages);
   if (desc->by_segment != 0 && desc->by_segment != 1)
@@ -313,8 +315,8 @@ sgdkv_status sgdkv_paged_attention(const sgdkv_page_pool* pool, const sgdkv_page
   size_t bytes = 0;
   if (sgdkv_status st = plan_paged(pool, desc, a, bytes)) return st;
   if (sgdkv_status st = check_pool(pool)) return st;
-  if (desc->max_pages < 1 || desc->max_pages > kMaxInt / pool->page_size)
-    return fail(SGDKV_ERR_INVALID_ARG, "max_pages %d outside [1, (2^31 - 1) / page_size]", desc->max_pages);
+  if (desc->max_pages < 1 || desc->max_pages > kMaxRows / pool->page_size)
+    return fail(SGDKV_ERR_INVALID_ARG, "max_pages %d outside [1, (2^31 - 2049) / page_size]", desc->max_pages);
   if (a.T > 0)
     if (sgdkv_status st =
             check_ptrs({{q, "q"}, {tables, "tables"}, {rows, "rows"}, {cu_new, "cu_new"}, {out, "out"}}))

@@ -4,7 +4,11 @@
 // all four waves share through LDS: two buffers, one barrier per tile, and the next tile on its way from memory
 // straight into LDS while one is computed (no registers, no LDS writes). Products are 32x32 MFMAs. Every row
 // keeps a reference for its exponentials that only moves when a tile's sum shows that it fell too far behind,
-// so a logit costs one fma, one exp2 and one add.
+// so a logit costs one fma, one exp2 and one add. 32 query rows a wave and two workgroups a compute unit are what the
+// registers (o takes 64, the queries 32, a tile's logits 32) and LDS (64 KB each) hold; the second workgroup runs
+// while the first waits. Bound by the matrix unit and the vector unit one after the other, at the socket's power:
+// two sequences of 8192 tokens over 16K rows, 64 / 8 heads of 128, bf16: 10.5 ms, 0.99 PFLOP/s, at 1.7 to 1.8 GHz
+// (8.5 ms on zeros).
 #include <type_traits>
 
 #include "paged_attention.h"
@@ -156,8 +160,8 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
       // One tile of keys, from key0 on, out of LDS. EDGE: some row does not see all of it; `left` is how many of the
       // keys from 4 * half on this lane's row sees.
       auto attend = [&](char* kb, auto edge, int key0) {
-        const int left = seen - key0 - 4 * half;
         constexpr bool EDGE = decltype(edge)::value;
+        const int left = seen - key0 - 4 * half;
         char* vb = kb + S::TILE;
         // products first where waves compete: the other waves' exponentials fill in
         __builtin_amdgcn_s_setprio(1);
@@ -202,7 +206,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
           sum = (part[0] + part[1]) + (part[2] + part[3]);
         };
         exps(m);
-        // Without a lane of its own accord in the branch: the compiler then keeps o in place.
+        // All lanes take this branch or none, and none branches in it: so the compiler keeps o in place.
         if (__any(!(sum <= kFar) || m == -INFINITY)) {
           float mx = -INFINITY;
 #pragma unroll
@@ -258,9 +262,8 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
 #pragma unroll
             for (int i = 0; i < 16; ++i)
 #pragma unroll
-              for (int d = 0; d < ND; ++d) {
+              for (int d = 0; d < ND; ++d)
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(n, i, d), p.v[n][i], o[d], 0, 0, 0);
-              }
         }
         __builtin_amdgcn_s_setprio(0);
       };
@@ -300,8 +303,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
           for (int d = 0; d < ND; ++d)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              store_out4(a, row, D, 32 * d + 8 * i + 4 * half,
-                         result(d, i) * inv);
+              store_out4(a, row, D, 32 * d + 8 * i + 4 * half, result(d, i) * inv);
           if (a.lse && half == 0) a.lse[row] = lse_of(m, s);
         } else {
           const int64_t slot = 2 * (int64_t)w + (at.start > share * w ? 1 : 0);
@@ -309,8 +311,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
           for (int d = 0; d < ND; ++d)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              *reinterpret_cast<f32x4*>(a.part + (slot * M + r) * D + 32 * d + 8 * i + 4 * half) =
-                  result(d, i);
+              *reinterpret_cast<f32x4*>(a.part + (slot * M + r) * D + 32 * d + 8 * i + 4 * half) = result(d, i);
           if (half == 0) {
             a.part_ms[(slot * M + r) * 2] = m;
             a.part_ms[(slot * M + r) * 2 + 1] = s;

@@ -761,3 +761,41 @@ def test_many_segments(hq, new):
     c = Case(n, [(i * 53) % 70 + n[i // 2] for i in range(1200)], hq, 2, 64, 16, BF, seed=61)
     out, lse = c.call(out_dtype=F32)
     c.check(out, lse)
+
+
+def test_a_step_without_pages_does_nothing():
+    """Too few pages: the step's calls that follow store nothing, attend to nothing and change no length."""
+    _say("no pages")
+    B, hq, hkv, d, page = 2, 4, 2, 64, 16
+    st = _serve_state(B, hkv, page, 8, 3, d, F32)
+    up = sg.page_update(st["rows"], _i32([1, 1]), st["tables"], st["free"], st["head"], page_size=page, n_slots=B,
+                        rows_out=st["rows"], head_out=st["head"])
+    assert int(up["status"]) == sg.PAGES_SHORT and (up["slots"] == -1).all() and not up["cu"].any()
+    x = torch.randn(B, hkv, d, device=DEV)
+    q = sg.norm_rope_store(torch.randn(B, hq, d, device=DEV), x, x, _i32([0, 0]), up["slots"], st["k"], st["v"])
+    assert st["k"].isnan().all() and st["v"].isnan().all()
+    out = torch.full_like(q, 5.0)
+    sg.paged_attention(q, st["k"], st["v"], st["tables"], st["rows"], up["cu"], hkv, max_new=1, out=out)
+    assert (out == 5.0).all() and not st["rows"].any() and int(st["head"]) == 0
+
+
+@pytest.mark.parametrize("new", [[1], [20]])
+def test_table_of_repeated_pages_past_2_to_25_rows(new):
+    """A segment of 40 million rows whose table names the same 64 pages over and over: its softmax is that of the
+    pages' rows, each many times, so out is that of one round of them and lse larger by the log of the rounds.
+    Equal parts of the sums round together: the tolerances are those of one round with this many rows."""
+    _say(f"long table {new}")
+    d, page, P, rounds = 64, 1024, 64, 620
+    g = torch.Generator(device=DEV).manual_seed(0)
+    kp, vp = (torch.randn(P, page, d, generator=g, device=DEV).to(BF) for _ in range(2))
+    tables = torch.arange(P, dtype=torch.int32, device=DEV).repeat(rounds)[None].contiguous()
+    q = torch.randn(sum(new), 4, d, generator=g, device=DEV).to(BF)
+    rows = _i32([P * page * rounds])
+    out, lse = sg.paged_attention(q, kp, vp, tables, rows, _i32([0, len(q)]), 1, max_new=max(new), causal=False,
+                                  out_dtype=F32)
+    y = q.double().flatten(0, 1) @ kp.view(-1, d).double().T / 8
+    want = torch.softmax(y, 1) @ vp.view(-1, d).double()
+    wlse = torch.logsumexp(y, 1) + math.log(rounds)
+    # a worker adds 79000 rows, 4 at a time per lane group and 16 per product: 2500 roundings at most meet in a sum
+    assert (out.double().flatten(0, 1) - want).abs().max() < 2500 * 2.0 ** -24 * 1.0 + 2e-5
+    assert (lse.double().flatten() - wlse).abs().max() < 2500 * 2.0 ** -24 + 2e-5
