@@ -297,13 +297,14 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
 
 // Joins the parts of the query tiles that several workers shared: workgroup (x, y) looks at entry x of `shared`.
 // Lanes in groups of D / 4 hold a row, four columns each.
-//   MANY = false: tiles of few rows and up to hundreds of parts. A workgroup takes one row; the groups take its
+//   Few parts: a group takes a row of its own and its parts in batches, each all under way at once.
+//   Many (a long segment and few others): a workgroup takes rows y, y + gridDim.y, ...; its groups take a row's
 //     parts in turn with a running maximum and are then joined in order.
-//   MANY = true: tiles of many rows and seldom more than three parts. A group takes a row of its own (the rows
-//     one after the other with the groups on the parts took 17 us for what takes 5 so).
-template <int D, bool MANY>
+// Whichever has fewer rounds of reads. (21 tokens over 57K rows of one head, 443 parts: 142 us and 39. 300 tokens
+// over 900 rows of four heads, 8 or 9 parts and two rows a workgroup: 32 us and 34.)
+template <int D>
 __global__ __launch_bounds__(kAttnBlock) void paged_merge_kernel(PagedAttnArgs a) {
-  constexpr int LPS = D / 4, NG = kAttnBlock / LPS;
+  constexpr int LPS = D / 4, NG = kAttnBlock / LPS, kBatch = 8;
   __shared__ float ms[NG], ss[NG];
   __shared__ __attribute__((aligned(16))) float os[NG][D];
   const int tid = threadIdx.x, grp = tid / LPS, col = 4 * (tid % LPS);
@@ -317,46 +318,65 @@ __global__ __launch_bounds__(kAttnBlock) void paged_merge_kernel(PagedAttnArgs a
   const int w = left.z >> 1;
   const int M = a.tile_rows, h = seg % a.Hkv, tok0 = left.y * a.tokens;
   const int nrow = min(a.tokens, g.n - tok0) * a.G, parts = left.w - w + 1;
-  const int r = MANY ? blockIdx.y * NG + grp : blockIdx.y;
-  if (r >= nrow) return;
-  float m = -INFINITY, s = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  // kBatch parts' loads are under way together; a part past the last repeats it with weight zero
-  constexpr int kBatch = 8, STRIDE = MANY ? 1 : NG;
-  for (int i0 = MANY ? 0 : grp; i0 < parts; i0 += kBatch * STRIDE) {
-    float pm[kBatch], ps[kBatch];
-    f32x4 po[kBatch];
+
+  float m, s;
+  f32x4 o;
+  // parts first, first + stride, ... of row r; a part past the last repeats it with weight zero
+  auto join = [&](int r, int first, int stride) {
+    m = -INFINITY;
+    s = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i0 = first; i0 < parts; i0 += kBatch * stride) {
+      float pm[kBatch], ps[kBatch];
+      f32x4 po[kBatch];
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      const int i = min(i0 + u * STRIDE, parts - 1);
-      const int64_t at = (2 * (int64_t)(w + i) + (i == 0 ? left.z & 1 : 0)) * M + r;
-      pm[u] = a.part_ms[at * 2];
-      ps[u] = a.part_ms[at * 2 + 1];
-      po[u] = *reinterpret_cast<const f32x4*>(a.part + at * D + col);
+      for (int u = 0; u < kBatch; ++u) {
+        const int i = min(i0 + u * stride, parts - 1);
+        const int64_t at = (2 * (int64_t)(w + i) + (i == 0 ? left.z & 1 : 0)) * M + r;
+        pm[u] = a.part_ms[at * 2];
+        ps[u] = a.part_ms[at * 2 + 1];
+        po[u] = *reinterpret_cast<const f32x4*>(a.part + at * D + col);
+      }
+      float mn = m;
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, pm[u]);
+      const float ref = mn == -INFINITY ? 0.f : mn, fo = fast_exp2(m - ref);
+      m = mn;
+      s *= fo;
+      o *= fo;
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        if (i0 + u * stride >= parts) break;
+        const float fn = fast_exp2(pm[u] - ref);
+        s += ps[u] * fn;
+        o += po[u] * fn;
+      }
     }
-    float mn = m;
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, pm[u]);
-    const float ref = mn == -INFINITY ? 0.f : mn, fo = fast_exp2(m - ref);
-    m = mn;
-    s *= fo;
-    o *= fo;
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      if (i0 + u * STRIDE >= parts) break;
-      const float fn = fast_exp2(pm[u] - ref);
-      s += ps[u] * fn;
-      o += po[u] * fn;
-    }
+  };
+  auto write = [&](int r) {
+    const int tok = r / a.G, hd = r - tok * a.G;
+    const int64_t row = (int64_t)(g.t0 + tok0 + tok) * a.Hq + h * a.G + hd;
+    store_out4(a, row, D, col, o * (s == 0.f ? 0.f : 1.0f / s));
+    if (a.lse && col == 0) a.lse[row] = lse_of(m, s);
+  };
+  const int ny = gridDim.y;
+  if ((parts + kBatch - 1) / kBatch <= (nrow + ny - 1) / ny) {
+    const int r = blockIdx.y * NG + grp;
+    if (r >= nrow) return;
+    join(r, 0, 1);
+    write(r);
+    return;
   }
-  if (!MANY) {
+  for (int r = blockIdx.y; r < nrow; r += ny) {
+    join(r, grp, NG);
+    __syncthreads();  // the row before is done with LDS
     if (col == 0) {
       ms[grp] = m;
       ss[grp] = s;
     }
     *reinterpret_cast<f32x4*>(&os[grp][col]) = o;
     __syncthreads();
-    if (grp != 0) return;
+    if (grp != 0) continue;
     m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NG; ++i) m = fmaxf(m, ms[i]);
@@ -369,11 +389,8 @@ __global__ __launch_bounds__(kAttnBlock) void paged_merge_kernel(PagedAttnArgs a
       s += ss[i] * f;
       o += *reinterpret_cast<const f32x4*>(&os[i][col]) * f;
     }
+    write(r);
   }
-  const int tok = r / a.G, hd = r - tok * a.G;
-  const int64_t row = (int64_t)(g.t0 + tok0 + tok) * a.Hq + h * a.G + hd;
-  store_out4(a, row, D, col, o * (s == 0.f ? 0.f : 1.0f / s));
-  if (a.lse && col == 0) a.lse[row] = lse_of(m, s);
 }
 
 template <typename T, int D, int QB>
@@ -418,16 +435,12 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream) {
   prof_end(stream);
   if (e != hipSuccess) return e;
   prof_begin("paged_merge", stream);
-  const int rows = std::min(a.max_new, a.tokens) * a.G;
-  const int per = few ? 1 : kAttnBlock / (a.D / 4);  // rows of a workgroup
-  const dim3 grid(a.by_tile ? a.S * a.max_tiles : kPagedWorkers, (rows + per - 1) / per);
-  if (few) {
-    if (a.D == 128) paged_merge_kernel<128, false><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
-    else paged_merge_kernel<64, false><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
-  } else {
-    if (a.D == 128) paged_merge_kernel<128, true><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
-    else paged_merge_kernel<64, true><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
-  }
+  // A workgroup per row of a tile where that makes at most 4096, at least one per row group.
+  const int rows = std::min(a.max_new, a.tokens) * a.G, entries = a.by_tile ? a.S * a.max_tiles : kPagedWorkers;
+  const int groups = kAttnBlock / (a.D / 4);
+  const dim3 grid(entries, std::max((rows + groups - 1) / groups, std::min(rows, 4096 / entries)));
+  if (a.D == 128) paged_merge_kernel<128><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
+  else paged_merge_kernel<64><<<grid, dim3(kAttnBlock), 0, stream>>>(a);
   prof_end(stream);
   return hipGetLastError();
 }

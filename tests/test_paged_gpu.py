@@ -426,6 +426,21 @@ def test_paged_attention(case, causal):
         assert (out[n:] == 7.0).all() and (lse[n:] == 7.0).all()  # tokens of nobody
 
 
+@pytest.mark.parametrize("new,rows,hq,hkv,dtype", [
+    ([21], [56783], 5, 1, BF),               # one tile of 105 rows, hundreds of parts
+    ([7, 9], [9000, 9003, 40, 12345], 16, 2, F32),
+    ([128, 100], [2000] * 8, 28, 4, BF),     # about as many parts as a lane has under way, tiles of fewer rows
+    ([6] * 20, [3000] * 40, 16, 2, BF),
+])
+def test_paged_attention_of_many_parts(new, rows, hq, hkv, dtype):
+    _say(f"many parts {new[:3]} over {rows[:3]} {dtype}")
+    c = Case(new, rows, hq, hkv, 128, 64, dtype, seed=7)
+    out, lse = c.call(out_dtype=F32)
+    c.check(out, lse)
+    again = c.call(out_dtype=F32)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
 @pytest.mark.parametrize("new", [[1], [30]])
 @pytest.mark.parametrize("spread", [12.0, 0.0])
 def test_paged_attention_far_logits(new, spread):
