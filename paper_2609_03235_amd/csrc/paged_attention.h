@@ -207,8 +207,8 @@ __device__ __forceinline__ void leave_shared(const PagedAttnArgs& a, int w, int6
                                              int nkt, bool unshared) {
   const int64_t own = share * w;
   if (threadIdx.x != 0 || at.start < own) return;  // begun by a worker before
-  const int64_t last_key = at.start + (int64_t)(nkt - 1) * a.key_tile;
-  const int last = unshared || last_key < own + share ? -1 : (int)(last_key / share);
+  const int64_t past = at.start - own + (int64_t)(nkt - 1) * a.key_tile - share;  // the last key's place, from w + 1's
+  const int last = unshared || past < 0 ? -1 : w + 1 + (past < share ? 0 : (int)((uint32_t)past / (uint32_t)share));
   if (a.by_tile) a.shared[at.seg * a.max_tiles + at.tile] = make_int4(at.seg, at.tile, 2 * w + (at.start > own), last);
   else if (last >= 0) a.shared[w] = make_int4(at.seg, at.tile, 2 * w + (at.start > own), last);
 }

@@ -131,7 +131,10 @@ sgdkv_status plan_paged(const sgdkv_page_pool* pool, const sgdkv_paged_desc* d, 
   a.tokens = shape.rows / G;
   a.max_tiles = (a.max_new + a.tokens - 1) / a.tokens;
   a.by_tile = nseg * a.max_tiles <= sgdkv::kPagedWorkers;
-  a.min_shift = log2_of(shape.rows < 128 ? 128 : 2 * shape.key_tile);
+  // What a tile takes beside its keys is as much as so many keys. (128 query rows of bf16: prompts of 800 tokens with
+  // 64 / 8 heads 464 us with 128, 441 with 256, 455 with 512. fp32, whose keys take longer: 3 x 50 tokens over 1K
+  // 22.5 us with 64, 30 with 128.)
+  a.min_shift = log2_of(shape.rows < 128 ? 128 : (a.dtype ? 4 : 2) * shape.key_tile);
   // The workspace follows the bound the caller gave, whatever the tokens of this call.
   const int most_rows = sgdkv::paged_attn_shape(a.dtype, G, d->max_new).rows;
   bytes = (size_t)sgdkv::kPagedWorkers * (sizeof(int4) + 2 * (size_t)most_rows * (a.D + 2) * sizeof(float));

@@ -2,8 +2,10 @@
 //
 // A workgroup holds 128 query rows, 32 per wave, and walks the keys of its piece of the line in tiles that
 // all four waves share through LDS: two buffers, one barrier per tile, and the next tile on its way from memory
-// straight into LDS while one is computed (no registers, no LDS writes). Products are 32x32 MFMAs. Every row
-// keeps a reference for its exponentials that only moves when a tile's sum shows that it fell too far behind,
+// straight into LDS while one is computed (no registers, no LDS writes). A query tile's first keys and its queries
+// are under way while the results of the one before are written, whole lines at a time (312 prompts of 64 tokens,
+// 64 / 8 heads: 247 us with one after the other, 16 bytes of a row at a time; 206 so). Products are 32x32 MFMAs. Every
+// row keeps a reference for its exponentials that only moves when a tile's sum shows that it fell too far behind,
 // so a logit costs one fma, one exp2 and one add. 32 query rows a wave and two workgroups a compute unit are what the
 // registers (o takes 64, the queries 32, a tile's logits 32) and LDS (64 KB each) hold; the second workgroup runs
 // while the first waits. Bound by the matrix unit and the vector unit one after the other, at the socket's power:
@@ -37,8 +39,8 @@ struct ManyShape {
 
 // A query tile of at most so many keys is one worker's alone where that is at most twice a worker's share: a part
 // of a tile costs 64 KB of partial results, as much time as about 400 keys, written and read again (8 sequences of
-// 512 tokens with 28 / 4 heads 65 us shared, 59 so; 3 of 128 over 600 rows, whose tiles the second half leaves
-// shared, 32 and 36).
+// 512 tokens with 28 / 4 heads 61 us with 256 for 512, 52 so; 3 of 128 over 600 rows, whose tiles the second half
+// leaves shared, 32 and 36).
 template <typename T>
 constexpr int kUnshared = sizeof(T) == 2 ? 512 : 128;
 
@@ -75,13 +77,21 @@ struct Probs<__bf16, true, NK> : Probs<float, false, NK> {
   }
 };
 
+// A tile of the line as its worker does it.
+struct ManyTile {
+  LineTile at;
+  int limit, nkt;  // rows that it sees, in so many key tiles
+  int j0, j1;      // the worker's
+  bool own;        // not shared
+};
+
 template <typename T, int D, bool FINE>
 __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs a) {
   using S = ManyShape<T, D>;
   constexpr int EB = S::EB, RB = S::RB, KT = S::KT, NC = S::NC, NK = S::NK, ND = S::ND, NL = S::NL;
   constexpr int M = 128;
   __shared__ __attribute__((aligned(16))) char lds[2][2][S::TILE];  // two buffers of keys and values
-  __shared__ __attribute__((aligned(16))) int first_odd[D];
+  __shared__ __attribute__((aligned(16))) int odd[2][D];            // first_odd of this tile and of the next
   __shared__ LineScratch sc;
 
   const int tid = threadIdx.x, wid = uniform(tid >> 6), lane = tid & 63;
@@ -105,224 +115,285 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
   }
   const uint32_t lds0 = lds_address(&lds[0][0][0]);
 
-  while (pos < end) {
-    if (at.tile >= at.g.tiles) {  // the next segment
-      if (++at.seg >= a.S) return;
-      at.tile = 0;
-      at.g = paged_seg(a, at.seg);
-      continue;
+  // The next tile of the piece that this worker does, if there is one.
+  auto advance = [&](ManyTile& t) {
+    while (pos < end) {
+      if (at.tile >= at.g.tiles) {  // the next segment
+        if (++at.seg >= a.S) return false;
+        at.tile = 0;
+        at.g = paged_seg(a, at.seg);
+        continue;
+      }
+      t.at = at;
+      t.limit = uniform(tile_rows(a, at.g, at.tile));
+      t.nkt = max((t.limit + KT - 1) / KT, 1);
+      // A tile of few keys is not shared: the worker that it starts with does all of it.
+      t.own = t.limit <= kUnshared<T> && t.limit + (1 << a.min_shift) <= 2 * share;
+      t.j0 = t.own ? (at.start < share * w ? t.nkt : 0) : (int)((pos - at.start + KT - 1) / KT);
+      t.j1 = t.own ? t.nkt : (int)min((int64_t)t.nkt, (end - at.start + KT - 1) / KT);
+      at.start = pos = at.start + max(t.limit, 1) + (1 << a.min_shift);
+      ++at.tile;
+      if (t.j0 < t.j1) return true;
     }
-    const PagedSeg& g = at.g;
-    const int limit = uniform(tile_rows(a, g, at.tile));
-    const int nkt = max((limit + KT - 1) / KT, 1);
-    // A tile of few keys is not shared: the worker that it starts with does all of it.
-    const bool own = limit <= kUnshared<T> && limit + (1 << a.min_shift) <= 2 * share;
-    const int j0 = own ? (at.start < share * w ? nkt : 0) : (int)((pos - at.start + KT - 1) / KT);
-    const int j1 = own ? nkt : (int)min((int64_t)nkt, (end - at.start + KT - 1) / KT);
-    if (j0 < j1) {
-      const int h = at.seg % a.Hkv;
-      const int tok0 = at.tile * a.tokens, ntok = min(a.tokens, g.n - tok0);
-      const int nrow = ntok * a.G;
-      const int r = wid * 32 + lq, tok = r / a.G, hd = r - tok * a.G;
+    return false;
+  };
+
+  const int r = wid * 32 + lq, tok = r / a.G, hd = r - tok * a.G;  // the lane's row of a tile
+  const int32_t* table;
+  int page;
+  u32x4 q[NC];
+  auto load = [&](const ManyTile& t, int j) {
+    const int r0 = j * KT + my_row;
+    const u32x4 kr = group_words(a, a.k_pages, page, r0, t.limit - r0, S::RPW, RB);
+    const u32x4 vr = group_words(a, a.v_pages, page, r0, t.limit - r0, S::RPW, RB);
+    const uint32_t to = uniform((int)(lds0 + (j & 1) * 2 * S::TILE + my_row * RB));
+#pragma unroll
+    for (int i = 0; i < NL; ++i) load_to_lds(kr, koff[i], to + i * 1024);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) load_to_lds(vr, voff[i], to + S::TILE + i * 1024);
+  };
+  // Sets a tile's queries and first keys on their way; by then all waves are done with the keys before.
+  auto begin = [&](const ManyTile& t, int which) {
+    table = a.tables + (int64_t)t.at.seg * a.max_pages;
+    // Both pages are read before the loads: a wait for a read waits for all that were sent before it.
+    page = group_page(a, table, t.j0 * KT + my_row, t.limit);
+    const int page2 = uniform(group_page(a, table, (t.j0 + 1) * KT + my_row, t.limit));
+    page = uniform(page);
+    load(t, t.j0);
+    page = page2;
+    const int tok0 = t.at.tile * a.tokens, ntok = min(a.tokens, t.at.g.n - tok0);
+    const rsrc_t qr = make_rsrc(
+        static_cast<const char*>(a.q) + ((int64_t)(t.at.g.t0 + tok0) * a.Hq + t.at.seg % a.Hkv * a.G) * RB,
+        ((uint64_t)(ntok - 1) * a.Hq + a.G) * RB);
+    uint32_t from = r < ntok * a.G ? (uint32_t)((tok * a.Hq + hd) * RB + 16 * half) : 0xFFFFF000u;  // or past the end
+    asm("" : "+v"(from));  // one path for both: the compiler makes two of every load otherwise
+#pragma unroll
+    for (int c = 0; c < NC; ++c) q[c] = ld128(qr, from + 32 * c);
+    if (tid < D) odd[which][tid] = 0x7FFFFFFF;
+  };
+
+  ManyTile now, t;
+  bool busy = false;
+  int which = 0;
+  float m, s;
+  f32x16 o[ND];
+  for (;;) {
+    // The next tile's reads go out before the results of the one before.
+    const bool more = advance(t);
+    if (more) begin(t, which);
+    if (busy) {
+      leave_shared(a, w, share, now.at, now.nkt, now.own);
+      const PagedSeg& g = now.at.g;
+      const int tok0 = now.at.tile * a.tokens, h = now.at.seg % a.Hkv;
+      const int nrow = min(a.tokens, g.n - tok0) * a.G;
       const bool on = r < nrow;
       const int seen = on ? seen_by(a, g, tok0 + tok) : 0;
-      const int first_seen = seen_by(a, g, tok0);
-      // the rows of this wave see at most hi keys
-      const int hi = wid * 32 < nrow ? uniform(seen_by(a, g, tok0 + (min(nrow, wid * 32 + 32) - 1) / a.G)) : 0;
-
-      const int32_t* table = a.tables + (int64_t)at.seg * a.max_pages;
-      int page = uniform(group_page(a, table, j0 * KT + my_row, limit));
-      auto load = [&](int j) {
-        const int r0 = j * KT + my_row;
-        const u32x4 kr = group_words(a, a.k_pages, page, r0, limit - r0, S::RPW, RB);
-        const u32x4 vr = group_words(a, a.v_pages, page, r0, limit - r0, S::RPW, RB);
-        const uint32_t to = uniform((int)(lds0 + (j & 1) * 2 * S::TILE + my_row * RB));
-#pragma unroll
-        for (int i = 0; i < NL; ++i) load_to_lds(kr, koff[i], to + i * 1024);
-#pragma unroll
-        for (int i = 0; i < NL; ++i) load_to_lds(vr, voff[i], to + S::TILE + i * 1024);
-      };
-      u32x4 q[NC];
-      {
-        const rsrc_t qr = make_rsrc(static_cast<const char*>(a.q) + ((int64_t)(g.t0 + tok0) * a.Hq + h * a.G) * RB,
-                                    ((uint64_t)(ntok - 1) * a.Hq + a.G) * RB);
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-          q[c] = ld128(qr, on ? (uint32_t)((tok * a.Hq + hd) * RB + 32 * c + 16 * half) : 0xFFFFFF00u);
-      }
-      float m = on ? -INFINITY : 0.f, s = 0.f;
-      f32x16 o[ND];
-#pragma unroll
-      for (int d = 0; d < ND; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-
-      // One tile of keys, from key0 on, out of LDS. EDGE: some row does not see all of it; `left` is how many of the
-      // keys from 4 * half on this lane's row sees.
-      auto attend = [&](char* kb, auto edge, int key0) {
-        constexpr bool EDGE = decltype(edge)::value;
-        const int left = seen - key0 - 4 * half;
-        char* vb = kb + S::TILE;
-        // products first where waves compete: the other waves' exponentials fill in
-        __builtin_amdgcn_s_setprio(1);
-        f32x16 y[NK];
-        const int ksw = S::key_swizzle(lq);  // of every block's row: 32 rows on it repeats
-#pragma unroll
-        for (int n = 0; n < NK; ++n) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) y[n][i] = 0.f;
-#pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            const u32x4 kf =
-                *reinterpret_cast<const u32x4*>(kb + (32 * n + lq) * RB + (((2 * c + half) ^ ksw) * 16));
-            if constexpr (EB == 2) {
-              y[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
-                                                             __builtin_bit_cast(bf16x8, q[c]), y[n], 0, 0, 0);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                y[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(q[c][e]), y[n], 0,
-                                                            0, 0);
-            }
-          }
-        }
-        __builtin_amdgcn_s_setprio(0);
-        // lane: query row lq; register i of block n: key 32n + 8(i / 4) + 4 half + i % 4
-        auto sees = [&](int n, int i) { return !EDGE || 32 * n + 8 * (i / 4) + i % 4 < left; };
-        float sum;
-        Probs<T, FINE, NK> p;
-        auto exps = [&](float ref) {
-          float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int n = 0; n < NK; ++n)
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-              const float e0 = fast_exp2(fmaf(y[n][i], a.c2, -ref)), e1 = fast_exp2(fmaf(y[n][i + 1], a.c2, -ref));
-              const float p0 = sees(n, i) ? e0 : 0.f, p1 = sees(n, i + 1) ? e1 : 0.f;
-              part[(i / 2) & 3] += p0;
-              part[(i / 2) & 3] += p1;
-              p.set(n, i, p0, p1);
-            }
-          sum = (part[0] + part[1]) + (part[2] + part[3]);
-        };
-        exps(m);
-        // All lanes take this branch or none, and none branches in it: so the compiler keeps o in place.
-        if (__any(!(sum <= kFar) || m == -INFINITY)) {
-          float mx = -INFINITY;
-#pragma unroll
-          for (int n = 0; n < NK; ++n)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sees(n, i) ? y[n][i] * a.c2 : -INFINITY);
-          mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-          const float mn = fmaxf(m, mx);
-          const float alpha = m == mn ? 1.f : fast_exp2(m - mn);  // before the first key s and o are 0
-          s *= alpha;
-#pragma unroll
-          for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
-          m = mn;
-          exps(m == -INFINITY ? 0.f : m);  // nothing seen so far: all are 0
-        }
-        s += sum;
-        if constexpr (EDGE) clean_values<EB, RB>(vb, key0, max(first_seen - key0, 0), min(limit - key0, KT), first_odd,
-                                               S::value_swizzle);
-        __builtin_amdgcn_s_setprio(1);
-        if constexpr (EB == 2) {
-          const int l16 = lane & 15;
-          const int row = 4 * half + l16 / 4;                        // and 8, 16, ... further on: the same swizzle
-          const int place = 2 * ((lane >> 4) & 1) + (l16 & 3) / 2;  // of a block's four pieces
-          const char* vp = vb + row * RB + (l16 & 1) * 8;
-          auto values = [&](int t, int d) {
-            const char* vd = vp + (((4 * d + place) ^ S::value_swizzle(row)) * 16);
-            const u32x2 v0 = lds_transposed(vd + 16 * t * RB), v1 = lds_transposed(vd + (16 * t + 8) * RB);
-            return u32x4{v0.x, v0.y, v1.x, v1.y};
-          };
-#pragma unroll
-          for (int t = 0; t < KT / 16; ++t) {
-            u32x4 piece[FINE ? 3 : 1];
-            p.pieces(t, piece);
-#pragma unroll
-            for (int d = 0; d < ND; ++d) {
-              const bf16x8 vt = __builtin_bit_cast(bf16x8, values(t, d));
-#pragma unroll
-              for (int k = 0; k < (FINE ? 3 : 1); ++k)
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, __builtin_bit_cast(bf16x8, piece[k]), o[d], 0, 0,
-                                                               0);
-            }
-          }
-        } else {
-          auto value = [&](int n, int i, int d) {
-            const int row = 32 * n + 8 * (i / 4) + 4 * half + i % 4;
-            const int at = ((8 * d + lq / 4) ^ S::value_swizzle(4 * half)) * 16 + (lq & 3) * 4;
-            return *reinterpret_cast<const float*>(vb + row * RB + at);
-          };
-#pragma unroll
-          for (int n = 0; n < NK; ++n)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-#pragma unroll
-              for (int d = 0; d < ND; ++d)
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(n, i, d), p.v[n][i], o[d], 0, 0, 0);
-        }
-        __builtin_amdgcn_s_setprio(0);
-      };
-
-      __syncthreads();  // the buffers of the tile before are done with
-      if (tid < D) first_odd[tid] = 0x7FFFFFFF;
-      load(j0);
-      page = uniform(group_page(a, table, (j0 + 1) * KT + my_row, limit));
-      wait_loads();
-      __syncthreads();
-      // the tiles that every row sees whole, then the others
-      int j = j0;
-      auto tiles = [&](int to, auto edge) {
-        for (; j < to; ++j) {
-          // the page of the tile after the next, asked for before the next tile's loads and used after them
-          const int page2 = group_page(a, table, (j + 2) * KT + my_row, limit);
-          if (j + 1 < j1) load(j + 1);
-          if (j * KT < hi) attend(lds[j & 1][0], edge, j * KT);
-          wait_loads();
-          page = uniform(page2);
-          __syncthreads();
-        }
-      };
-      tiles(min(j1, first_seen / KT), std::false_type{});
-      tiles(j1, std::true_type{});
+      const int* first_odd = odd[which ^ 1];
       s += __shfl_xor(s, 32, 64);
       auto result = [&](int d, int i) {
         return lose_odd(f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]}, first_odd,
                         32 * d + 8 * i + 4 * half, seen);
       };
-      if (on) {
-        const bool whole = j0 == 0 && j1 == nkt;
-        if (whole) {
-          const int64_t row = (int64_t)(g.t0 + tok0 + tok) * a.Hq + h * a.G + hd;
-          const float inv = s == 0.f ? 0.f : 1.0f / s;
+      if (now.j0 == 0 && now.j1 == now.nkt) {
+        const int64_t row0 = (int64_t)(g.t0 + tok0) * a.Hq + h * a.G;  // the tile's first
+        const float inv = s == 0.f ? 0.f : 1.0f / s;
+        // Through LDS, in the buffer that the next tile's first keys do not go to, so that whole lines are written:
+        // the wave's 32 rows of 2 * D bytes, a bf16 row or half of an fp32 one.
+        char* mine = lds[~t.j0 & 1][0] + wid * (S::TILE / 2);
+        auto store = [&](auto out) {
+          constexpr int OB = sizeof(out), LPR = D / 8, DP = 2 * ND / OB;  // lanes to a row, blocks of 32 columns
+          char* to = static_cast<char*>(a.out) + row0 * (D * OB);
 #pragma unroll
-          for (int d = 0; d < ND; ++d)
+          for (int d0 = 0; d0 < ND; d0 += DP) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              store_out4(a, row, D, 32 * d + 8 * i + 4 * half, result(d, i) * inv);
-          if (a.lse && half == 0) a.lse[row] = lse_of(m, s);
-        } else {
-          const int64_t slot = 2 * (int64_t)w + (at.start > share * w ? 1 : 0);
+            for (int d = 0; d < DP; ++d)
 #pragma unroll
-          for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              *reinterpret_cast<f32x4*>(a.part + (slot * M + r) * D + 32 * d + 8 * i + 4 * half) = result(d, i);
-          if (half == 0) {
-            a.part_ms[(slot * M + r) * 2] = m;
-            a.part_ms[(slot * M + r) * 2 + 1] = s;
+              for (int i = 0; i < 4; ++i) {
+                const f32x4 v = result(d0 + d, i) * inv;
+                const int byte = (32 * d + 8 * i + 4 * half) * OB;
+                char* place = mine + lq * (2 * D) + (((byte / 16) ^ (lq & (LPR - 1))) * 16) + byte % 16;
+                if constexpr (OB == 2)
+                  *reinterpret_cast<u32x2*>(place) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+                else
+                  *reinterpret_cast<f32x4*>(place) = v;
+              }
+#pragma unroll 2
+            for (int r0 = 0; r0 < 32; r0 += 64 / LPR) {
+              const int from = r0 + lane / LPR, c = lane % LPR;
+              const u32x4 v = *reinterpret_cast<const u32x4*>(mine + from * (2 * D) + ((c ^ (from & (LPR - 1))) * 16));
+              const uint32_t row = __shfl(tok * a.Hq + hd, from, 64);
+              if (wid * 32 + from < nrow)
+                *reinterpret_cast<u32x4*>(to + (row * (D * OB) + (uint32_t)(d0 * 32 * OB + c * 16))) = v;
+            }
           }
+        };
+        if (FINE || (EB == 4 && !a.out_dtype)) store(float{});
+        else store(__bf16{});
+        if (on && a.lse && half == 0) a.lse[row0 + tok * a.Hq + hd] = lse_of(m, s);
+      } else if (on) {
+        const int64_t slot = 2 * (int64_t)w + (now.at.start > share * w ? 1 : 0);
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<f32x4*>(a.part + (slot * M + r) * D + 32 * d + 8 * i + 4 * half) = result(d, i);
+        if (half == 0) {
+          a.part_ms[(slot * M + r) * 2] = m;
+          a.part_ms[(slot * M + r) * 2 + 1] = s;
         }
       }
     }
-    const int64_t next = at.start + max(limit, 1) + (1 << a.min_shift);
-    leave_shared(a, w, share, at, nkt, own);
-    at.start = pos = next;
-    ++at.tile;
+    if (!more) return;
+    busy = true;
+    now = t;
+    const PagedSeg& g = now.at.g;
+    const int limit = now.limit, tok0 = now.at.tile * a.tokens;
+    const int nrow = min(a.tokens, g.n - tok0) * a.G;
+    const bool on = r < nrow;
+    const int seen = on ? seen_by(a, g, tok0 + tok) : 0;
+    const int first_seen = seen_by(a, g, tok0);
+    // the rows of this wave see at most hi keys
+    const int hi = wid * 32 < nrow ? uniform(seen_by(a, g, tok0 + (min(nrow, wid * 32 + 32) - 1) / a.G)) : 0;
+    int* first_odd = odd[which];
+    m = on ? -INFINITY : 0.f;
+    s = 0.f;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+
+    // One tile of keys, from key0 on, out of LDS. EDGE: some row does not see all of it; `left` is how many of the
+    // keys from 4 * half on this lane's row sees.
+    auto attend = [&](char* kb, auto edge, int key0) {
+      constexpr bool EDGE = decltype(edge)::value;
+      const int left = seen - key0 - 4 * half;
+      char* vb = kb + S::TILE;
+      // products first where waves compete: the other waves' exponentials fill in
+      __builtin_amdgcn_s_setprio(1);
+      f32x16 y[NK];
+      const int ksw = S::key_swizzle(lq);  // of every block's row: 32 rows on it repeats
+#pragma unroll
+      for (int n = 0; n < NK; ++n) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[n][i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const u32x4 kf =
+              *reinterpret_cast<const u32x4*>(kb + (32 * n + lq) * RB + (((2 * c + half) ^ ksw) * 16));
+          if constexpr (EB == 2) {
+            y[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
+                                                           __builtin_bit_cast(bf16x8, q[c]), y[n], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              y[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(q[c][e]), y[n], 0,
+                                                          0, 0);
+          }
+        }
+      }
+      __builtin_amdgcn_s_setprio(0);
+      // lane: query row lq; register i of block n: key 32n + 8(i / 4) + 4 half + i % 4
+      auto sees = [&](int n, int i) { return !EDGE || 32 * n + 8 * (i / 4) + i % 4 < left; };
+      float sum;
+      Probs<T, FINE, NK> p;
+      auto exps = [&](float ref) {
+        float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            const float e0 = fast_exp2(fmaf(y[n][i], a.c2, -ref)), e1 = fast_exp2(fmaf(y[n][i + 1], a.c2, -ref));
+            const float p0 = sees(n, i) ? e0 : 0.f, p1 = sees(n, i + 1) ? e1 : 0.f;
+            part[(i / 2) & 3] += p0;
+            part[(i / 2) & 3] += p1;
+            p.set(n, i, p0, p1);
+          }
+        sum = (part[0] + part[1]) + (part[2] + part[3]);
+      };
+      exps(m);
+      // All lanes take this branch or none, and none branches in it: so the compiler keeps o in place.
+      if (__any(!(sum <= kFar) || m == -INFINITY)) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sees(n, i) ? y[n][i] * a.c2 : -INFINITY);
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float mn = fmaxf(m, mx);
+        const float alpha = m == mn ? 1.f : fast_exp2(m - mn);  // before the first key s and o are 0
+        s *= alpha;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+        m = mn;
+        exps(m == -INFINITY ? 0.f : m);  // nothing seen so far: all are 0
+      }
+      s += sum;
+      if constexpr (EDGE) clean_values<EB, RB>(vb, key0, max(first_seen - key0, 0), min(limit - key0, KT), first_odd,
+                                             S::value_swizzle);
+      __builtin_amdgcn_s_setprio(1);
+      if constexpr (EB == 2) {
+        const int l16 = lane & 15;
+        const int row = 4 * half + l16 / 4;                        // and 8, 16, ... further on: the same swizzle
+        const int place = 2 * ((lane >> 4) & 1) + (l16 & 3) / 2;  // of a block's four pieces
+        const char* vp = vb + row * RB + (l16 & 1) * 8;
+        auto values = [&](int t, int d) {
+          const char* vd = vp + (((4 * d + place) ^ S::value_swizzle(row)) * 16);
+          const u32x2 v0 = lds_transposed(vd + 16 * t * RB), v1 = lds_transposed(vd + (16 * t + 8) * RB);
+          return u32x4{v0.x, v0.y, v1.x, v1.y};
+        };
+#pragma unroll
+        for (int t = 0; t < KT / 16; ++t) {
+          u32x4 piece[FINE ? 3 : 1];
+          p.pieces(t, piece);
+#pragma unroll
+          for (int d = 0; d < ND; ++d) {
+            const bf16x8 vt = __builtin_bit_cast(bf16x8, values(t, d));
+#pragma unroll
+            for (int k = 0; k < (FINE ? 3 : 1); ++k)
+              o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, __builtin_bit_cast(bf16x8, piece[k]), o[d], 0, 0,
+                                                             0);
+          }
+        }
+      } else {
+        auto value = [&](int n, int i, int d) {
+          const int row = 32 * n + 8 * (i / 4) + 4 * half + i % 4;
+          const int at = ((8 * d + lq / 4) ^ S::value_swizzle(4 * half)) * 16 + (lq & 3) * 4;
+          return *reinterpret_cast<const float*>(vb + row * RB + at);
+        };
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+              o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(n, i, d), p.v[n][i], o[d], 0, 0, 0);
+      }
+      __builtin_amdgcn_s_setprio(0);
+    };
+
+    wait_loads();
+    // Tells the compiler that the queries are there too: it would wait for them in the loop, and so for its loads.
+#pragma unroll
+    for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(q[c]));
+    __syncthreads();
+    // the tiles that every row sees whole, then the others
+    int j = now.j0;
+    auto tiles = [&](int to, auto edge) {
+      for (; j < to; ++j) {
+        // the page of the tile after the next, asked for before the next tile's loads and used after them
+        const int page2 = group_page(a, table, (j + 2) * KT + my_row, limit);
+        if (j + 1 < now.j1) load(now, j + 1);
+        if (j * KT < hi) attend(lds[j & 1][0], edge, j * KT);
+        wait_loads();
+        page = uniform(page2);
+        __syncthreads();
+      }
+    };
+    tiles(min(now.j1, first_seen / KT), std::false_type{});
+    tiles(now.j1, std::true_type{});
+    which ^= 1;
   }
 }
 

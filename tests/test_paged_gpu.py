@@ -441,6 +441,34 @@ def test_paged_attention_of_many_parts(new, rows, hq, hkv, dtype):
     assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
 
 
+@pytest.mark.parametrize("dtype,out_dtype,d", [(BF, BF, 128), (BF, F32, 128), (BF, BF, 64), (F32, F32, 64),
+                                               (F32, BF, 128)])
+def test_paged_attention_of_many_prompts(dtype, out_dtype, d):
+    """More tiles than workers: each does several, one after the other, and a value that is not finite in one tile
+    stays out of the others."""
+    new = [40, 33, 0, 70, 5, 1] * 50
+    rows = [n + (17 * i) % 150 for i, n in enumerate(x for n in new for x in (n, n))]
+    _say(f"many prompts {dtype} -> {out_dtype} d {d}")
+    c = Case(new, rows, 16, 2, d, 32, dtype, seed=d)
+    out, lse = c.call(out_dtype=out_dtype)
+    c.check(out, lse)
+    t0 = 0
+    want = out.clone()
+    for b, n in enumerate(new):
+        for h in range(2):
+            seg = 2 * b + h
+            if n >= 33 and seg % 3 == 0:
+                row, col = rows[seg] - n + n // 2, (7 * seg) % d  # the row of new token n / 2
+                page = int(c.tables[seg, row // 32])
+                c.v_pages[page, row % 32, col] = float("inf")
+                want[t0 + n // 2:t0 + n, 8 * h:8 * h + 8, col] = float("nan")
+        t0 += n
+    out, lse2 = c.call(out_dtype=out_dtype)
+    assert torch.equal(lse, lse2)
+    seen = want.isnan()
+    assert not torch.isfinite(out[seen]).any() and torch.equal(out[~seen], want[~seen])
+
+
 @pytest.mark.parametrize("new", [[1], [30]])
 @pytest.mark.parametrize("spread", [12.0, 0.0])
 def test_paged_attention_far_logits(new, spread):
