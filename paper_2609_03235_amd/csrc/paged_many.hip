@@ -264,7 +264,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
 
     // One tile of keys, from key0 on, out of LDS. EDGE: some row does not see all of it; `left` is how many of the
     // keys from 4 * half on this lane's row sees.
-    auto attend = [&](char* kb, auto edge, int key0) {
+    auto attend = [&](char* kb, auto edge, int key0, bool first) {
       constexpr bool EDGE = decltype(edge)::value;
       const int left = seen - key0 - 4 * half;
       char* vb = kb + S::TILE;
@@ -310,7 +310,10 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
           }
         sum = (part[0] + part[1]) + (part[2] + part[3]);
       };
-      exps(m);
+      // The first keys of a tile have no reference yet: at once to the branch (prompts of 64 tokens 3 % faster; in
+      // the tiles that every row sees whole the test costs long calls as much).
+      if (EDGE && first) sum = INFINITY;
+      else exps(m);
       // All lanes take this branch or none, and none branches in it: so the compiler keeps o in place.
       if (__any(!(sum <= kFar) || m == -INFINITY)) {
         float mx = -INFINITY;
@@ -385,7 +388,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
         // the page of the tile after the next, asked for before the next tile's loads and used after them
         const int page2 = group_page(a, table, (j + 2) * KT + my_row, limit);
         if (j + 1 < now.j1) load(now, j + 1);
-        if (j * KT < hi) attend(lds[j & 1][0], edge, j * KT);
+        if (j * KT < hi) attend(lds[j & 1][0], edge, j * KT, j == now.j0);
         wait_loads();
         page = uniform(page2);
         __syncthreads();
