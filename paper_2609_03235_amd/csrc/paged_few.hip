@@ -6,7 +6,7 @@
 // layout, values straight into LDS that only this wave uses (two buffers), for the transposing read. The next
 // step's loads start as soon as the step's keys are used up, so that all but the logits of a step runs beside
 // them: 8 waves of a compute unit have 128 KB under way. 32 tokens over 4 x 32K rows each (28 / 4 heads of 128, bf16)
-// take 335 us, 6.4 TB/s; 1 to 6 tokens of 16 sequences over 8 x 20K rows (64 / 8 heads, fp32 out) 228, 5.7 TB/s.
+// take 335 us, 6.4 TB/s; 1 to 6 tokens of 16 sequences over 8 x 20K rows (64 / 8 heads, fp32 out) 226, 5.7 TB/s.
 #include <algorithm>
 
 #include "paged_attention.h"

@@ -9,7 +9,7 @@
 // so a logit costs one fma, one exp2 and one add. 32 query rows a wave and two workgroups a compute unit are what the
 // registers (o takes 64, the queries 32, a tile's logits 32) and LDS (64 KB each) hold; the second workgroup runs
 // while the first waits. Bound by the matrix unit and the vector unit one after the other, at the socket's power:
-// two sequences of 8192 tokens over 16K rows, 64 / 8 heads of 128, bf16: 10.5 ms, 0.99 PFLOP/s, at 1.7 to 1.8 GHz
+// two sequences of 8192 tokens over 16K rows, 64 / 8 heads of 128, bf16: 10.6 ms, 0.98 PFLOP/s, at 1.7 to 1.8 GHz
 // (8.5 ms on zeros).
 #include <type_traits>
 
