@@ -9,7 +9,7 @@
 // so a logit costs one fma, one exp2 and one add. 32 query rows a wave and two workgroups a compute unit are what the
 // registers (o takes 64, the queries 32, a tile's logits 32) and LDS (64 KB each) hold; the second workgroup runs
 // while the first waits. Bound by the matrix unit and the vector unit one after the other, at the socket's power:
-// two sequences of 8192 tokens over 16K rows, 64 / 8 heads of 128, bf16: 10.6 ms, 0.98 PFLOP/s, at 1.7 to 1.8 GHz
+// two sequences of 8192 tokens over 16K rows, 64 / 8 heads of 128, bf16: 10.4 ms, 1.00 PFLOP/s, at 1.7 to 1.8 GHz
 // (8.5 ms on zeros).
 #include <type_traits>
 
@@ -273,23 +273,43 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
       f32x16 y[NK];
       const int ksw = S::key_swizzle(lq);  // of every block's row: 32 rows on it repeats
 #pragma unroll
-      for (int n = 0; n < NK; ++n) {
+      for (int n = 0; n < NK; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i) y[n][i] = 0.f;
+      auto key = [&](int n, int c) {
+        return *reinterpret_cast<const u32x4*>(kb + (32 * n + lq) * RB + (((2 * c + half) ^ ksw) * 16));
+      };
+      if constexpr (EB == 2) {
+        // Four pieces are read while the four before are multiplied. (Left alone, the compiler reads each just before
+        // its product and waits: with the same for the values, 8192 tokens over 16K rows 10.8 ms, 10.4 so.)
+        u32x4 kf[2][4];
+        auto read = [&](int g) {
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          const u32x4 kf =
-              *reinterpret_cast<const u32x4*>(kb + (32 * n + lq) * RB + (((2 * c + half) ^ ksw) * 16));
-          if constexpr (EB == 2) {
-            y[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
-                                                           __builtin_bit_cast(bf16x8, q[c]), y[n], 0, 0, 0);
-          } else {
+          for (int e = 0; e < 4; ++e) kf[g & 1][e] = key(e % NK, 2 * g + e / NK);
+        };
+        read(0);
+#pragma unroll
+        for (int g = 0; g < NK * NC / 4; ++g) {
+          if (g + 1 < NK * NC / 4) read(g + 1);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            y[e % NK] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[g & 1][e]),
+                                                                __builtin_bit_cast(bf16x8, q[2 * g + e / NK]),
+                                                                y[e % NK], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      } else {
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            const u32x4 kf = key(n, c);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              y[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(q[c][e]), y[n], 0,
-                                                          0, 0);
+              y[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(q[c][e]), y[n], 0, 0,
+                                                          0);
           }
-        }
       }
       __builtin_amdgcn_s_setprio(0);
       // lane: query row lq; register i of block n: key 32n + 8(i / 4) + 4 half + i % 4
@@ -346,18 +366,25 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
           const u32x2 v0 = lds_transposed(vd + 16 * t * RB), v1 = lds_transposed(vd + (16 * t + 8) * RB);
           return u32x4{v0.x, v0.y, v1.x, v1.y};
         };
+        u32x4 vf[2][ND];
+        auto read = [&](int t) {
+#pragma unroll
+          for (int d = 0; d < ND; ++d) vf[t & 1][d] = values(t, d);
+        };
+        read(0);
 #pragma unroll
         for (int t = 0; t < KT / 16; ++t) {
+          if (t + 1 < KT / 16) read(t + 1);
           u32x4 piece[FINE ? 3 : 1];
           p.pieces(t, piece);
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int d = 0; d < ND; ++d) {
-            const bf16x8 vt = __builtin_bit_cast(bf16x8, values(t, d));
+          for (int k = 0; k < (FINE ? 3 : 1); ++k)
 #pragma unroll
-            for (int k = 0; k < (FINE ? 3 : 1); ++k)
-              o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, __builtin_bit_cast(bf16x8, piece[k]), o[d], 0, 0,
-                                                             0);
-          }
+            for (int d = 0; d < ND; ++d)
+              o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[t & 1][d]),
+                                                             __builtin_bit_cast(bf16x8, piece[k]), o[d], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
         }
       } else {
         auto value = [&](int n, int i, int d) {
