@@ -507,8 +507,9 @@ sgdkv_status sgdkv_paged_attention_workspace_size(const sgdkv_page_pool* pool, c
  * [0, T]. out: device [T][Hq][d] out_dtype, lse_out: optional device [T][Hq]
  * fp32; tokens in no sequence, and those past a sequence's first max_new,
  * keep what these held.
- * Probabilities are rounded to bf16 for bf16 out of bf16 inputs and keep their
- * fp32 bits otherwise. A value that is not finite makes the outputs of its
+ * Probabilities are rounded to bf16 for bf16 out of bf16 inputs with more than
+ * 48 query rows per KV head (min(max_new, T) * Hq/Hkv) and keep their fp32 bits
+ * otherwise. A value that is not finite makes the outputs of its
  * column, of the tokens that see its row, not finite, and no others.
  * Errors (nothing enqueued): a bad pool; sizes out of range; Hq % Hkv; more
  * than 16 query heads per KV head, 8192 query heads or 65535 segments

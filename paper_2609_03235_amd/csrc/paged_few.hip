@@ -29,9 +29,12 @@ struct FewShape {
   }
 };
 
-// QB: 16-row query blocks. FINE: probabilities as three bf16 terms, all their 24 bits (fp32 output of
-// bf16 inputs).
-template <typename T, int D, int QB, bool FINE>
+// QB: 16-row query blocks. The probabilities of bf16 inputs go into the product as three bf16 terms, all their 24
+// bits, whatever the output's type: the products run beside the loads that bound the call (1 token of 32 sequences over
+// 32K rows 337 us with one term, 335 with three; 48 rows, 16 x 6 tokens over 4 x 20K rows, 127 and 131), and one term
+// adds an error of its own (64 x 1 tokens over 5K rows 1.72e-3 of the output, rms, where the output's own rounding is
+// 1.67e-3).
+template <typename T, int D, int QB>
 __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs a) {
   using S = FewShape<T, D>;
   constexpr int EB = S::EB, RB = S::RB, NC = S::NC, ND = S::ND, U = S::U, STEP = S::STEP, KT = S::KT, NV = S::NV;
@@ -201,15 +204,12 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
           }
         }
         if constexpr (EB == 2) {
-          u32x4 piece[QB][FINE ? 3 : 1];
+          u32x4 piece[QB][3];
 #pragma unroll
           for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float x = p[qb][e / 2][2 * (e % 2)], y = p[qb][e / 2][2 * (e % 2) + 1];
-              if constexpr (FINE) split_bf16(x, y, piece[qb], e);
-              else piece[qb][0][e] = pack_bf16(x, y);
-            }
+            for (int e = 0; e < 4; ++e)
+              split_bf16(p[qb][e / 2][2 * (e % 2)], p[qb][e / 2][2 * (e % 2) + 1], piece[qb], e);
           const int row = 4 * lg + lr / 4;  // and 16 further on: the same swizzle
           const char* vp = vals + row * RB + (lr & 1) * 8;
 #pragma unroll
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-              for (int k = 0; k < (FINE ? 3 : 1); ++k) o[qb][d] = mma(vt, Frag<__bf16>{piece[qb][k]}, o[qb][d]);
+              for (int k = 0; k < 3; ++k) o[qb][d] = mma(vt, Frag<__bf16>{piece[qb][k]}, o[qb][d]);
           }
         } else {
 #pragma unroll
@@ -395,13 +395,7 @@ __global__ __launch_bounds__(kAttnBlock) void paged_merge_kernel(PagedAttnArgs a
 
 template <typename T, int D, int QB>
 void launch_few(const PagedAttnArgs& a, hipStream_t stream) {
-  if constexpr (sizeof(T) == 2) {
-    if (a.out_dtype == 0) {
-      paged_few_kernel<T, D, QB, true><<<dim3(kPagedWorkers), dim3(kAttnBlock), 0, stream>>>(a);
-      return;
-    }
-  }
-  paged_few_kernel<T, D, QB, false><<<dim3(kPagedWorkers), dim3(kAttnBlock), 0, stream>>>(a);
+  paged_few_kernel<T, D, QB><<<dim3(kPagedWorkers), dim3(kAttnBlock), 0, stream>>>(a);
 }
 
 template <typename T, int D>

@@ -842,3 +842,19 @@ def test_table_of_repeated_pages_past_2_to_25_rows(new):
     # a worker adds 79000 rows, 4 at a time per lane group and 16 per product: 2500 roundings at most meet in a sum
     assert (out.double().flatten(0, 1) - want).abs().max() < 2500 * 2.0 ** -24 * 1.0 + 2e-5
     assert (lse.double().flatten() - wlse).abs().max() < 2500 * 2.0 ** -24 + 2e-5
+
+
+@pytest.mark.parametrize("new,rows,hq,hkv,d", [
+    ([1, 1], [700, 30000, 1, 64], 16, 2, 128),          # 8 rows of 16
+    ([1, 2, 1], [90, 4000, 333], 16, 1, 64),            # 32 rows
+    ([6, 1, 3], [5000, 129, 7, 700, 16, 90], 16, 2, 128),  # 48 rows
+])
+def test_paged_attention_of_few_rows_keeps_the_probabilities_bits(new, rows, hq, hkv, d):
+    """bf16 output of up to 48 query rows per KV head is the fp32 output rounded once: bit for bit, and within the
+    fp32 output's tolerance and half a bf16 step of the 64-bit value."""
+    _say(f"probabilities {new} {hq}/{hkv}/{d}")
+    c = Case(new, rows, hq, hkv, d, 16, BF, seed=17)
+    out, lse = c.call(out_dtype=BF)
+    fine, lse2 = c.call(out_dtype=F32)
+    c.check(fine, lse2)
+    assert torch.equal(out, fine.to(BF)) and torch.equal(lse, lse2)
