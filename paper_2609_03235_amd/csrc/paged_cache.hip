@@ -424,7 +424,7 @@ __global__ __launch_bounds__(kPageBlock) void norm_rope_kernel(NormRopeArgs a) {
         float p[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) p[e] = a.interleaved ? x[e ^ 1] : __shfl(x[e], partner, 64);
-        if (is_q || is_k) {
+        if (turns && (is_q || is_k)) {  // columns that do not turn: nothing times zero, which may be infinite
 #pragma unroll
           for (int e = 0; e < N; ++e) x[e] = fmaf(p[e], sn[e], x[e] * cs[e]);
         }

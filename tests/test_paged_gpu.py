@@ -858,3 +858,31 @@ def test_paged_attention_of_few_rows_keeps_the_probabilities_bits(new, rows, hq,
     fine, lse2 = c.call(out_dtype=F32)
     c.check(fine, lse2)
     assert torch.equal(out, fine.to(BF)) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("dtype,d,rot", [(BF, 128, 64), (F32, 128, 96), (F32, 64, 16), (BF, 64, 32)])
+def test_norm_rope_columns_that_do_not_turn(dtype, d, rot, inter):
+    """Without a norm the columns from rot on are copied, whatever they hold: infinities, NaN and both zeros bit for
+    bit; and the others come out as if those held ordinary values."""
+    _say(f"columns that do not turn {dtype} {d}/{rot}")
+    g = torch.Generator(device=DEV).manual_seed(rot)
+    T, hq, hkv = 9, 5, 2
+    q, k, v = (torch.randn(T, h, d, generator=g, device=DEV).to(dtype) for h in (hq, hkv, hkv))
+    inv = (1e4 ** (-torch.arange(0, rot, 2, device=DEV) / rot)).float()
+    pos = 11 + 1000 * torch.arange(T, device=DEV, dtype=torch.int32)
+    slots = torch.arange(T * hkv, device=DEV, dtype=torch.int32).view(T, hkv)
+    outs = []
+    for odd in (False, True):
+        kp, vp = (torch.zeros(2, 16, d, device=DEV, dtype=dtype) for _ in range(2))
+        if odd:
+            special = torch.tensor([math.inf, -math.inf, math.nan, -0.0, 0.0, 1.0, -2.0], device=DEV).to(dtype)
+            for x in (q, k):
+                x[..., rot:] = special[torch.randint(0, 7, x[..., rot:].shape, generator=g, device=DEV)]
+        out = sg.norm_rope_store(q, k, v, pos, slots, kp, vp, inv_freq=inv, interleaved=inter)
+        stored = kp.view(-1, d)[:T * hkv].view(T, hkv, d)
+        bits = torch.int16 if dtype == BF else torch.int32
+        for got, had in ((out, q), (stored, k)):
+            assert torch.equal(got[..., rot:].contiguous().view(bits), had[..., rot:].contiguous().view(bits))
+        outs.append((out[..., :rot], stored[..., :rot]))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
