@@ -273,26 +273,28 @@ __global__ __launch_bounds__(kPageBlock) void paged_store_kernel(PagedStoreArgs 
 // ------------------------------------------------------------------ norm, rotation, store
 // sin and cos of position * freq. In turns the angle is position * freq / (2 pi): both products are carried with
 // their rounding errors, and the nearest quarter turn is taken off in 64 bits, which leaves an angle x in
-// [-pi/4, pi/4] for the Taylor sums (the first terms left out are below 2e-9 and 2e-10). So the angle of a position
-// of 2^31 is as good as that of a small one.
+// [-pi/4, pi/4] for the Taylor sums (the first terms left out are below 2e-9 and 2e-10 of a radian). So the angle of a
+// position of 2^31 is as good as that of a small one. The sums are in 64 bits too, and what they give is rounded once: an
+// x rounded to 32 bits alone is off by up to 2^-25, 2^-27.7 turns. (A lane does this once per token, for all heads.)
 __device__ __forceinline__ void sincos_at(double position, double freq, float& sin_t, float& cos_t) {
   constexpr double kHi = 0.15915494309189535, kLo = -9.839338337591243e-18;  // 1 / (2 pi)
   const double a0 = position * freq, a1 = fma(position, freq, -a0);
   const double t = a0 * kHi, t1 = fma(a0, kHi, -t) + fma(a0, kLo, a1 * kHi);
   const double n = rint(4.0 * t);
-  const float x = (float)((fma(-0.25, n, t) + t1) * 6.283185307179586476925);
-  const float z = x * x;
-  float s = fmaf(z, 2.7557319e-6f, -1.9841270e-4f);
-  s = fmaf(z, s, 8.3333333e-3f);
-  s = fmaf(z, s, -1.6666667e-1f);
-  s = fmaf(x * z, s, x);
-  float c = fmaf(z, -2.7557319e-7f, 2.4801587e-5f);
-  c = fmaf(z, c, -1.3888889e-3f);
-  c = fmaf(z, c, 4.1666667e-2f);
-  c = fmaf(z, c, -0.5f);
-  c = fmaf(z, c, 1.0f);
+  const double x = (fma(-0.25, n, t) + t1) * 6.283185307179586476925;
+  const double z = x * x;
+  double s = fma(z, 1.0 / 362880, -1.0 / 5040);
+  s = fma(z, s, 1.0 / 120);
+  s = fma(z, s, -1.0 / 6);
+  s = fma(x * z, s, x);
+  double c = fma(z, -1.0 / 3628800, 1.0 / 40320);
+  c = fma(z, c, -1.0 / 720);
+  c = fma(z, c, 1.0 / 24);
+  c = fma(z, c, -0.5);
+  c = fma(z, c, 1.0);
   const int quarter = (int)((long long)n & 3);
-  const float a = quarter & 1 ? c : s, b = quarter & 1 ? s : c;
+  const float sx = (float)s, cx = (float)c;
+  const float a = quarter & 1 ? cx : sx, b = quarter & 1 ? sx : cx;
   sin_t = quarter & 2 ? -a : a;
   cos_t = quarter == 1 || quarter == 2 ? -b : b;
 }

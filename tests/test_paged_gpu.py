@@ -886,3 +886,34 @@ def test_norm_rope_columns_that_do_not_turn(dtype, d, rot, inter):
             assert torch.equal(got[..., rot:].contiguous().view(bits), had[..., rot:].contiguous().view(bits))
         outs.append((out[..., :rot], stored[..., :rot]))
     assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("first", [0, 131072, 2**31 - 3000, -3000])
+def test_norm_rope_angles(first, inter):
+    """Pairs (1, 0) turn into (cos t, sin t) with no rounding of their own, so what comes out is the cosine and sine: off
+    by an angle of 2^-31 turns at most (their slope is 1 at most) and by their rounding to fp32, half a step of the
+    value. The reference takes the exact product of position and frequency in 80 bits and its sine in 64."""
+    _say(f"angles from {first}")
+    np = pytest.importorskip("numpy")
+    T, d = 3000, 128
+    half = d // 2
+    pos = first + torch.arange(T, dtype=torch.int64)
+    inv = (1e6 ** (-torch.arange(0, d, 2, dtype=torch.float64) / d)).float()
+    k = torch.zeros(T, 1, d, device=DEV)
+    k[..., 0::2] = 1.0 if inter else 0.0
+    if not inter:
+        k[..., :half] = 1.0
+    kp, vp = (torch.zeros(-(-T // 16), 16, d, device=DEV) for _ in range(2))
+    slots = torch.arange(T, device=DEV, dtype=torch.int32)[:, None].contiguous()
+    sg.norm_rope_store(None, k, k, pos.to(torch.int32).to(DEV), slots, kp, vp, inv_freq=inv.to(DEV), interleaved=inter)
+    out = kp.view(-1, d)[:T].cpu().double()
+    cos, sin = (out[:, 0::2], out[:, 1::2]) if inter else (out[:, :half], out[:, half:])
+    # a 31-bit position by a 24-bit frequency is exact in 80 bits; so is nearly its rest of whole turns (2^-64 2^31)
+    pi2 = np.longdouble(2 * math.pi) + np.longdouble(2.449293598294706e-16)
+    t = pos.numpy().astype(np.longdouble)[:, None] * inv.numpy().astype(np.longdouble)[None]
+    t = torch.from_numpy((t - np.rint(t / pi2) * pi2).astype(np.float64))
+    for got, want in ((cos, torch.cos(t)), (sin, torch.sin(t))):
+        tol = 2.0 ** -24 * want.abs() + 2 * math.pi * 2.0 ** -31
+        err = (got - want).abs()
+        assert (err <= tol).all(), float((err / tol).max())
