@@ -461,32 +461,62 @@ hipError_t launch_page_update(const PageArgs& a, int cus, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_paged_store(const PagedStoreArgs& a, hipStream_t stream) {
-  if (a.n == 0) return hipSuccess;
-  const int64_t per = kStoreVecs * kPageBlock, blocks = ((a.n << a.row_shift) + per - 1) / per;
+// A launch holds fewer than 2^32 threads; more rows or tokens than that go in several.
+constexpr int64_t kMaxBlocks = (int64_t(1) << 23);
+
+hipError_t launch_paged_store(const PagedStoreArgs& args, hipStream_t stream) {
+  const int64_t per = kStoreVecs * kPageBlock, most = (kMaxBlocks * per) >> args.row_shift;
+  const int64_t row_bytes = int64_t(16) << args.row_shift;
+  if (args.n == 0) return hipSuccess;
   prof_begin("paged_store", stream);
-  paged_store_kernel<<<dim3((unsigned)blocks), dim3(kPageBlock), 0, stream>>>(a);
+  for (int64_t first = 0; first < args.n; first += most) {
+    PagedStoreArgs a = args;
+    a.n = std::min(most, args.n - first);
+    a.k = static_cast<const char*>(args.k) + first * row_bytes;
+    a.v = static_cast<const char*>(args.v) + first * row_bytes;
+    a.slots = args.slots + first;
+    const int64_t blocks = ((a.n << a.row_shift) + per - 1) / per;
+    paged_store_kernel<<<dim3((unsigned)blocks), dim3(kPageBlock), 0, stream>>>(a);
+  }
   prof_end(stream);
   return hipGetLastError();
 }
 
-hipError_t launch_norm_rope(const NormRopeArgs& args, hipStream_t stream) {
-  NormRopeArgs a = args;
-  if (a.T == 0) return hipSuccess;
-  // Few tokens share their heads out over several waves, up to about eight waves per compute unit in all.
-  const int row_lanes = a.D * (a.dtype ? 2 : 4) / 16, heads = a.Hq + 2 * a.Hkv;
-  const int steps = (heads * row_lanes + 63) / 64;  // steps of a wave that takes all heads
-  const int64_t want = (2048 + a.T - 1) / a.T;
-  a.parts = want < steps ? (int)want : steps;
+namespace {
+void launch_norm_rope_part(const NormRopeArgs& a, hipStream_t stream) {
   const int64_t waves = (int64_t)a.T * a.parts;
   const dim3 grid((unsigned)((waves + kWavesPerBlock - 1) / kWavesPerBlock)), block(kPageBlock);
-  prof_begin("norm_rope_store", stream);
   if (a.dtype) {
     if (a.D == 128) norm_rope_kernel<__bf16, 128><<<grid, block, 0, stream>>>(a);
     else norm_rope_kernel<__bf16, 64><<<grid, block, 0, stream>>>(a);
   } else {
     if (a.D == 128) norm_rope_kernel<float, 128><<<grid, block, 0, stream>>>(a);
     else norm_rope_kernel<float, 64><<<grid, block, 0, stream>>>(a);
+  }
+}
+}  // namespace
+
+hipError_t launch_norm_rope(const NormRopeArgs& args, hipStream_t stream) {
+  if (args.T == 0) return hipSuccess;
+  // Few tokens share their heads out over several waves, up to about eight waves per compute unit in all.
+  const int eb = args.dtype ? 2 : 4, row_lanes = args.D * eb / 16, heads = args.Hq + 2 * args.Hkv;
+  const int steps = (heads * row_lanes + 63) / 64;  // steps of a wave that takes all heads
+  const int64_t want = (2048 + (int64_t)args.T - 1) / args.T;
+  const int64_t most = kMaxBlocks * kWavesPerBlock;  // tokens of a launch: beyond 2048 a token is a wave's
+  prof_begin("norm_rope_store", stream);
+  for (int64_t first = 0; first < args.T; first += most) {
+    NormRopeArgs a = args;
+    a.parts = want < steps ? (int)want : steps;
+    a.T = (int)std::min(most, args.T - first);
+    if (a.Hq) {
+      a.q = static_cast<const char*>(args.q) + first * args.q_stride;
+      a.q_out = static_cast<char*>(args.q_out) + first * args.Hq * args.D * eb;
+    }
+    a.k = static_cast<const char*>(args.k) + first * args.k_stride;
+    a.v = static_cast<const char*>(args.v) + first * args.v_stride;
+    a.positions = args.positions + first;
+    a.slots = args.slots + first * args.Hkv;
+    launch_norm_rope_part(a, stream);
   }
   prof_end(stream);
   return hipGetLastError();

@@ -917,3 +917,27 @@ def test_norm_rope_angles(first, inter):
         tol = 2.0 ** -24 * want.abs() + 2 * math.pi * 2.0 ** -31
         err = (got - want).abs()
         assert (err <= tol).all(), float((err / tol).max())
+
+
+def test_norm_rope_of_more_tokens_than_a_launch_holds():
+    """2^26 + 37 tokens, a wave each, are more threads than one launch takes; tokens around each power of two from 2^24
+    on are compared, and the slots of the others are -1."""
+    _say("norm_rope of 2^26 + 37 tokens")
+    T, d = 2**26 + 37, 64
+    g = torch.Generator(device=DEV).manual_seed(4)
+    k = torch.zeros(T, 1, d, device=DEV, dtype=BF)
+    pos = torch.zeros(T, device=DEV, dtype=torch.int32)
+    slots = torch.full((T, 1), -1, device=DEV, dtype=torch.int32)
+    some = torch.tensor([0, *(2**i + j for i in (24, 25, 26) for j in (-1, 0, 1)), T - 1], device=DEV)
+    k[some] = torch.randn(len(some), 1, d, generator=g, device=DEV).to(BF)
+    pos[some] = (some % 100003).to(torch.int32)
+    slots[some, 0] = torch.arange(len(some), device=DEV, dtype=torch.int32)
+    inv = (1e4 ** (-torch.arange(0, d, 2, device=DEV) / d)).float()
+    kp, vp = (torch.zeros(1, 16, d, device=DEV, dtype=BF) for _ in range(2))
+    out = sg.norm_rope_store(k, k, k, pos, slots, kp, vp, inv_freq=inv)
+    small = torch.zeros_like(kp)
+    want = sg.norm_rope_store(k[some], k[some], k[some], pos[some], slots[some], small, vp.clone(), inv_freq=inv)
+    assert torch.equal(out[some], want) and torch.equal(kp, small)
+    assert torch.equal(vp[0, :len(some)], k[some, 0])
+    _check_rounded(want, _plain_rope(k[some], None, pos[some], inv, 0.0, False),
+                   2 ** 0.5 * k[some].double().abs().amax(-1, keepdim=True), 32)
