@@ -396,7 +396,9 @@ def _switched(fn, index, stream, args, kw):
         if stream is None:
             return fn(*args, **kw)
         if not hasattr(stream, "cuda_stream"):
-            stream = torch.cuda.ExternalStream(int(stream), device=torch.device("cuda", index))
+            # ExternalStream takes a handle of 0 for "none given" and makes a new stream
+            stream = (torch.cuda.ExternalStream(int(stream), device=torch.device("cuda", index)) if int(stream)
+                      else torch.cuda.default_stream(index))
         if stream.device.index != index:
             _refuse(f"the stream is on {stream.device}, the tensors on cuda:{index}")
         with torch.cuda.stream(stream):

@@ -941,3 +941,23 @@ def test_norm_rope_of_more_tokens_than_a_launch_holds():
     assert torch.equal(vp[0, :len(some)], k[some, 0])
     _check_rounded(want, _plain_rope(k[some], None, pos[some], inv, 0.0, False),
                    2 ** 0.5 * k[some].double().abs().amax(-1, keepdim=True), 32)
+
+
+def test_the_default_streams_handle():
+    """stream=0 is the default stream: the call comes after what was sent there before, and before what comes next."""
+    _say("stream 0")
+    c = Case([40, 1], [500, 40, 300, 77], 14, 2, 128, 16, BF, seed=12)
+    want, want_lse = c.call()
+    q = c.q.clone()
+    ws = sg.alloc_workspace(sg.paged_attention_workspace_size(q, 2, 2, max_new=40), DEV)
+    out, lse = torch.zeros_like(want), torch.zeros_like(want_lse)
+    for _ in range(3):
+        c.q.zero_()
+        out.zero_()
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)  # about 10 ms, far longer than the call
+        c.q.copy_(q)
+        c.call(stream=0, out=out, lse=lse, workspace=ws)
+        got = out.clone()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(lse, want_lse)
