@@ -12,6 +12,9 @@ Entry points (same names as the C ABI without the ``sgdkv_`` prefix):
   decode_workspace_size, decode_attention                        (device)
   page_update, paged_store, norm_rope_store                      (device)
   paged_attention_workspace_size, paged_attention                (device)
+
+A stream is a torch.cuda.Stream or a raw handle; the calls over the paged cache mark their tensors as in use on the
+former, and with a raw handle the caller keeps them alive until the call is done.
 """
 from __future__ import annotations
 
@@ -390,12 +393,15 @@ def _raw_stream(index):
 def _switched(fn, index, stream, args, kw):
     """fn(*args, **kw) with GPU `index` current and `stream` (None: that GPU's current one) torch's current stream, so
     that what the call allocates belongs to the stream it is used on; the tensors it is given are marked as in use
-    there, so that the allocator does not hand their memory to other work before the call is done."""
+    there, so that the allocator does not hand their memory to other work before the call is done. For a raw handle
+    keeping them alive is the caller's: torch would use the mark, and so the handle, when a tensor is freed, and the
+    caller may have destroyed the stream by then."""
     import torch
     with torch.cuda.device(index):
         if stream is None:
             return fn(*args, **kw)
-        if not hasattr(stream, "cuda_stream"):
+        mark = hasattr(stream, "cuda_stream")
+        if not mark:
             # ExternalStream takes a handle of 0 for "none given" and makes a new stream
             stream = (torch.cuda.ExternalStream(int(stream), device=torch.device("cuda", index)) if int(stream)
                       else torch.cuda.default_stream(index))
@@ -403,9 +409,10 @@ def _switched(fn, index, stream, args, kw):
             _refuse(f"the stream is on {stream.device}, the tensors on cuda:{index}")
         with torch.cuda.stream(stream):
             result = fn(*args, **kw)
-        for t in (*args, *kw.values()):
-            if isinstance(t, torch.Tensor):
-                t.record_stream(stream)
+        if mark:
+            for t in (*args, *kw.values()):
+                if isinstance(t, torch.Tensor):
+                    t.record_stream(stream)
         return result
 
 

@@ -961,3 +961,20 @@ def test_the_default_streams_handle():
         got = out.clone()
         torch.cuda.synchronize()
         assert torch.equal(got, want) and torch.equal(lse, want_lse)
+
+
+def test_tensors_are_marked_on_torchs_streams_alone(monkeypatch):
+    """A mark outlives the call: torch uses its stream when the tensor is freed. So the tensors of a call are marked on
+    a torch.cuda.Stream, and not on a raw handle, whose stream may be gone by then."""
+    _say("marks")
+    c = Case([3], [40], 4, 1, 64, 16, BF)
+    side = torch.cuda.Stream()
+    ws = sg.alloc_workspace(sg.paged_attention_workspace_size(c.q, 1, 1, max_new=3), DEV)
+    side.wait_stream(torch.cuda.current_stream())
+    marked, mark = [], torch.Tensor.record_stream
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: (marked.append(t.data_ptr()), mark(t, s)) and None)
+    c.call(stream=side.cuda_stream, workspace=ws)
+    assert not marked
+    c.call(stream=side, workspace=ws)
+    assert {t.data_ptr() for t in (c.q, c.k_pages, c.v_pages, c.tables, c.rows, c.cu, ws)} == set(marked)
+    side.synchronize()
