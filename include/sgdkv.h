@@ -412,8 +412,8 @@ typedef struct sgdkv_page_desc {
  *        back on it below head, in (segment, position) order; then each segment
  *        takes its new pages from it, in that order.
  * head:  device [1] int32.
- * rows_out [B*Hkv], head_out [1]: rows and head afterwards; each may be the
- *        input itself.
+ * rows_out [B*Hkv], head_out [1]: rows and head afterwards; rows_out may be
+ *        rows itself and head_out head itself.
  * cu_out: device int32, the new rows before each sequence [B+1] (by_segment:
  *        before each segment [B*Hkv+1]): max(add, 0) summed up.
  * slots: by token [num_slots][Hkv] int32, row t for token t of the step
@@ -423,7 +423,7 @@ typedef struct sgdkv_page_desc {
  * status: device [1] int32, SGDKV_PAGES_*. Other than OK: tables, free_pages,
  *        rows and head keep their values (rows_out and head_out get the old
  *        ones), all slots are -1 and cu_out is all 0.
- * Only rows_out and head_out may overlap other arguments.
+ * Otherwise nothing that is written may overlap another argument.
  * Errors (nothing enqueued): sizes out of range; more than 4096 segments
  * (UNSUPPORTED); NULL or misaligned pointers (slots may be NULL with
  * num_slots 0); reserved not 0. */

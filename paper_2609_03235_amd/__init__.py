@@ -444,6 +444,12 @@ def _check_dense(t, name, shape, dtype):
         _refuse(f"{name} must be a dense {tuple(shape)} of {dtype}, not {tuple(t.shape)} of {t.dtype}")
 
 
+def _overlap(a, b) -> bool:
+    """Two contiguous tensors have bytes in common."""
+    a0, b0 = a.data_ptr(), b.data_ptr()
+    return a0 < b0 + b.numel() * b.element_size() and b0 < a0 + a.numel() * a.element_size()
+
+
 def page_pool(k_pages, v_pages) -> PagePool:
     """The descriptor of a pool k_pages, v_pages [num_pages, page_size, d]."""
     if k_pages.dim() != 3 or k_pages.shape != v_pages.shape or k_pages.dtype is not v_pages.dtype:
@@ -459,8 +465,8 @@ def page_update(rows, add, tables, free_pages, head, *, page_size: int, n_slots:
     """Pages and slots for the rows that segments gain or lose (sgdkv_page_update). rows [B * Hkv], tables
     [B * Hkv, max_pages] (updated in place), free_pages [n] (a stack, updated in place) and head [1] are int32;
     add is int32 [B], or [B * Hkv] with by_segment. Returns slots ([n_slots, Hkv] or [n_slots]), rows, head, cu,
-    status and the updated tables and free_pages. rows_out and head_out may be rows and head. Results that the
-    caller does not bring share one allocation."""
+    status and the updated tables and free_pages. rows_out may be rows and head_out head; no other two arguments that
+    share memory. Results that the caller does not bring share one allocation."""
     import torch
     index = _gpu_of(rows, add, tables, free_pages, head, rows_out, head_out, slots, cu, status)
     if rows.dim() != 1 or add.dim() != 1 or tables.dim() != 2 or free_pages.dim() != 1:
@@ -481,6 +487,12 @@ def page_update(rows, add, tables, free_pages, head, *, page_size: int, n_slots:
                           (slots, "slots", shape)):
         if t is not None:
             _check_int32(t, name, want)
+    for t, name, own in ((rows_out, "rows_out", rows), (head_out, "head_out", head)):
+        if t is not None and t.data_ptr() != own.data_ptr():
+            for other in (rows, add, tables, free_pages, head, slots, cu, status,
+                          head_out if name == "rows_out" else rows_out):
+                if other is not None and _overlap(t, other):
+                    _refuse(f"{name} overlaps another argument: it may only be the tensor that it replaces")
     handle = _raw_stream(index) if stream is None else None
     if handle is None:
         return _switched(page_update, index, stream, (rows, add, tables, free_pages, head),

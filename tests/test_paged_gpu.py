@@ -978,3 +978,22 @@ def test_tensors_are_marked_on_torchs_streams_alone(monkeypatch):
     c.call(stream=side, workspace=ws)
     assert {t.data_ptr() for t in (c.q, c.k_pages, c.v_pages, c.tables, c.rows, c.cu, ws)} == set(marked)
     side.synchronize()
+
+
+def test_page_update_refuses_results_over_other_arguments():
+    """rows_out over add, or over a part of rows, would be written by one workgroup while another still reads it."""
+    _say("overlapping results")
+    pool = _i32([0] * 64)
+    rows, add, head = pool[:8], pool[16:24], pool[32:33]
+    tables, free = _i32([[0] * 4] * 8), _i32([1, 2, 3])
+    kw = dict(page_size=16, n_slots=4, by_segment=True)
+    cu, slots = _i32([0] * 9), _i32([0] * 4)
+    for bad in (dict(rows_out=add), dict(rows_out=pool[4:12]), dict(head_out=rows[:1]), dict(head_out=free[2:3]),
+                dict(rows_out=pool[40:48], head_out=pool[44:45]), dict(rows_out=cu[:8], cu=cu),
+                dict(head_out=slots[:1], slots=slots), dict(rows_out=tables.view(-1)[8:16])):
+        with pytest.raises(sg.SgdkvError) as e:
+            sg.page_update(rows, add, tables, free, head, **kw, **bad)
+        assert e.value.status == sg.ERR_INVALID_ARG and "overlaps" in e.value.message
+    for good in (dict(rows_out=rows, head_out=head), dict(rows_out=pool[40:48], head_out=pool[48:49])):
+        up = sg.page_update(rows, add, tables, free, head, **kw, **good)
+        assert int(up["status"]) == 0 and not up["rows"].any()
