@@ -482,7 +482,7 @@ typedef struct sgdkv_paged_desc {
   int32_t max_new;       /* >= 1: at least the longest sequence's new tokens */
   int32_t max_pages;     /* columns of tables, >= 1; max_pages * page_size <= 2^31 - 2049 */
   int32_t causal;        /* 1: a token sees the rows up to its own; 0: all of its segment's */
-  float scale;           /* logit scale; 0 selects 1/sqrt(head_dim) */
+  float scale;           /* logit scale, up to 2.35e38 in size; 0 selects 1/sqrt(head_dim) */
 } sgdkv_paged_desc;
 
 /* Bytes of device workspace for sgdkv_paged_attention. Depends on the pool's

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -108,7 +109,6 @@ sgdkv_status plan_paged(const sgdkv_page_pool* pool, const sgdkv_paged_desc* d, 
                 (long long)d->num_tokens);
   if (d->max_new < 1) return fail(SGDKV_ERR_INVALID_ARG, "max_new %d < 1", d->max_new);
   if (d->causal != 0 && d->causal != 1) return fail(SGDKV_ERR_INVALID_ARG, "causal %d is not 0 or 1", d->causal);
-  if (!std::isfinite(d->scale)) return fail(SGDKV_ERR_INVALID_ARG, "scale is not finite");
   a = sgdkv::PagedAttnArgs{};
   a.B = d->batch;
   a.Hq = d->num_q_heads;
@@ -124,7 +124,10 @@ sgdkv_status plan_paged(const sgdkv_page_pool* pool, const sgdkv_paged_desc* d, 
   a.max_pages = d->max_pages;
   a.max_new = (int)std::min<int64_t>(d->max_new, std::max<int64_t>(d->num_tokens, 1));
   const double scale = d->scale == 0.f ? 1.0 / std::sqrt((double)a.D) : (double)d->scale;
-  a.c2 = (float)(scale * 1.4426950408889634074);
+  const double c2 = scale * 1.4426950408889634074;
+  if (!(std::fabs(c2) <= (double)FLT_MAX))
+    return fail(SGDKV_ERR_INVALID_ARG, "scale %g: scale * log2(e) is not finite in fp32", d->scale);
+  a.c2 = (float)c2;
   const sgdkv::PagedAttnShape shape = sgdkv::paged_attn_shape(a.dtype, G, a.max_new);
   a.tile_rows = shape.rows;
   a.key_tile = shape.key_tile;

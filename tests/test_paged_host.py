@@ -126,6 +126,16 @@ def test_paged_attention_sizes(kw, status):
     assert _status("sgdkv_paged_attention", _pool(), _attn_desc(**kw), A, A, A, A, A, A, A, 1 << 40, None) == status
 
 
+@pytest.mark.parametrize("scale", [3e38, -3e38, 2.4e38, float("-inf")])
+def test_paged_attention_scales_that_the_kernels_cannot_hold(scale):
+    """The kernels take scale * log2(e) in fp32: past 2.358e38 that is infinite, and every logit of 0 would be NaN."""
+    n = ctypes.c_size_t(0)
+    desc = _attn_desc(scale=scale)
+    assert _status("sgdkv_paged_attention_workspace_size", _pool(), desc, ctypes.byref(n)) == sg.ERR_INVALID_ARG
+    assert _status("sgdkv_paged_attention", _pool(), desc, *[A] * 7, 1 << 40, None) == sg.ERR_INVALID_ARG
+    assert _status("sgdkv_paged_attention_workspace_size", _pool(), _attn_desc(scale=2.3e38), ctypes.byref(n)) == sg.OK
+
+
 def test_paged_attention_pointers_and_workspace():
     for i in range(6):
         args = [A] * 6
