@@ -997,3 +997,128 @@ def test_page_update_refuses_results_over_other_arguments():
     for good in (dict(rows_out=rows, head_out=head), dict(rows_out=pool[40:48], head_out=pool[48:49])):
         up = sg.page_update(rows, add, tables, free, head, **kw, **good)
         assert int(up["status"]) == 0 and not up["rows"].any()
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("hq,new,rows,dtype", [
+    (2, [5, 1], [70, 200, 33, 1000], BF),        # 5 query rows of 16
+    (6, [6, 3], [9000, 61, 33, 1000], BF),       # 18 of 32, a segment cut into many parts
+    (6, [16, 1], [130, 12000, 33, 40], BF),      # 48
+    (8, [40, 33], [70, 9000, 33, 1000], BF),     # 128
+    (2, [13, 1], [9000, 200, 33, 90], F32),      # 13 of 16
+    (4, [15, 15], [70, 7000, 15, 16], F32),      # 30 of 32
+    (8, [40, 33], [7000, 200, 40, 1000], F32),   # 128
+])
+@pytest.mark.parametrize("d", [64, 128])
+def test_paged_attention_values_alone_that_are_not_finite(hq, new, rows, dtype, d, bad):
+    """Values that are not finite, keys all finite: not finite are the outputs of exactly their columns of the tokens
+    that see their rows; every other output, and every lse, is that of the clean run bit for bit. The rows are those of
+    the last two tokens, so that some of a tile's rows see them and others do not; the columns are an odd and an even
+    one (both halves of a word), the first and the last."""
+    _say(f"values {bad} {dtype} {new} over {rows} d {d}")
+    c = Case(new, rows, hq, 2, d, 16, dtype, seed=13)
+    n, G = new[0], hq // 2
+    for od in (BF, F32):
+        clean, clean_lse = c.call(out_dtype=od)
+        odd = torch.zeros(clean.shape, dtype=torch.bool, device=DEV)
+        saved = c.v_pages.clone()
+        for s, token, cols in ((0, n - 2, (5, 8)), (0, n - 1, (0, d - 1)), (1, n - 1, (6, 7)), (1, n - 2, (d - 2,))):
+            row = rows[s] - n + token
+            page = int(c.tables[s, row // 16])
+            for col in cols:
+                c.v_pages[page, row % 16, col] = bad
+                odd[token:n, s * G:(s + 1) * G, col] = True
+        out, lse = c.call(out_dtype=od)
+        assert torch.equal(lse, clean_lse)
+        assert not torch.isfinite(out[odd]).any() and torch.equal(out[~odd], clean[~odd])
+        c.v_pages = saved
+
+
+@pytest.mark.parametrize("hq,new,max_new,dtype", [(4, 5, 2, BF), (6, 16, 3, BF), (8, 100, 37, BF), (8, 100, 5, BF),
+                                                  (4, 16, 7, F32), (4, 90, 33, F32)])
+def test_paged_attention_of_the_first_max_new_tokens(hq, new, max_new, dtype):
+    """A chunk longer than max_new: its first max_new tokens come out as they do with the rest, within the tolerance
+    of the 64-bit values, whichever kernel; the others' out and lse are left alone."""
+    _say(f"max_new {max_new} of {new}")
+    c = Case([new], [64 + new, 700], hq, 2, 64, 16, dtype, seed=8)
+    for od in (BF, F32):
+        out = torch.full((c.T, hq, 64), 3.0, device=DEV, dtype=od)
+        lse = torch.full((c.T, hq), 3.0, device=DEV)
+        c.call(max_new=max_new, out=out, lse=lse, out_dtype=od)
+        assert (out[max_new:] == 3.0).all() and (lse[max_new:] == 3.0).all()
+        c.check(out, lse, only=torch.arange(c.T, device=DEV) < max_new)
+
+
+def _in_place_steps(rows, steps, hkv, page, by_segment, width):
+    """Calls in a row with rows_out = rows and head_out = head, each against lists of integers."""
+    n_pages = sum(-(-r // page) for r in rows) + 3 + sum(sum(-(-max(a, 0) // page) + 1 for a in add) * (
+        1 if by_segment else hkv) for add in steps)
+    tables, free, head = _start(rows, page, width, n_pages, 11)
+    d = dict(rows=_i32(rows), tables=_i32(tables), free=_i32(free), head=_i32([head]))
+    state = (rows, tables, free, head)
+    for add in steps:
+        n_slots = sum(max(a, 0) for a in add) + 2
+        want = _plain_update(*state[:1], add, *state[1:], page, n_slots, hkv, by_segment)
+        assert want["status"] == 0
+        got = sg.page_update(d["rows"], _i32(add), d["tables"], d["free"], d["head"], page_size=page, n_slots=n_slots,
+                             by_segment=by_segment, rows_out=d["rows"], head_out=d["head"])
+        assert got["rows"] is d["rows"] and got["head"] is d["head"]
+        _check_update(got, want)
+        state = (want["rows"], want["tables"], want["free_pages"], want["head"])
+
+
+def test_page_update_by_segment_in_place():
+    """The rows of a batch of compressed prompts in place, over many workgroups; then some given back, some taken."""
+    _say("page_update by segment in place")
+    S = 64
+    first = [(i * 977) % 5000 + 17 for i in range(S)]
+    second = [-((i * 331) % 900) if i % 3 else (i * 977) % 3000 for i in range(S)]
+    _in_place_steps([0] * S, [first, second, [-10000] * S], 1, 16, True, 600)
+
+
+def test_page_update_of_a_token_each_in_place_with_wide_tables():
+    """One token for 512 segments whose tables have 1200 columns: the tables alone make it many workgroups."""
+    _say("page_update 512 x 1200 in place")
+    rows = [(i * 53) % 3000 for i in range(512)]
+    _in_place_steps(rows, [[1] * 64, [1 if i % 5 else -40 for i in range(64)]], 8, 16, False, 1200)
+
+
+@pytest.mark.parametrize("chunks", [[5, 1, 1], [70, 3, 40]])
+def test_steps_against_64_bits(chunks):
+    """Steps of page_update, norm_rope_store and paged_attention, each against 64 bits: the stored keys against the
+    whole sequence's norm and rotation, the outputs against the softmax over the rows stored so far."""
+    _say(f"steps {chunks} in 64 bits")
+    B, hq, hkv, d, page = 3, 8, 2, 64, 16
+    g = torch.Generator(device=DEV).manual_seed(7)
+    n = sum(chunks)
+    q, k, v = (torch.randn(B, n, h, d, generator=g, device=DEV) for h in (hq, hkv, hkv))
+    inv = (1e4 ** (-torch.arange(0, d, 2, device=DEV) / d)).float()
+    wts = [1 + 0.1 * torch.randn(d, generator=g, device=DEV) for _ in range(2)]
+    pos = torch.arange(n, device=DEV, dtype=torch.int32)
+    wq, wk = (torch.stack([_plain_rope(x[b], w, pos, inv, 1e-6, False) for b in range(B)])
+              for x, w in zip((q, k), wts))
+    big = lambda w: 2 ** 0.5 * w.abs().amax(-1, keepdim=True)
+    st = _serve_state(B, hkv, page, 16, 100, d, F32)
+    done = 0
+    for m in chunks:
+        up = sg.page_update(st["rows"], _i32([m] * B), st["tables"], st["free"], st["head"], page_size=page,
+                            n_slots=B * m, rows_out=st["rows"], head_out=st["head"])
+        cut = lambda x: x[:, done:done + m].reshape(B * m, -1, d)
+        qr = sg.norm_rope_store(cut(q), cut(k), cut(v), pos[done:done + m].repeat(B), up["slots"], st["k"], st["v"],
+                                inv_freq=inv, q_weight=wts[0], k_weight=wts[1])
+        out, lse = sg.paged_attention(qr, st["k"], st["v"], st["tables"], up["rows"], up["cu"], hkv, max_new=m)
+        done += m
+        _check_rounded(qr.view(B, m, hq, d), wq[:, done - m:done], big(wq[:, done - m:done]), 32)
+        # the attention's reference takes the rotated queries and the rows as they were stored
+        c = Case.__new__(Case)
+        c.new, c.rows_host, c.hq, c.hkv, c.d, c.T = [m] * B, [done] * (B * hkv), hq, hkv, d, B * m
+        c.q, c.k, c.v = qr, [], []
+        for s in range(B * hkv):
+            at = torch.arange(done, device=DEV)
+            slot = st["tables"][s].long()[at // page] * page + at % page
+            c.k.append(st["k"].view(-1, d)[slot])
+            c.v.append(st["v"].view(-1, d)[slot])
+            b, h = divmod(s, hkv)
+            _check_rounded(c.k[-1], wk[b, :done, h], big(wk[b, :done, h]), 32)
+            assert torch.equal(c.v[-1], v[b, :done, h])
+        c.check(out, lse)
