@@ -245,7 +245,8 @@ __device__ __forceinline__ u32x4 group_words(const PagedAttnArgs& a, const void*
 
 // 64 x 16 bytes from a buffer into LDS at lds + 16 * lane; out-of-range lanes write zeros. The compiler does not
 // see that these loads are under way: wait_loads() before the data is read (and a barrier, if by other waves).
-// There is no destination register that could be reused too early; m0 is no allocatable register.
+// There is no destination register that could be reused too early. m0 is a reserved register, which cannot be named as
+// clobbered; nothing else in these kernels uses it, and each load sets it for itself.
 __device__ __forceinline__ uint32_t lds_address(const char* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
 }

@@ -274,8 +274,8 @@ __global__ __launch_bounds__(kPageBlock) void paged_store_kernel(PagedStoreArgs 
 // sin and cos of position * freq. In turns the angle is position * freq / (2 pi): both products are carried with
 // their rounding errors, and the nearest quarter turn is taken off in 64 bits, which leaves an angle x in
 // [-pi/4, pi/4] for the Taylor sums (the first terms left out are below 2e-9 and 2e-10 of a radian). So the angle of a
-// position of 2^31 is as good as that of a small one. The sums are in 64 bits too, and what they give is rounded once: an
-// x rounded to 32 bits alone is off by up to 2^-25, 2^-27.7 turns. (A lane does this once per token, for all heads.)
+// position of 2^31 is as good as that of a small one. The sums are in 64 bits too, and what they give is rounded once:
+// an x rounded to 32 bits alone is off by up to 2^-25, 2^-27.7 turns. (A lane does this once per token, for all heads.)
 __device__ __forceinline__ void sincos_at(double position, double freq, float& sin_t, float& cos_t) {
   constexpr double kHi = 0.15915494309189535, kLo = -9.839338337591243e-18;  // 1 / (2 pi)
   const double a0 = position * freq, a1 = fma(position, freq, -a0);

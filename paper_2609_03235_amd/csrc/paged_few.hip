@@ -6,7 +6,8 @@
 // layout, values straight into LDS that only this wave uses (two buffers), for the transposing read. The next
 // step's loads start as soon as the step's keys are used up, so that all but the logits of a step runs beside
 // them: 8 waves of a compute unit have 128 KB under way. 32 tokens over 4 x 32K rows each (28 / 4 heads of 128, bf16)
-// take 335 us, 6.4 TB/s; 1 to 6 tokens of 16 sequences over 8 x 20K rows (64 / 8 heads, fp32 out) 226, 5.7 TB/s.
+// take 335 us, 6.4 TB/s; 1 to 6 tokens of 16 sequences over 8 x 20K rows (64 / 8 heads, fp32 out) 226 to 236, 5.6 to
+// 5.8 TB/s; fp32, one token of 8 sequences over 4 x 20K rows 117, 5.7 TB/s.
 #include <algorithm>
 
 #include "paged_attention.h"
@@ -300,7 +301,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
 //   Few parts: a group takes a row of its own and its parts in batches, each all under way at once.
 //   Many (a long segment and few others): a workgroup takes rows y, y + gridDim.y, ...; its groups take a row's
 //     parts in turn with a running maximum and are then joined in order.
-// Whichever has fewer rounds of reads. (21 tokens over 57K rows of one head, 443 parts: 142 us and 39. 300 tokens
+// Whichever has fewer rounds of reads. (21 tokens over 57K rows of one head, 443 parts: 142 us and 34. 300 tokens
 // over 900 rows of four heads, 8 or 9 parts and two rows a workgroup: 32 us and 34.)
 template <int D>
 __global__ __launch_bounds__(kAttnBlock) void paged_merge_kernel(PagedAttnArgs a) {

@@ -1,5 +1,5 @@
 // Internal interface between the C-ABI layer of the paged cache (paged_host.cpp) and its HIP
-// kernels (paged_cache.hip, paged_attention.hip). Not installed; not part of the ABI.
+// kernels (paged_cache.hip, paged_few.hip, paged_many.hip). Not installed; not part of the ABI.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -1,16 +1,17 @@
 // Paged attention for many query rows per KV head (chunks of new tokens). See paged_attention.h.
 //
-// A workgroup holds 128 query rows, 32 per wave, and walks the keys of its piece of the line in tiles that
-// all four waves share through LDS: two buffers, one barrier per tile, and the next tile on its way from memory
-// straight into LDS while one is computed (no registers, no LDS writes). A query tile's first keys and its queries
-// are under way while the results of the one before are written, whole lines at a time (312 prompts of 64 tokens,
-// 64 / 8 heads: 247 us with one after the other, 16 bytes of a row at a time; 206 so). Products are 32x32 MFMAs. Every
-// row keeps a reference for its exponentials that only moves when a tile's sum shows that it fell too far behind,
-// so a logit costs one fma, one exp2 and one add. 32 query rows a wave and two workgroups a compute unit are what the
+// A workgroup holds 128 query rows, 32 per wave, and walks the keys of its piece of the line in tiles that all four
+// waves share through LDS: two buffers, one barrier per tile, and the next tile on its way from memory straight into
+// LDS while one is computed (no registers, no LDS writes). A query tile's first keys and its queries are under way
+// while the results of the one before are written, whole lines at a time (312 prompts of 64 tokens, 64 / 8 heads: 247
+// us with one after the other, 16 bytes of a row at a time; 206 with this, 194 now). Products are 32x32 MFMAs. Every
+// row keeps a reference for its exponentials that only moves when a tile's sum shows that it fell too far behind, so a
+// logit costs one fma, one exp2 and one add. 32 query rows a wave and two workgroups a compute unit are what the
 // registers (o takes 64, the queries 32, a tile's logits 32) and LDS (64 KB each) hold; the second workgroup runs
-// while the first waits. Bound by the matrix unit and the vector unit one after the other, at the socket's power:
-// two sequences of 8192 tokens over 16K rows, 64 / 8 heads of 128, bf16: 10.4 ms, 1.00 PFLOP/s, at 1.7 to 1.8 GHz
-// (8.5 ms on zeros).
+// while the first waits. Bound by the matrix unit and the vector unit, 29 % of the matrix unit's cycles at once and
+// the others one after the other, at the clock that the socket's power leaves (1.64 GHz; 2.36 on zeros): two sequences
+// of 8192 tokens over 16K rows, 64 / 8 heads of 128, bf16: 10.3 to 10.7 ms, 0.97 to 1.01 PFLOP/s (0.93 on the slowest
+// card seen; 8.5 to 9.0 ms on zeros).
 #include <type_traits>
 
 #include "paged_attention.h"
@@ -47,11 +48,11 @@ constexpr int kUnshared = sizeof(T) == 2 ? 512 : 128;
 // Reference kept while a tile's sum of exponentials stays below this.
 constexpr float kFar = 1024.f;
 
-// A tile's probabilities of one lane, as the operand of the product with the values. bf16 output of bf16 inputs: rounded
-// to bf16, half a step of 2^-8 each. The errors of the keys average out: 1 x 1999 tokens over 8K rows, 28 / 4 heads, are
-// off by 2.00e-3 of the output (rms), of which its own rounding to bf16 makes 1.66e-3. FINE (fp32 output) keeps all 24
-// bits in three terms, 6.6e-7, at three times these products: 445 us for 268, and 18.0 ms for 10.5 with two sequences of
-// 8192 tokens over 16K rows, 64 / 8 heads. A caller who wants them asks for fp32 output.
+// A tile's probabilities of one lane, as the operand of the product with the values. bf16 output of bf16 inputs:
+// rounded to bf16, each off by up to 2^-8 of itself. The keys' errors average out: 1 x 1999 tokens over 8K rows, 28 / 4
+// heads, are off by 2.00e-3 of the output (rms), of which its own rounding to bf16 makes 1.66e-3. FINE (fp32 output)
+// keeps all 24 bits in three terms, 6.6e-7, at three times these products: 445 us for 268, and 18.0 ms for 10.5 with
+// two sequences of 8192 tokens over 16K rows, 64 / 8 heads. A caller who wants them asks for fp32 output.
 template <typename T, bool FINE, int NK>
 struct Probs;
 template <int NK>
@@ -285,7 +286,8 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
       };
       if constexpr (EB == 2) {
         // Four pieces are read while the four before are multiplied. (Left alone, the compiler reads each just before
-        // its product and waits: with the same for the values, 8192 tokens over 16K rows 10.8 ms, 10.4 so.)
+        // its product and waits: with the same for the values, 8192 tokens over 16K rows took 10.8 ms, and 10.4 so, in
+        // turn on one card.)
         u32x4 kf[2][4];
         auto read = [&](int g) {
 #pragma unroll

@@ -891,8 +891,8 @@ def test_norm_rope_columns_that_do_not_turn(dtype, d, rot, inter):
 @pytest.mark.parametrize("inter", [False, True])
 @pytest.mark.parametrize("first", [0, 131072, 2**31 - 3000, -3000])
 def test_norm_rope_angles(first, inter):
-    """Pairs (1, 0) turn into (cos t, sin t) with no rounding of their own, so what comes out is the cosine and sine: off
-    by an angle of 2^-31 turns at most (their slope is 1 at most) and by their rounding to fp32, half a step of the
+    """Pairs (1, 0) turn into (cos t, sin t) with no rounding of their own, so what comes out is the cosine and sine:
+    off by an angle of 2^-31 turns at most (their slope is 1 at most) and by their rounding to fp32, half a step of the
     value. The reference takes the exact product of position and frequency in 80 bits and its sine in 64."""
     _say(f"angles from {first}")
     np = pytest.importorskip("numpy")
