@@ -6,7 +6,7 @@ Tolerances of the attention, derived before the first run. With y the logits, A 
     delta = 2^-21 scale max_r sum_d |q_d k_d| (DELTA below also holds the rounding of the exponent's
     fp32 argument and of exp2, 2^-22 (1 + |y|)); a weight is then off by 2 delta relative;
   * probabilities are rounded to bf16 (half a step: 2^-8 relative) for bf16 output of bf16 inputs, or keep
-    their fp32 bits (2^-24);
+    their fp32 bits (2^-24), as they do for bf16 output too up to 48 query rows per KV head;
   * an fp32 accumulator takes one rounding per 16 keys and one per merged part: (rows / 4 + 64) 2^-24 A
     covers them at four roundings each;
   * the output is rounded to its type: half a step of |o|.
