@@ -519,6 +519,72 @@ sgdkv_status sgdkv_paged_attention(const sgdkv_page_pool* pool, const sgdkv_page
                                    float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------ */
+/* The paged cache in 8 bits (device).                                 */
+
+/* The same pages with rows of half the bytes (a quarter of fp32's): a row is
+ * head_dim e4m3 numbers (4 exponent bits with bias 7, 3 of mantissa, the
+ * largest 448; 0x7F and 0xFF are NaN) and one e8m0 code c, and holds the
+ * numbers times 2^(c - 127). Keys and values of every token and KV head have
+ * a code each, so a row does not depend on those beside it, nor on the calls
+ * that brought them. A step is sgdkv_page_update, whose tables and slots serve
+ * this pool too, sgdkv_norm_rope_store_fp8 and sgdkv_paged_attention_fp8;
+ * sgdkv_paged_store_fp8 brings the rows of a compressed cache.
+ *
+ * A stored row's power 2^e is the smallest with which its largest finite value
+ * is at most 448 2^e, and at least 2^-110 (a row of zeros has that one); a value
+ * x becomes the e4m3 number nearest to x / 2^e, ties to even: off by 2^-4 of x
+ * at most, or by 2^(e - 10) where that is more. An infinity or a NaN becomes
+ * NaN and the others keep their values. */
+typedef struct sgdkv_page_pool_fp8 {
+  void* k_pages;      /* device [num_pages][page_size][head_dim] e4m3 */
+  void* v_pages;      /* the same shape */
+  void* k_scales;     /* device [num_pages][page_size] e8m0 */
+  void* v_scales;     /* the same shape */
+  int64_t num_pages;  /* >= 1; num_pages * page_size <= 2^31 - 1 */
+  int32_t page_size;  /* a power of two, 16 to 1024 */
+  int32_t head_dim;   /* d: 64 or 128 */
+  int32_t row_dtype;  /* of the rows, queries and weights beside it: SGDKV_DTYPE_F32 or SGDKV_DTYPE_BF16 */
+  int32_t reserved;   /* must be 0 */
+} sgdkv_page_pool_fp8;
+
+/* Rounds row i of k_rows and v_rows (device [n][d] row_dtype) to 8 bits and
+ * writes it to slot slots[i] (device [n] int32). A slot outside the pool, -1
+ * say, keeps nothing. A slot given twice ends up with either row, or with
+ * pieces of both.
+ * Errors (nothing enqueued): a bad pool; n < 0 or n*d beyond 2^40; NULL or
+ * misaligned pointers (with n > 0). */
+sgdkv_status sgdkv_paged_store_fp8(const sgdkv_page_pool_fp8* pool, const void* k_rows, const void* v_rows,
+                                   const int32_t* slots, int64_t n, void* stream);
+
+/* sgdkv_norm_rope_store into such a pool. Keys and values are rounded to 8
+ * bits from the fp32 values of norm and rotation; queries are rounded to
+ * row_dtype. rope_factor multiplies the rotated elements of queries and keys,
+ * the factor that some scalings of positions for long contexts bring (1: none):
+ *   (a, b) <- f (a cos t - b sin t, b cos t + a sin t)
+ * Errors: those of sgdkv_norm_rope_store; rope_factor not finite. */
+sgdkv_status sgdkv_norm_rope_store_fp8(const sgdkv_page_pool_fp8* pool, const sgdkv_norm_rope_desc* desc,
+                                       float rope_factor, const void* q, const void* k, const void* v,
+                                       const int32_t* positions, const int32_t* slots, const float* inv_freq,
+                                       const void* q_weight, const void* k_weight, void* q_out, void* stream);
+
+/* Bytes of device workspace for sgdkv_paged_attention_fp8, as
+ * sgdkv_paged_attention_workspace_size (of the pool, row_dtype and head_dim
+ * are looked at). */
+sgdkv_status sgdkv_paged_attention_fp8_workspace_size(const sgdkv_page_pool_fp8* pool, const sgdkv_paged_desc* desc,
+                                                      size_t* bytes);
+
+/* sgdkv_paged_attention over such a pool: q is row_dtype, and the rows' values
+ * enter the formula as they are held, none rounded again. Rows past a segment's
+ * last one and the codes of those are not read into a result, whatever they
+ * hold. Probabilities as there; a value that is not finite makes the outputs of
+ * its column, of the tokens that see its row, not finite, and no others; a row
+ * of code 255 (e8m0's NaN) all columns'.
+ * Errors (nothing enqueued): those of sgdkv_paged_attention. */
+sgdkv_status sgdkv_paged_attention_fp8(const sgdkv_page_pool_fp8* pool, const sgdkv_paged_desc* desc, const void* q,
+                                       const int32_t* tables, const int32_t* rows, const int32_t* cu_new, void* out,
+                                       float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------ */
 /* Kernel timing for benchmarks (not part of the method).             */
 
 /* While enabled (on != 0), every kernel the library launches is bracketed by

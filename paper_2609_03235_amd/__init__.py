@@ -12,6 +12,8 @@ Entry points (same names as the C ABI without the ``sgdkv_`` prefix):
   decode_workspace_size, decode_attention                        (device)
   page_update, paged_store, norm_rope_store                      (device)
   paged_attention_workspace_size, paged_attention                (device)
+  paged_store_fp8, norm_rope_store_fp8                           (device)
+  paged_attention_fp8_workspace_size, paged_attention_fp8        (device)
 
 A stream is a torch.cuda.Stream or a raw handle; the calls over the paged cache mark their tensors as in use on the
 former, and with a raw handle the caller keeps them alive until the call is done.
@@ -36,6 +38,8 @@ SYMBOLS = ("sgdkv_last_error", "sgdkv_version", "sgdkv_reduce_query_head_scores"
            "sgdkv_decode_workspace_size", "sgdkv_decode_attention", "sgdkv_decode_workspace_size_ex",
            "sgdkv_decode_attention_ex", "sgdkv_decode_attention_noalloc", "sgdkv_append_kv", "sgdkv_page_update",
            "sgdkv_paged_store", "sgdkv_norm_rope_store", "sgdkv_paged_attention_workspace_size",
+           "sgdkv_paged_store_fp8", "sgdkv_norm_rope_store_fp8", "sgdkv_paged_attention_fp8_workspace_size",
+           "sgdkv_paged_attention_fp8",
            "sgdkv_paged_attention", "sgdkv_profile_enable",
            "sgdkv_profile_reset", "sgdkv_profile_read")
 
@@ -106,6 +110,10 @@ def load_library():
         "sgdkv_norm_rope_store": [P, P, P, P, P, P, P, P, P, P, P, P],
         "sgdkv_paged_attention_workspace_size": [P, P, P],
         "sgdkv_paged_attention": [P, P, P, P, P, P, P, P, P, ctypes.c_size_t, P],
+        "sgdkv_paged_store_fp8": [P, P, P, P, i64, P],
+        "sgdkv_norm_rope_store_fp8": [P, P, ctypes.c_float, P, P, P, P, P, P, P, P, P, P],
+        "sgdkv_paged_attention_fp8_workspace_size": [P, P, P],
+        "sgdkv_paged_attention_fp8": [P, P, P, P, P, P, P, P, P, ctypes.c_size_t, P],
         "sgdkv_profile_enable": [i32],
         "sgdkv_profile_reset": [],
         "sgdkv_profile_read": [i32, P, P, P, P],
@@ -358,6 +366,12 @@ class PagePool(ctypes.Structure):
                 ("reserved", ctypes.c_int32)]
 
 
+class PagePoolFp8(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("num_pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("row_dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 class PageDesc(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("max_pages", ctypes.c_int32), ("by_segment", ctypes.c_int32), ("reserved", ctypes.c_int32),
@@ -545,23 +559,16 @@ def _token_stride(t, name, d):
     return t.stride(0) if T > 1 else heads * d
 
 
-def norm_rope_store(q, k, v, positions, slots, k_pages, v_pages, *, inv_freq=None, q_weight=None, k_weight=None,
-                    eps: float = 1e-6, interleaved: bool = False, q_out=None, stream=None):
-    """New tokens' heads in one pass (sgdkv_norm_rope_store): queries [T, Hq, d] and keys [T, Hkv, d] normalised per
-    head (with q_weight, k_weight [d]) and rotated by positions (int32 [T]) with inv_freq (fp32 [rot_dim / 2];
-    None: no rotation), keys and values stored to slots (int32 [T, Hkv], -1 for none). q, k and v may be parts of
-    one projection's output. q may be None. Returns q_out [T, Hq, d]."""
+def _norm_rope_desc(q, k, v, positions, slots, d, dt, inv_freq, q_weight, k_weight, eps, interleaved,
+                    q_out) -> NormRopeDesc:
     import torch
-    index = _gpu_of(k_pages, v_pages, q, k, v, positions, slots, inv_freq, q_weight, k_weight, q_out)
-    pool = page_pool(k_pages, v_pages)
-    dt, d = k_pages.dtype, k_pages.shape[2]
     if k.dim() != 3 or v.shape != k.shape or k.shape[2] != d or k.dtype is not dt or v.dtype is not dt:
-        _refuse("k and v must be [T, Hkv, d] of the pool's dtype")
+        _refuse(f"k and v must be [T, Hkv, {d}] of {dt}")
     T, Hkv, _ = k.shape
     Hq = q_stride = 0
     if q is not None:
         if q.dim() != 3 or q.shape[0] != T or q.shape[2] != d or q.dtype is not dt:
-            _refuse("q must be [T, Hq, d] of the pool's dtype")
+            _refuse(f"q must be [T, Hq, {d}] of {dt}")
         Hq = q.shape[1]
         q_stride = _token_stride(q, "q", d)
         if q_out is not None:
@@ -574,15 +581,29 @@ def norm_rope_store(q, k, v, positions, slots, k_pages, v_pages, *, inv_freq=Non
         _check_dense(inv_freq, "inv_freq", (inv_freq.numel(),), torch.float32)
     _check_int32(positions, "positions", (T,))
     _check_int32(slots, "slots", (T, Hkv))
-    desc = NormRopeDesc(T, Hq, Hkv, q_stride, _token_stride(k, "k", d), _token_stride(v, "v", d),
+    return NormRopeDesc(T, Hq, Hkv, q_stride, _token_stride(k, "k", d), _token_stride(v, "v", d),
                         0 if inv_freq is None else 2 * inv_freq.shape[0], 1 if interleaved else 0, eps, 0)
+
+
+def norm_rope_store(q, k, v, positions, slots, k_pages, v_pages, *, inv_freq=None, q_weight=None, k_weight=None,
+                    eps: float = 1e-6, interleaved: bool = False, q_out=None, stream=None):
+    """New tokens' heads in one pass (sgdkv_norm_rope_store): queries [T, Hq, d] and keys [T, Hkv, d] normalised per
+    head (with q_weight, k_weight [d]) and rotated by positions (int32 [T]) with inv_freq (fp32 [rot_dim / 2];
+    None: no rotation), keys and values stored to slots (int32 [T, Hkv], -1 for none). q, k and v may be parts of
+    one projection's output. q may be None. Returns q_out [T, Hq, d]."""
+    import torch
+    index = _gpu_of(k_pages, v_pages, q, k, v, positions, slots, inv_freq, q_weight, k_weight, q_out)
+    pool = page_pool(k_pages, v_pages)
+    desc = _norm_rope_desc(q, k, v, positions, slots, k_pages.shape[2], k_pages.dtype, inv_freq, q_weight, k_weight,
+                           eps, interleaved, q_out)
     handle = _raw_stream(index) if stream is None else None
     if handle is None:
         return _switched(norm_rope_store, index, stream, (q, k, v, positions, slots, k_pages, v_pages),
                          dict(inv_freq=inv_freq, q_weight=q_weight, k_weight=k_weight, eps=eps,
                               interleaved=interleaved, q_out=q_out))
+    Hq = desc.num_q_heads
     if Hq and q_out is None:
-        q_out = torch.empty((T, Hq, d), dtype=dt, device=q.device)
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     st = load_library().sgdkv_norm_rope_store(
         ctypes.byref(pool), ctypes.byref(desc), q.data_ptr() if Hq else None, k.data_ptr(), v.data_ptr(),
         positions.data_ptr(), slots.data_ptr(), None if inv_freq is None else inv_freq.data_ptr(),
@@ -611,51 +632,168 @@ def paged_attention_workspace_size(q, num_kv_heads: int, batch: int, *, max_new:
     return int(n.value)
 
 
-def paged_attention(q, k_pages, v_pages, tables, rows, cu_new, num_kv_heads: int, *, max_new: int, causal: bool = True,
-                    scale: float = 0.0, out_dtype=None, with_lse: bool = True, out=None, lse=None, workspace=None,
-                    stream=None):
-    """Attention of the new tokens q [T, Hq, d] over the paged rows of their segments, their own included
-    (sgdkv_paged_attention): tables int32 [B * Hkv, max_pages], rows int32 [B * Hkv], cu_new int32 [B + 1], all on
-    the GPU; max_new is at least the longest sequence's number of new tokens. Returns (out, lse)."""
+def _attention_desc(q, tables, rows, cu_new, num_kv_heads, max_new, causal, scale, out_dtype, with_lse, out, lse,
+                    workspace) -> PagedDesc:
     import torch
-    index = _gpu_of(q, k_pages, v_pages, tables, rows, cu_new, out, lse, workspace)
-    pool = page_pool(k_pages, v_pages)
-    if q.dim() != 3 or q.shape[2] != k_pages.shape[2] or q.dtype is not k_pages.dtype or not q.is_contiguous():
-        _refuse("q must be a dense [T, Hq, d] of the pool's dtype")
     if tables.dim() != 2 or rows.dim() != 1 or cu_new.dim() != 1 or cu_new.shape[0] < 2:
         _refuse("tables must be [B * Hkv, max_pages], rows [B * Hkv] and cu_new [B + 1]")
-    B, shape = cu_new.shape[0] - 1, q.shape
+    B = cu_new.shape[0] - 1
     if not rows.shape[0] == tables.shape[0] == B * num_kv_heads:
         _refuse(f"{rows.shape[0]} rows and {tables.shape[0]} tables for {B} sequences of {num_kv_heads} KV heads")
     _check_int32(tables, "tables")
     _check_int32(rows, "rows")
     _check_int32(cu_new, "cu_new")
     desc = _paged_desc(q, num_kv_heads, B, max_new, tables.shape[1], out_dtype, causal, scale)
-    od = torch.bfloat16 if desc.out_dtype == DTYPE_BF16 else torch.float32
     if out is not None:
-        _check_dense(out, "out", shape, od)
+        _check_dense(out, "out", q.shape, torch.bfloat16 if desc.out_dtype == DTYPE_BF16 else torch.float32)
     if workspace is not None and not workspace.is_contiguous():
         _refuse("workspace must be contiguous")
     if with_lse and lse is not None:
-        _check_dense(lse, "lse", shape[:2], torch.float32)
+        _check_dense(lse, "lse", q.shape[:2], torch.float32)
+    return desc
+
+
+def _attend(call, workspace_size, pool, desc, q, tables, rows, cu_new, with_lse, out, lse, workspace, handle):
+    import torch
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.bfloat16 if desc.out_dtype == DTYPE_BF16 else torch.float32,
+                          device=q.device)
+    if with_lse and lse is None:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    if workspace is None:
+        size = workspace_size(q, desc.num_kv_heads, desc.batch, max_new=desc.max_new)
+        workspace = alloc_workspace(size, q.device)
+    st = call(ctypes.byref(pool), ctypes.byref(desc), q.data_ptr(), tables.data_ptr(), rows.data_ptr(),
+              cu_new.data_ptr(), out.data_ptr(), lse.data_ptr() if with_lse else None, workspace.data_ptr(),
+              workspace.numel() * workspace.element_size(), handle)
+    if st:
+        _check(st)
+    return out, (lse if with_lse else None)
+
+
+def paged_attention(q, k_pages, v_pages, tables, rows, cu_new, num_kv_heads: int, *, max_new: int, causal: bool = True,
+                    scale: float = 0.0, out_dtype=None, with_lse: bool = True, out=None, lse=None, workspace=None,
+                    stream=None):
+    """Attention of the new tokens q [T, Hq, d] over the paged rows of their segments, their own included
+    (sgdkv_paged_attention): tables int32 [B * Hkv, max_pages], rows int32 [B * Hkv], cu_new int32 [B + 1], all on
+    the GPU; max_new is at least the longest sequence's number of new tokens. Returns (out, lse)."""
+    index = _gpu_of(q, k_pages, v_pages, tables, rows, cu_new, out, lse, workspace)
+    pool = page_pool(k_pages, v_pages)
+    if q.dim() != 3 or q.shape[2] != k_pages.shape[2] or q.dtype is not k_pages.dtype or not q.is_contiguous():
+        _refuse("q must be a dense [T, Hq, d] of the pool's dtype")
+    desc = _attention_desc(q, tables, rows, cu_new, num_kv_heads, max_new, causal, scale, out_dtype, with_lse, out,
+                           lse, workspace)
     handle = _raw_stream(index) if stream is None else None
     if handle is None:
         return _switched(paged_attention, index, stream, (q, k_pages, v_pages, tables, rows, cu_new, num_kv_heads),
                          dict(max_new=max_new, causal=causal, scale=scale, out_dtype=out_dtype, with_lse=with_lse,
                               out=out, lse=lse, workspace=workspace))
-    if out is None:
-        out = torch.empty(shape, dtype=od, device=q.device)
-    if with_lse and lse is None:
-        lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device)
-    if workspace is None:
-        workspace = alloc_workspace(paged_attention_workspace_size(q, num_kv_heads, B, max_new=max_new), q.device)
-    st = load_library().sgdkv_paged_attention(
-        ctypes.byref(pool), ctypes.byref(desc), q.data_ptr(), tables.data_ptr(), rows.data_ptr(), cu_new.data_ptr(),
-        out.data_ptr(), lse.data_ptr() if with_lse else None, workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), handle)
+    return _attend(load_library().sgdkv_paged_attention, paged_attention_workspace_size, pool, desc, q, tables, rows,
+                   cu_new, with_lse, out, lse, workspace, handle)
+
+
+# ----------------------------------------------- paged cache in 8 bits
+def page_pool_fp8(k_pages, v_pages, k_scales, v_scales, row_dtype) -> PagePoolFp8:
+    """The descriptor of a pool in 8 bits: k_pages, v_pages float8_e4m3fn [num_pages, page_size, d] and k_scales,
+    v_scales float8_e8m0fnu [num_pages, page_size], for rows and queries of row_dtype."""
+    import torch
+    shape = k_pages.shape
+    if len(shape) != 3 or v_pages.shape != shape or k_scales.shape != shape[:2] or v_scales.shape != shape[:2]:
+        _refuse("k_pages and v_pages must be [num_pages, page_size, d], k_scales and v_scales [num_pages, page_size]")
+    if k_pages.dtype is not torch.float8_e4m3fn or v_pages.dtype is not torch.float8_e4m3fn:
+        _refuse("k_pages and v_pages must be float8_e4m3fn")
+    if k_scales.dtype is not torch.float8_e8m0fnu or v_scales.dtype is not torch.float8_e8m0fnu:
+        _refuse("k_scales and v_scales must be float8_e8m0fnu")
+    if not (k_pages.is_contiguous() and v_pages.is_contiguous() and k_scales.is_contiguous()
+            and v_scales.is_contiguous()):
+        _refuse("k_pages, v_pages, k_scales and v_scales must be contiguous")
+    dtype = DTYPE_BF16 if row_dtype is torch.bfloat16 else DTYPE_F32 if row_dtype is torch.float32 else None
+    if dtype is None:
+        _refuse(f"rows and queries beside a pool in 8 bits must be bfloat16 or float32, not {row_dtype}")
+    return PagePoolFp8(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), shape[0],
+                       shape[1], shape[2], dtype, 0)
+
+
+def paged_store_fp8(k_rows, v_rows, slots, k_pages, v_pages, k_scales, v_scales, *, stream=None):
+    """Round rows [n, d] (bfloat16 or float32) to 8 bits and write them to their slots (sgdkv_paged_store_fp8): slots
+    int32 [n], -1 for none; the pool as in page_pool_fp8."""
+    index = _gpu_of(k_pages, v_pages, k_scales, v_scales, k_rows, v_rows, slots)
+    pool = page_pool_fp8(k_pages, v_pages, k_scales, v_scales, k_rows.dtype)
+    if k_rows.dim() != 2:
+        _refuse("k_rows and v_rows must be [n, d]")
+    shape = (k_rows.shape[0], pool.head_dim)
+    _check_dense(k_rows, "k_rows", shape, k_rows.dtype)
+    _check_dense(v_rows, "v_rows", shape, k_rows.dtype)
+    _check_int32(slots, "slots", shape[:1])
+    handle = _raw_stream(index) if stream is None else None
+    if handle is None:
+        return _switched(paged_store_fp8, index, stream, (k_rows, v_rows, slots, k_pages, v_pages, k_scales, v_scales),
+                         {})
+    st = load_library().sgdkv_paged_store_fp8(ctypes.byref(pool), k_rows.data_ptr(), v_rows.data_ptr(),
+                                              slots.data_ptr(), shape[0], handle)
     if st:
         _check(st)
-    return out, (lse if with_lse else None)
+
+
+def norm_rope_store_fp8(q, k, v, positions, slots, k_pages, v_pages, k_scales, v_scales, *, inv_freq=None,
+                        q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
+                        rope_factor: float = 1.0, q_out=None, stream=None):
+    """norm_rope_store into a pool in 8 bits (sgdkv_norm_rope_store_fp8; the pool as in page_pool_fp8). rope_factor
+    multiplies the rotated elements of queries and keys. Returns q_out [T, Hq, d], of the inputs' type."""
+    import torch
+    index = _gpu_of(k_pages, v_pages, k_scales, v_scales, q, k, v, positions, slots, inv_freq, q_weight, k_weight,
+                    q_out)
+    pool = page_pool_fp8(k_pages, v_pages, k_scales, v_scales, k.dtype)
+    desc = _norm_rope_desc(q, k, v, positions, slots, pool.head_dim, k.dtype, inv_freq, q_weight, k_weight, eps,
+                           interleaved, q_out)
+    handle = _raw_stream(index) if stream is None else None
+    if handle is None:
+        return _switched(norm_rope_store_fp8, index, stream,
+                         (q, k, v, positions, slots, k_pages, v_pages, k_scales, v_scales),
+                         dict(inv_freq=inv_freq, q_weight=q_weight, k_weight=k_weight, eps=eps,
+                              interleaved=interleaved, rope_factor=rope_factor, q_out=q_out))
+    Hq = desc.num_q_heads
+    if Hq and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    st = load_library().sgdkv_norm_rope_store_fp8(
+        ctypes.byref(pool), ctypes.byref(desc), rope_factor, q.data_ptr() if Hq else None, k.data_ptr(), v.data_ptr(),
+        positions.data_ptr(), slots.data_ptr(), None if inv_freq is None else inv_freq.data_ptr(),
+        None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+        q_out.data_ptr() if Hq else None, handle)
+    if st:
+        _check(st)
+    return q_out
+
+
+def paged_attention_fp8_workspace_size(q, num_kv_heads: int, batch: int, *, max_new: int) -> int:
+    """Bytes of workspace of paged_attention_fp8 for queries like q [T, Hq, d] and chunks of up to max_new tokens."""
+    pool = PagePoolFp8(None, None, None, None, 1, 16, q.shape[2], _dtype_code(q), 0)
+    desc = _paged_desc(q, num_kv_heads, batch, max_new, 1, None, True, 0.0)
+    n = ctypes.c_size_t(0)
+    _check(load_library().sgdkv_paged_attention_fp8_workspace_size(ctypes.byref(pool), ctypes.byref(desc),
+                                                                   ctypes.byref(n)))
+    return int(n.value)
+
+
+def paged_attention_fp8(q, k_pages, v_pages, k_scales, v_scales, tables, rows, cu_new, num_kv_heads: int, *,
+                        max_new: int, causal: bool = True, scale: float = 0.0, out_dtype=None, with_lse: bool = True,
+                        out=None, lse=None, workspace=None, stream=None):
+    """paged_attention over a pool in 8 bits (sgdkv_paged_attention_fp8; the pool as in page_pool_fp8): q [T, Hq, d]
+    is bfloat16 or float32, out of the same type unless out_dtype says otherwise. Returns (out, lse)."""
+    index = _gpu_of(q, k_pages, v_pages, k_scales, v_scales, tables, rows, cu_new, out, lse, workspace)
+    pool = page_pool_fp8(k_pages, v_pages, k_scales, v_scales, q.dtype)
+    if q.dim() != 3 or q.shape[2] != pool.head_dim or not q.is_contiguous():
+        _refuse("q must be a dense [T, Hq, d]")
+    desc = _attention_desc(q, tables, rows, cu_new, num_kv_heads, max_new, causal, scale, out_dtype, with_lse, out,
+                           lse, workspace)
+    handle = _raw_stream(index) if stream is None else None
+    if handle is None:
+        return _switched(paged_attention_fp8, index, stream,
+                         (q, k_pages, v_pages, k_scales, v_scales, tables, rows, cu_new, num_kv_heads),
+                         dict(max_new=max_new, causal=causal, scale=scale, out_dtype=out_dtype, with_lse=with_lse,
+                              out=out, lse=lse, workspace=workspace))
+    return _attend(load_library().sgdkv_paged_attention_fp8, paged_attention_fp8_workspace_size, pool, desc, q,
+                   tables, rows, cu_new, with_lse, out, lse, workspace, handle)
 
 
 # ------------------------------------------------------- kernel timing

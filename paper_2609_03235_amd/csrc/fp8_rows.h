@@ -1,0 +1,72 @@
+// Rows of a cache in 8 bits (gfx950): e4m3 numbers (4 exponent bits with bias 7, 3 of mantissa, the largest 448, no
+// infinities) times a power of two per row, an e8m0 code c for 2^(c - 127).
+//
+// A row's power is the smallest with which its largest finite value is at most 448, and at least 2^kMinRowExp. A power
+// of two makes both ways exact but for the one rounding to four bits of mantissa: x / 2^e is exact in fp32, and a
+// number times 2^e is exact in bf16, so that the hardware's conversions with a scale, one instruction for two numbers,
+// give the value itself. The rounding of e4m3 is relative (half a step is 2^-4 of the value, down to 2^-6), so a scale
+// other than a power of two, or one of fewer columns, would not make it smaller.
+#pragma once
+
+#include "mfma_frag.h"
+
+namespace sgdkv {
+
+struct E4m3 {
+  uint8_t bits;
+};
+
+// Keeps the smallest number of a row, 2^-9 times its power, a normal one in fp32 and bf16.
+constexpr int kMinRowExp = -110;
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// The power of two of a code; 255 becomes an infinity, which the conversions below take for NaN.
+__device__ __forceinline__ float power_of(uint32_t code) { return __uint_as_float(code << 23); }
+
+// Numbers 2 * HI and 2 * HI + 1 of a word, times a power of two.
+template <int HI>
+__device__ __forceinline__ uint32_t e4m3_to_bf16(uint32_t w, float power) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, HI));
+}
+template <int HI>
+__device__ __forceinline__ f32x2 e4m3_to_f32(uint32_t w, float power) {
+  return __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, power, HI));
+}
+
+// Eight numbers (two words) as an operand.
+template <typename T>
+__device__ __forceinline__ Frag<T> widen_piece(uint32_t w0, uint32_t w1, float power) {
+  Frag<T> f;
+  if constexpr (sizeof(T) == 2) {
+    f.v = u32x4{e4m3_to_bf16<0>(w0, power), e4m3_to_bf16<1>(w0, power), e4m3_to_bf16<0>(w1, power),
+                e4m3_to_bf16<1>(w1, power)};
+  } else {
+    const f32x2 a = e4m3_to_f32<0>(w0, power), b = e4m3_to_f32<1>(w0, power);
+    const f32x2 c = e4m3_to_f32<0>(w1, power), d = e4m3_to_f32<1>(w1, power);
+    f.v0 = u32x4{__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y)};
+    f.v1 = u32x4{__float_as_uint(c.x), __float_as_uint(c.y), __float_as_uint(d.x), __float_as_uint(d.y)};
+  }
+  return f;
+}
+
+// |x| where it counts for the row's power.
+__device__ __forceinline__ uint32_t finite_size(float x) {
+  const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
+  return b < 0x7F800000u ? b : 0u;
+}
+// The code of a row whose largest size is `size` (bits of a finite fp32 number): 448 is 1.75 * 2^8.
+__device__ __forceinline__ int row_code(uint32_t size) {
+  const int e = (int)(size >> 23) - 127 - 8 + ((size & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  return max(e, kMinRowExp) + 127;
+}
+// 2^-e for a code.
+__device__ __forceinline__ float inverse_power(int code) { return __uint_as_float((uint32_t)(254 - code) << 23); }
+// Four values, already divided by the row's power, to nearest even; infinities and NaN become NaN.
+__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+}  // namespace sgdkv

@@ -16,6 +16,7 @@
 #pragma once
 
 #include "device_common.h"
+#include "fp8_rows.h"
 #include "mfma_frag.h"
 #include "paged_internal.h"
 #include "sgdkv_internal.h"
@@ -24,8 +25,6 @@ namespace sgdkv {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kAttnBlock = 256;
 constexpr int kAttnWaves = kAttnBlock / 64;
@@ -225,15 +224,19 @@ __device__ __forceinline__ int worker_of() {
 __device__ __forceinline__ int group_page(const PagedAttnArgs& a, const int32_t* table, int r0, int limit) {
   return r0 < limit ? table[r0 >> a.page_shift] : -1;
 }
-__device__ __forceinline__ rsrc_t group_rsrc(const PagedAttnArgs& a, const void* pool, int page, int r0, int valid,
-                                             int row_bytes) {
+__device__ __forceinline__ rsrc_t rows_rsrc(const PagedAttnArgs& a, const void* pool, int page, int r0, int valid,
+                                            int rows, int row_bytes) {
   const bool ok = page >= 0 && page < a.num_pages && valid > 0;
   const int64_t row = ok ? ((int64_t)page << a.page_shift) + (r0 & ((1 << a.page_shift) - 1)) : 0;
-  const int n = ok ? min(valid, 16) : 0;
+  const int n = ok ? min(valid, rows) : 0;
   return make_rsrc(static_cast<const char*>(pool) + row * row_bytes, (uint64_t)(n * row_bytes));
 }
+__device__ __forceinline__ rsrc_t group_rsrc(const PagedAttnArgs& a, const void* pool, int page, int r0, int valid,
+                                             int row_bytes) {
+  return rows_rsrc(a, pool, page, r0, valid, 16, row_bytes);
+}
 
-// The same buffer, of at most `rows` rows, as four scalar words.
+// The same buffer as four scalar words.
 __device__ __forceinline__ u32x4 group_words(const PagedAttnArgs& a, const void* pool, int page, int r0, int valid,
                                              int rows, int row_bytes) {
   const bool ok = page >= 0 && page < a.num_pages && valid > 0;
@@ -241,6 +244,17 @@ __device__ __forceinline__ u32x4 group_words(const PagedAttnArgs& a, const void*
   const uint64_t p = reinterpret_cast<uint64_t>(pool) + row * row_bytes;
   return u32x4{(uint32_t)uniform((int)p), (uint32_t)uniform((int)(p >> 32)),
                (uint32_t)uniform(ok ? min(valid, rows) * row_bytes : 0), (uint32_t)kRsrcWord3};
+}
+
+// The codes of the same rows (8-bit pools), one byte each. A code may mean NaN where no row is, and NaN times the zeros
+// read there is NaN: those who use a code before the masks read none past the last row (zero, a power that zeros do
+// not mind). With ROUND, for reads of four codes at once, all 16 of the group are there: they lie in its page.
+template <bool ROUND>
+__device__ __forceinline__ rsrc_t code_rsrc(const PagedAttnArgs& a, const uint8_t* codes, int page, int r0, int valid,
+                                            int rows) {
+  const bool ok = page >= 0 && page < a.num_pages && valid > 0;
+  const int64_t row = ok ? ((int64_t)page << a.page_shift) + (r0 & ((1 << a.page_shift) - 1)) : 0;
+  return make_rsrc(codes + row, ok ? (ROUND ? 16 : min(valid, rows)) : 0);
 }
 
 // 64 x 16 bytes from a buffer into LDS at lds + 16 * lane; out-of-range lanes write zeros. The compiler does not
@@ -282,6 +296,13 @@ __device__ __forceinline__ u32x2 lds_transposed(const char* p) {
   typedef __attribute__((address_space(3))) bf16x4* lds_ptr;
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)(p)));
 }
+// Eight keys of bytes likewise: lane i receives column i of the eight rows that the group's lanes point at (lane
+// 2r + c at row r, columns 8c .. 8c + 7).
+__device__ __forceinline__ u32x2 lds_transposed8(const char* p) {
+  typedef int i32x2 __attribute__((ext_vector_type(2)));
+  typedef __attribute__((address_space(3))) i32x2* lds_ptr;
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_ptr)(p)));
+}
 
 // Masked keys have probability zero, and zero times a value that is not finite is NaN. Keys past every row's last
 // one are loaded as zeros. In a tile with keys that some rows see and others do not, clean_values sets values that
@@ -317,6 +338,28 @@ __device__ __forceinline__ void clean_values(char* vals, int key0, int r0, int r
     *at = v;
   }
 }
+// The same for rows of e4m3 numbers, whose only values that are not finite are the bytes 0x7F and 0xFF.
+template <int RB, typename F>
+__device__ __forceinline__ void clean_values8(char* vals, int key0, int r0, int r1, int* first_odd, F swizzle) {
+  constexpr int VPR = RB / 16;
+#pragma unroll 2
+  for (int i = r0 * VPR + (threadIdx.x & 63); i < r1 * VPR; i += 64) {
+    const int r = i / VPR, col = ((i % VPR) ^ swizzle(r)) * 16;
+    u32x4* at = reinterpret_cast<u32x4*>(vals + i * 16);
+    u32x4 v = *at;
+    uint32_t any = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) any |= (v[e] & 0x7F7F7F7Fu) + 0x01010101u;
+    if (!(any & 0x80808080u)) continue;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      if ((v[e / 4] >> (8 * (e % 4)) & 0x7F) != 0x7F) continue;
+      atomicMin(&first_odd[col + e], key0 + r);
+      v[e / 4] &= ~(0xFFu << (8 * (e % 4)));
+    }
+    *at = v;
+  }
+}
 // Columns col .. col + 3 of a row that sees `seen` keys.
 __device__ __forceinline__ f32x4 lose_odd(f32x4 o, const int* first_odd, int col, int seen) {
   const int4 odd = *reinterpret_cast<const int4*>(first_odd + col);
@@ -341,5 +384,6 @@ __device__ __forceinline__ float lse_of(float m, float s) {
 
 hipError_t launch_paged_few(const PagedAttnArgs& a, hipStream_t stream);
 hipError_t launch_paged_many(const PagedAttnArgs& a, hipStream_t stream);
+hipError_t launch_paged_many_fp8(const PagedAttnArgs& a, hipStream_t stream);
 
 }  // namespace sgdkv

@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "device_common.h"
+#include "fp8_rows.h"
 #include "paged_internal.h"
 #include "sgdkv_internal.h"
 
@@ -276,7 +277,8 @@ __global__ __launch_bounds__(kPageBlock) void paged_store_kernel(PagedStoreArgs 
 // [-pi/4, pi/4] for the Taylor sums (the first terms left out are below 2e-9 and 2e-10 of a radian). So the angle of a
 // position of 2^31 is as good as that of a small one. The sums are in 64 bits too, and what they give is rounded once:
 // an x rounded to 32 bits alone is off by up to 2^-25, 2^-27.7 turns. (A lane does this once per token, for all heads.)
-__device__ __forceinline__ void sincos_at(double position, double freq, float& sin_t, float& cos_t) {
+// `factor` multiplies both.
+__device__ __forceinline__ void sincos_at(double position, double freq, double factor, float& sin_t, float& cos_t) {
   constexpr double kHi = 0.15915494309189535, kLo = -9.839338337591243e-18;  // 1 / (2 pi)
   const double a0 = position * freq, a1 = fma(position, freq, -a0);
   const double t = a0 * kHi, t1 = fma(a0, kHi, -t) + fma(a0, kLo, a1 * kHi);
@@ -293,7 +295,7 @@ __device__ __forceinline__ void sincos_at(double position, double freq, float& s
   c = fma(z, c, -0.5);
   c = fma(z, c, 1.0);
   const int quarter = (int)((long long)n & 3);
-  const float sx = (float)s, cx = (float)c;
+  const float sx = (float)(s * factor), cx = (float)(c * factor);
   const float a = quarter & 1 ? cx : sx, b = quarter & 1 ? sx : cx;
   sin_t = quarter & 2 ? -a : a;
   cos_t = quarter == 1 || quarter == 2 ? -b : b;
@@ -333,6 +335,14 @@ struct RowPiece<float> {
   }
 };
 
+// Largest over the LPR lanes of a row, the same in each.
+template <int LPR>
+__device__ __forceinline__ uint32_t row_max(uint32_t x) {
+#pragma unroll
+  for (int o = LPR / 2; o >= 1; o >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, o, 64));
+  return x;
+}
+
 // Sum over the LPR lanes of a row, the same in each.
 template <int LPR>
 __device__ __forceinline__ float row_sum(float x) {
@@ -343,13 +353,69 @@ __device__ __forceinline__ float row_sum(float x) {
   return x + __shfl_xor(x, 1, 64);
 }
 
+// A row in 8 bits (see fp8_rows.h), of which this lane holds the N values x: its numbers, and the row's code.
+template <int LPR, int N>
+__device__ __forceinline__ int bytes_of_row(const float (&x)[N], uint32_t (&w)[N / 4]) {
+  uint32_t size = 0;
+#pragma unroll
+  for (int e = 0; e < N; ++e) size = max(size, finite_size(x[e]));
+  const int code = row_code(row_max<LPR>(size));
+  const float f = inverse_power(code);
+#pragma unroll
+  for (int e = 0; e < N; e += 4) w[e / 4] = to_e4m3(x[e] * f, x[e + 1] * f, x[e + 2] * f, x[e + 3] * f);
+  return code;
+}
+
+// Rows to their slots in 8 bits. A lane takes eight values of a row, D / 8 lanes a row; the rows' largest value goes
+// round their lanes. Bound by HBM.
+template <typename T, int D>
+__global__ __launch_bounds__(kPageBlock) void store_fp8_kernel(StoreFp8Args a) {
+  constexpr int LPR = D / 8, NV = sizeof(T) / 2, V = kStoreVecs;  // 16-byte pieces of a lane, places of a thread
+  const int64_t total = a.n * LPR, first = (int64_t)blockIdx.x * (V * kPageBlock) + threadIdx.x;
+  u32x4 rows[2][V][NV];
+  int64_t slot[V];
+#pragma unroll
+  for (int u = 0; u < V; ++u) {
+    const int64_t i = first + u * kPageBlock;
+    slot[u] = -1;
+#pragma unroll
+    for (int h = 0; h < NV; ++h) rows[0][u][h] = rows[1][u][h] = u32x4{0, 0, 0, 0};
+    if (i >= total) continue;
+    slot[u] = a.slots[i / LPR];
+#pragma unroll
+    for (int h = 0; h < NV; ++h) {
+      rows[0][u][h] = __builtin_nontemporal_load(static_cast<const u32x4*>(a.k) + i * NV + h);
+      rows[1][u][h] = __builtin_nontemporal_load(static_cast<const u32x4*>(a.v) + i * NV + h);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < V; ++u)
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      float x[8];
+      if constexpr (NV == 1) {
+        RowPiece<__bf16>::widen(rows[kv][u][0], x);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(rows[kv][u][e / 4][e % 4]);
+      }
+      uint32_t w[2];
+      const int code = bytes_of_row<LPR, 8>(x, w);  // every lane takes part
+      if (slot[u] < 0 || slot[u] >= a.total_slots) continue;
+      const int at = threadIdx.x % LPR;
+      reinterpret_cast<u32x2*>(kv ? a.v_pages : a.k_pages)[slot[u] * LPR + at] = u32x2{w[0], w[1]};
+      if (at == 0) (kv ? a.v_scales : a.k_scales)[slot[u]] = (uint8_t)code;
+    }
+}
+
 // A wave takes one token (or 1/parts of its heads): LPR lanes hold a head's row, 16 bytes each, so 64/LPR
 // heads go at once. Lane l computes the token's angle l; the sines and cosines go through LDS once and stay
 // in registers, where every head uses them. Sum of squares, norm and rotation are in 32 bits, rounded once
 // at the store. Bound by HBM: four heads' loads ahead of their use and stores that do not displace the inputs from
 // the caches (80 heads of 8191 tokens, 168 MB in and out: 95 us without either, 80 and 73 with the first, 60 to 70
 // with both; the stores make no difference up to 4096 tokens).
-template <typename T, int D>
+// FP8: into an 8-bit pool.
+template <typename T, int D, bool FP8>
 __global__ __launch_bounds__(kPageBlock) void norm_rope_kernel(NormRopeArgs a) {
   using P = RowPiece<T>;
   constexpr int N = P::N, LPR = D / N, HPW = 64 / LPR;
@@ -363,7 +429,7 @@ __global__ __launch_bounds__(kPageBlock) void norm_rope_kernel(NormRopeArgs a) {
 
   if (live && lane < half) {
     float s, c;
-    sincos_at(a.positions[token], a.inv_freq[lane], s, c);
+    sincos_at(a.positions[token], a.inv_freq[lane], FP8 ? a.factor : 1.0, s, c);
     sines[wid][lane] = s;
     cosines[wid][lane] = c;
   }
@@ -431,7 +497,18 @@ __global__ __launch_bounds__(kPageBlock) void norm_rope_kernel(NormRopeArgs a) {
           for (int e = 0; e < N; ++e) x[e] = fmaf(p[e], sn[e], x[e] * cs[e]);
         }
       }
-      if (is_q || is_k) y = P::narrow(x);
+      if (is_q || (is_k && !FP8)) y = P::narrow(x);
+      if constexpr (FP8) {
+        uint32_t w8[N / 4];
+        const int code = bytes_of_row<LPR, N>(x, w8);  // of every row: its lanes go together
+        if (!is_q && slot[u] >= 0 && slot[u] < a.total_slots) {
+          uint8_t* to = static_cast<uint8_t*>(is_k ? a.k_pages : a.v_pages) + slot[u] * D + col;
+          if constexpr (N == 8) *reinterpret_cast<u32x2*>(to) = u32x2{w8[0], w8[1]};
+          else *reinterpret_cast<uint32_t*>(to) = w8[0];
+          if (lane % LPR == 0) (is_k ? a.k_scales : a.v_scales)[slot[u]] = (uint8_t)code;
+        }
+        slot[u] = -1;
+      }
       if (is_q) {
         __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(a.q_out) + (token * a.Hq + h) * LPR + lane % LPR);
       } else if (slot[u] >= 0 && slot[u] < a.total_slots) {
@@ -482,28 +559,53 @@ hipError_t launch_paged_store(const PagedStoreArgs& args, hipStream_t stream) {
   return hipGetLastError();
 }
 
+hipError_t launch_paged_store_fp8(const StoreFp8Args& args, hipStream_t stream) {
+  const int64_t lanes = args.D / 8, per = kStoreVecs * kPageBlock, most = kMaxBlocks * per / lanes;
+  if (args.n == 0) return hipSuccess;
+  prof_begin("paged_store_fp8", stream);
+  for (int64_t first = 0; first < args.n; first += most) {
+    StoreFp8Args a = args;
+    const int64_t row_bytes = a.D * (a.dtype ? 2 : 4);
+    a.n = std::min(most, args.n - first);
+    a.k = static_cast<const char*>(args.k) + first * row_bytes;
+    a.v = static_cast<const char*>(args.v) + first * row_bytes;
+    a.slots = args.slots + first;
+    const dim3 grid((unsigned)((a.n * lanes + per - 1) / per)), block(kPageBlock);
+    if (a.dtype) {
+      if (a.D == 128) store_fp8_kernel<__bf16, 128><<<grid, block, 0, stream>>>(a);
+      else store_fp8_kernel<__bf16, 64><<<grid, block, 0, stream>>>(a);
+    } else {
+      if (a.D == 128) store_fp8_kernel<float, 128><<<grid, block, 0, stream>>>(a);
+      else store_fp8_kernel<float, 64><<<grid, block, 0, stream>>>(a);
+    }
+  }
+  prof_end(stream);
+  return hipGetLastError();
+}
+
 namespace {
+template <bool FP8>
 void launch_norm_rope_part(const NormRopeArgs& a, hipStream_t stream) {
   const int64_t waves = (int64_t)a.T * a.parts;
   const dim3 grid((unsigned)((waves + kWavesPerBlock - 1) / kWavesPerBlock)), block(kPageBlock);
   if (a.dtype) {
-    if (a.D == 128) norm_rope_kernel<__bf16, 128><<<grid, block, 0, stream>>>(a);
-    else norm_rope_kernel<__bf16, 64><<<grid, block, 0, stream>>>(a);
+    if (a.D == 128) norm_rope_kernel<__bf16, 128, FP8><<<grid, block, 0, stream>>>(a);
+    else norm_rope_kernel<__bf16, 64, FP8><<<grid, block, 0, stream>>>(a);
   } else {
-    if (a.D == 128) norm_rope_kernel<float, 128><<<grid, block, 0, stream>>>(a);
-    else norm_rope_kernel<float, 64><<<grid, block, 0, stream>>>(a);
+    if (a.D == 128) norm_rope_kernel<float, 128, FP8><<<grid, block, 0, stream>>>(a);
+    else norm_rope_kernel<float, 64, FP8><<<grid, block, 0, stream>>>(a);
   }
 }
-}  // namespace
 
-hipError_t launch_norm_rope(const NormRopeArgs& args, hipStream_t stream) {
+template <bool FP8>
+hipError_t launch_norm_rope_all(const NormRopeArgs& args, const char* name, hipStream_t stream) {
   if (args.T == 0) return hipSuccess;
   // Few tokens share their heads out over several waves, up to about eight waves per compute unit in all.
   const int eb = args.dtype ? 2 : 4, row_lanes = args.D * eb / 16, heads = args.Hq + 2 * args.Hkv;
   const int steps = (heads * row_lanes + 63) / 64;  // steps of a wave that takes all heads
   const int64_t want = (2048 + (int64_t)args.T - 1) / args.T;
   const int64_t most = kMaxBlocks * kWavesPerBlock;  // tokens of a launch: beyond 2048 a token is a wave's
-  prof_begin("norm_rope_store", stream);
+  prof_begin(name, stream);
   for (int64_t first = 0; first < args.T; first += most) {
     NormRopeArgs a = args;
     a.parts = want < steps ? (int)want : steps;
@@ -516,10 +618,18 @@ hipError_t launch_norm_rope(const NormRopeArgs& args, hipStream_t stream) {
     a.v = static_cast<const char*>(args.v) + first * args.v_stride;
     a.positions = args.positions + first;
     a.slots = args.slots + first * args.Hkv;
-    launch_norm_rope_part(a, stream);
+    launch_norm_rope_part<FP8>(a, stream);
   }
   prof_end(stream);
   return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_norm_rope(const NormRopeArgs& a, hipStream_t stream) {
+  return launch_norm_rope_all<false>(a, "norm_rope_store", stream);
+}
+hipError_t launch_norm_rope_fp8(const NormRopeArgs& a, hipStream_t stream) {
+  return launch_norm_rope_all<true>(a, "norm_rope_store_fp8", stream);
 }
 
 }  // namespace sgdkv

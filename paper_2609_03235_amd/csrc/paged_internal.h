@@ -50,6 +50,20 @@ struct PagedStoreArgs {
 };
 hipError_t launch_paged_store(const PagedStoreArgs& a, hipStream_t stream);
 
+struct StoreFp8Args {
+  int D, dtype;          // of the rows given
+  int64_t n;             // rows
+  int64_t total_slots;   // rows of the pool
+  const void* k;
+  const void* v;
+  const int32_t* slots;  // [n]
+  uint8_t* k_pages;
+  uint8_t* v_pages;
+  uint8_t* k_scales;
+  uint8_t* v_scales;
+};
+hipError_t launch_paged_store_fp8(const StoreFp8Args& a, hipStream_t stream);
+
 struct NormRopeArgs {
   int T, Hq, Hkv, D, dtype;
   int rot;          // rotated elements per head (0: none)
@@ -69,8 +83,13 @@ struct NormRopeArgs {
   void* k_pages;
   void* v_pages;
   int parts;    // waves that share a token's heads (set at the launch)
+  // a pool in 8 bits (k_pages and v_pages are e4m3 numbers)
+  uint8_t* k_scales;
+  uint8_t* v_scales;
+  double factor;  // of the rotated columns
 };
 hipError_t launch_norm_rope(const NormRopeArgs& a, hipStream_t stream);
+hipError_t launch_norm_rope_fp8(const NormRopeArgs& a, hipStream_t stream);
 
 // ------------------------------------------------------------- attention
 struct PagedAttnArgs {
@@ -101,6 +120,9 @@ struct PagedAttnArgs {
   int4* shared;
   float* part;       // [2 * kPagedWorkers][M][D]: o of a query tile that several workers share
   float* part_ms;    // [2 * kPagedWorkers][M][2]
+  // a pool in 8 bits (k_pages and v_pages are e4m3 numbers)
+  const uint8_t* k_scales;
+  const uint8_t* v_scales;
 };
 // The kernel instance for a shape: query rows per tile and key rows per step.
 struct PagedAttnShape {
@@ -109,5 +131,8 @@ struct PagedAttnShape {
 };
 PagedAttnShape paged_attn_shape(int dtype, int G, int max_new);
 hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream);
+// The same over a pool in 8 bits; dtype is the queries'.
+PagedAttnShape paged_attn_fp8_shape(int dtype, int G, int max_new);
+hipError_t launch_paged_attention_fp8(const PagedAttnArgs& a, hipStream_t stream);
 
 }  // namespace sgdkv

@@ -23,6 +23,7 @@ namespace {
 // Rows in LDS have no padding (a load writes its lanes' 16 bytes one after the other); the 16-byte pieces of a
 // row change places instead, piece c of row r lying at place c ^ key_swizzle(r) (value_swizzle): reads of one
 // piece of 16 rows, or of four pieces of four rows, touch every bank once.
+// T: the type of the queries, of the products and of the rows in LDS.
 template <typename T, int D>
 struct ManyShape {
   static constexpr int EB = sizeof(T), RB = D * EB;
@@ -82,6 +83,48 @@ struct Probs<__bf16, true, NK> : Probs<float, false, NK> {
   }
 };
 
+// Rows of an 8-bit pool on their way to LDS: a wave's share of a tile, a lane's 16 numbers of NL rows, which are
+// widened to T on the way (row `row` of the wave's, piece `col` of 16 numbers).
+template <typename T, int D>
+struct ByteRows {
+  using S = ManyShape<T, D>;
+  static constexpr int VPR = D / 16, RPL = 64 / VPR, NL = (S::RPW + RPL - 1) / RPL;
+  u32x4 raw[NL];
+  uint32_t code[NL];
+  __device__ __forceinline__ void load(const PagedAttnArgs& a, const void* pool, const uint8_t* codes, int page, int r0,
+                                       int valid, int lane) {
+    const rsrc_t rows = rows_rsrc(a, pool, page, r0, valid, S::RPW, D);
+    const rsrc_t powers = code_rsrc<false>(a, codes, page, r0, valid, S::RPW);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int r = i * RPL + lane / VPR;
+      raw[i] = ld128(rows, r * D + lane % VPR * 16);
+      code[i] = ld8(powers, r);
+    }
+  }
+  template <typename F>
+  __device__ __forceinline__ void store(char* to, int my_row, int lane, F swizzle) const {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int r = i * RPL + lane / VPR, c = lane % VPR;
+      if (RPL > S::RPW && r >= S::RPW) continue;
+      char* row = to + (my_row + r) * S::RB;
+      const int sw = swizzle(my_row + r);
+      const float p = power_of(code[i]);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const Frag<T> f = widen_piece<T>(raw[i][2 * e], raw[i][2 * e + 1], p);
+        if constexpr (sizeof(T) == 2) {
+          *reinterpret_cast<u32x4*>(row + ((2 * c + e) ^ sw) * 16) = f.v;
+        } else {
+          *reinterpret_cast<u32x4*>(row + ((4 * c + 2 * e) ^ sw) * 16) = f.v0;
+          *reinterpret_cast<u32x4*>(row + ((4 * c + 2 * e + 1) ^ sw) * 16) = f.v1;
+        }
+      }
+    }
+  }
+};
+
 // A tile of the line as its worker does it.
 struct ManyTile {
   LineTile at;
@@ -90,9 +133,11 @@ struct ManyTile {
   bool own;        // not shared
 };
 
-template <typename T, int D, bool FINE>
+// KV: the pool's rows, T or E4m3.
+template <typename T, typename KV, int D, bool FINE>
 __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs a) {
   using S = ManyShape<T, D>;
+  constexpr bool FP8 = sizeof(KV) == 1;
   constexpr int EB = S::EB, RB = S::RB, KT = S::KT, NC = S::NC, NK = S::NK, ND = S::ND, NL = S::NL;
   constexpr int M = 128;
   __shared__ __attribute__((aligned(16))) char lds[2][2][S::TILE];  // two buffers of keys and values
@@ -147,8 +192,14 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
   const int32_t* table;
   int page;
   u32x4 q[NC];
+  ByteRows<T, D> kbytes, vbytes;  // 8-bit pools: of the tile under way
   auto load = [&](const ManyTile& t, int j) {
     const int r0 = j * KT + my_row;
+    if constexpr (FP8) {
+      kbytes.load(a, a.k_pages, a.k_scales, page, r0, t.limit - r0, lane);
+      vbytes.load(a, a.v_pages, a.v_scales, page, r0, t.limit - r0, lane);
+      return;
+    }
     const u32x4 kr = group_words(a, a.k_pages, page, r0, t.limit - r0, S::RPW, RB);
     const u32x4 vr = group_words(a, a.v_pages, page, r0, t.limit - r0, S::RPW, RB);
     const uint32_t to = uniform((int)(lds0 + (j & 1) * 2 * S::TILE + my_row * RB));
@@ -156,6 +207,15 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
     for (int i = 0; i < NL; ++i) load_to_lds(kr, koff[i], to + i * 1024);
 #pragma unroll
     for (int i = 0; i < NL; ++i) load_to_lds(vr, voff[i], to + S::TILE + i * 1024);
+  };
+  // The rows under way into LDS (those of other pools are there already).
+  auto arrive = [&](int j) {
+    if constexpr (FP8) {
+      kbytes.store(lds[j & 1][0], my_row, lane, S::key_swizzle);
+      vbytes.store(lds[j & 1][1], my_row, lane, S::value_swizzle);
+    } else {
+      wait_loads();
+    }
   };
   // Sets a tile's queries and first keys on their way; by then all waves are done with the keys before.
   auto begin = [&](const ManyTile& t, int which) {
@@ -409,7 +469,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
       __builtin_amdgcn_s_setprio(0);
     };
 
-    wait_loads();
+    arrive(now.j0);
     // Tells the compiler that the queries are there too: it would wait for them in the loop, and so for its loads.
 #pragma unroll
     for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(q[c]));
@@ -422,7 +482,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
         const int page2 = group_page(a, table, (j + 2) * KT + my_row, limit);
         if (j + 1 < now.j1) load(now, j + 1);
         if (j * KT < hi) attend(lds[j & 1][0], edge, j * KT, j == now.j0);
-        wait_loads();
+        if (!FP8 || j + 1 < now.j1) arrive(j + 1);
         page = uniform(page2);
         __syncthreads();
       }
@@ -433,22 +493,28 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
   }
 }
 
-template <typename T, int D>
+template <typename T, typename KV, int D>
 void launch_many(const PagedAttnArgs& a, hipStream_t stream) {
   if constexpr (sizeof(T) == 2) {
     if (a.out_dtype == 0) {
-      paged_many_kernel<T, D, true><<<dim3(kPagedWorkers), dim3(kAttnBlock), 0, stream>>>(a);
+      paged_many_kernel<T, KV, D, true><<<dim3(kPagedWorkers), dim3(kAttnBlock), 0, stream>>>(a);
       return;
     }
   }
-  paged_many_kernel<T, D, false><<<dim3(kPagedWorkers), dim3(kAttnBlock), 0, stream>>>(a);
+  paged_many_kernel<T, KV, D, false><<<dim3(kPagedWorkers), dim3(kAttnBlock), 0, stream>>>(a);
 }
 
 }  // namespace
 
 hipError_t launch_paged_many(const PagedAttnArgs& a, hipStream_t stream) {
-  if (a.dtype) a.D == 128 ? launch_many<__bf16, 128>(a, stream) : launch_many<__bf16, 64>(a, stream);
-  else a.D == 128 ? launch_many<float, 128>(a, stream) : launch_many<float, 64>(a, stream);
+  if (a.dtype) a.D == 128 ? launch_many<__bf16, __bf16, 128>(a, stream) : launch_many<__bf16, __bf16, 64>(a, stream);
+  else a.D == 128 ? launch_many<float, float, 128>(a, stream) : launch_many<float, float, 64>(a, stream);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_many_fp8(const PagedAttnArgs& a, hipStream_t stream) {
+  if (a.dtype) a.D == 128 ? launch_many<__bf16, E4m3, 128>(a, stream) : launch_many<__bf16, E4m3, 64>(a, stream);
+  else a.D == 128 ? launch_many<float, E4m3, 128>(a, stream) : launch_many<float, E4m3, 64>(a, stream);
   return hipGetLastError();
 }
 
