@@ -28,7 +28,7 @@ ILP = ["-mllvm", "-amdgpu-sched-strategy=max-ilp"]
 FILE_FLAGS = {"lse_kernels_ilp.hip": ILP, "score_kernels_ilp.hip": ILP}
 KERNEL_SOURCES = ["lse_kernels.hip", "lse_kernels_ilp.hip", "score_kernels.hip", "score_kernels_ilp.hip",
                   "select_kernels.hip", "decode_kernels.hip", "decode_scratch.hip", "paged_cache.hip", "paged_few.hip",
-                  "paged_many.hip"]
+                  "paged_few_fp8.hip", "paged_many.hip"]
 HOST_SOURCES = ["sgdkv_host.cpp", "paged_host.cpp", "paged_fp8_host.cpp", "profile.cpp"]
 
 

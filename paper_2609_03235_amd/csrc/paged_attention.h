@@ -279,10 +279,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
   f32x2 v = {x, y};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
-// x and y as sums of three bf16 terms each, which hold all 24 bits: word e of each term.
-__device__ __forceinline__ void split_bf16(float x, float y, u32x4 (&to)[3], int e) {
+// x and y as sums of N bf16 terms each, of which three hold all 24 bits: word e of each term.
+template <int N>
+__device__ __forceinline__ void split_bf16(float x, float y, u32x4 (&to)[N], int e) {
 #pragma unroll
-  for (int k = 0; k < 3; ++k) {
+  for (int k = 0; k < N; ++k) {
     const uint32_t w = pack_bf16(x, y);
     to[k][e] = w;
     x -= bf16_lo(w);
@@ -384,6 +385,9 @@ __device__ __forceinline__ float lse_of(float m, float s) {
 
 hipError_t launch_paged_few(const PagedAttnArgs& a, hipStream_t stream);
 hipError_t launch_paged_many(const PagedAttnArgs& a, hipStream_t stream);
+hipError_t launch_paged_few_fp8(const PagedAttnArgs& a, hipStream_t stream);
 hipError_t launch_paged_many_fp8(const PagedAttnArgs& a, hipStream_t stream);
+// Joins the parts of shared tiles after an attention kernel.
+hipError_t launch_paged_merge(const PagedAttnArgs& a, hipStream_t stream);
 
 }  // namespace sgdkv

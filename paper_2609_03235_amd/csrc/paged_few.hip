@@ -18,22 +18,15 @@ namespace {
 
 // Rows of values in LDS have no padding (a load writes its lanes' 16 bytes one after the other); piece c of row r
 // lies at place c ^ swizzle(r), which spreads the pieces that a read takes from several rows over the banks.
-// T: the queries' type and the products'; KV: the rows', T or E4m3.
-template <typename T, typename KV, int D>
+template <typename T, int D>
 struct FewShape {
-  static constexpr bool FP8 = sizeof(KV) == 1;
-  static constexpr int EB = sizeof(KV), RB = D * EB, NC = D / 32, ND = D / 16;
-  static constexpr int U = EB <= 2 ? 2 : 1;              // 16-row groups per wave and step
+  static constexpr int EB = sizeof(T), RB = D * EB, NC = D / 32, ND = D / 16;
+  static constexpr int U = EB == 2 ? 2 : 1;              // 16-row groups per wave and step
   static constexpr int STEP = 16 * U, KT = STEP * kAttnWaves;
   static constexpr int VPR = RB / 16, RPL = 64 / VPR, NV = 16 / RPL;  // rows per load, loads per group
   static constexpr int STAGE = STEP * RB;
   static __device__ __forceinline__ int swizzle(int r) {
-    if (FP8) return RB == 128 ? ((r >> 1) & 3) | ((r >> 4) & 1) << 2 : ((r >> 2) & 1) | ((r >> 4) & 1) << 1;
     return EB == 4 ? ((r >> 2) & 3) << 2 : (RB == 128 ? ((r >> 1) & 3) << 1 : (r & 7) << 1);
-  }
-  static __device__ __forceinline__ void clean(char* vals, int key0, int r0, int r1, int* first_odd) {
-    if constexpr (FP8) clean_values8<RB>(vals, key0, r0, r1, first_odd, swizzle);
-    else clean_values<EB, RB>(vals, key0, r0, r1, first_odd, swizzle);
   }
 };
 
@@ -42,15 +35,13 @@ struct FewShape {
 // 32K rows 337 us with one term, 335 with three; 48 rows, 16 x 6 tokens over 4 x 20K rows, 127 and 131), and one term
 // adds an error of its own (64 x 1 tokens over 5K rows 1.72e-3 of the output, rms, where the output's own rounding is
 // 1.67e-3).
-template <typename T, typename KV, int D, int QB>
+template <typename T, int D, int QB>
 __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs a) {
-  using S = FewShape<T, KV, D>;
-  constexpr bool FP8 = S::FP8;
-  constexpr int EB = sizeof(T), QRB = D * EB, RB = S::RB, NC = S::NC, ND = S::ND, U = S::U, STEP = S::STEP;
-  constexpr int KT = S::KT, NV = S::NV;
+  using S = FewShape<T, D>;
+  constexpr int EB = S::EB, RB = S::RB, NC = S::NC, ND = S::ND, U = S::U, STEP = S::STEP, KT = S::KT, NV = S::NV;
   constexpr int M = 16 * QB;
   constexpr bool QLDS = QB > 2;    // query operands read from LDS at each use: no registers for them
-  constexpr int QP = QRB + 16;     // their pitch
+  constexpr int QP = RB + 16;      // their pitch
   constexpr int OP = D + 4;        // pitch of a row of o in LDS, in floats: the rows' writes spread over the banks
   constexpr int kMerge = 16 * OP * 4;
   constexpr int kWaveLds = 2 * S::STAGE > kMerge ? 2 * S::STAGE : kMerge;
@@ -71,16 +62,12 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
   int64_t pos = share * w;
   char* stage = lds[wid];
   const uint32_t stage0 = lds_address(stage);
-  // where this lane's 16 bytes of each load of a group come from (bytes: the groups' places differ)
-  constexpr int VU = FP8 ? U : 1;
-  uint32_t voff[VU][NV];
+  uint32_t voff[NV];  // where this lane's 16 bytes of each load of a group come from
 #pragma unroll
-  for (int u = 0; u < VU; ++u)
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int r = i * S::RPL + lane / S::VPR;
-      voff[u][i] = r * RB + ((lane % S::VPR) ^ S::swizzle(16 * u + r)) * 16;
-    }
+  for (int i = 0; i < NV; ++i) {
+    const int r = i * S::RPL + lane / S::VPR;
+    voff[i] = r * RB + ((lane % S::VPR) ^ S::swizzle(r)) * 16;
+  }
 
   while (pos < end) {
     if (at.tile >= at.g.tiles) {  // the next segment
@@ -110,14 +97,12 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
       // query rows as B operands: row lr of block qb is head row % G of token row / G
       Frag<T> q[QLDS ? 1 : QB][NC];
       int seen[QB];
-      const rsrc_t qr = make_rsrc(static_cast<const char*>(a.q) + ((int64_t)(g.t0 + tok0) * a.Hq + h * a.G) * QRB,
-                                  ((uint64_t)(ntok - 1) * a.Hq + a.G) * QRB);
+      const rsrc_t qr = make_rsrc(static_cast<const char*>(a.q) + ((int64_t)(g.t0 + tok0) * a.Hq + h * a.G) * RB,
+                                  ((uint64_t)(ntok - 1) * a.Hq + a.G) * RB);
       auto query_off = [&](int r) -> uint32_t {
         const int tok = r / a.G, hd = r - tok * a.G;
-        return r < nrow ? (uint32_t)((tok * a.Hq + hd) * QRB) : 0xFFFF0000u;
+        return r < nrow ? (uint32_t)((tok * a.Hq + hd) * RB) : 0xFFFF0000u;
       };
-      // The 8 columns of a lane's piece c. (A lane has 16 bytes of an 8-bit key at once: two pieces.)
-      auto piece_col = [&](int c) { return FP8 ? 64 * (c / 2) + 16 * lg + 8 * (c % 2) : 32 * c + 8 * lg; };
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
         const int r = 16 * qb + lr;
@@ -125,18 +110,18 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
         if constexpr (!QLDS) {
           const uint32_t off = query_off(r);
 #pragma unroll
-          for (int c = 0; c < NC; ++c) q[qb][c] = gload_frag<T>(qr, off + piece_col(c) * EB);
+          for (int c = 0; c < NC; ++c) q[qb][c] = gload_frag<T>(qr, off + (32 * c + 8 * lg) * EB);
         }
       }
       if constexpr (QLDS) {
-        for (int i = tid; i < M * (QRB / 16); i += kAttnBlock) {
-          const int r = i / (QRB / 16), c = i % (QRB / 16);
+        for (int i = tid; i < M * S::VPR; i += kAttnBlock) {
+          const int r = i / S::VPR, c = i % S::VPR;
           *reinterpret_cast<u32x4*>(qlds + r * QP + c * 16) = ld128(qr, query_off(r) + c * 16);
         }
         __syncthreads();
       }
       auto query = [&](int qb, int c) {
-        if constexpr (QLDS) return lds_frag<T>(qlds, (16 * qb + lr) * QP + piece_col(c) * EB);
+        if constexpr (QLDS) return lds_frag<T>(qlds, (16 * qb + lr) * QP + (32 * c + 8 * lg) * EB);
         else return q[qb][c];
       };
       float m[QB], s[QB];
@@ -150,8 +135,6 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
       }
 
       Frag<T> k[U][NC];
-      u32x4 kraw[FP8 ? U : 1][FP8 ? NC / 2 : 1];  // the keys as they come
-      uint32_t kcode[U], vcode[U];                // the codes of row lr, and of rows 4lg .. 4lg + 3
       auto load = [&](int j) {
         const int r0 = first_row(j);
         const uint32_t to = uniform((int)(stage0 + (j & 1) * S::STAGE));
@@ -159,21 +142,13 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
         for (int u = 0; u < U; ++u) {
           const u32x4 vr = group_words(a, a.v_pages, uniform(page[u]), r0 + 16 * u, limit - r0 - 16 * u, 16, RB);
 #pragma unroll
-          for (int i = 0; i < NV; ++i) load_to_lds_nt(vr, voff[FP8 ? u : 0][i], to + u * 16 * RB + i * 1024);
+          for (int i = 0; i < NV; ++i) load_to_lds_nt(vr, voff[i], to + u * 16 * RB + i * 1024);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const rsrc_t kr = group_rsrc(a, a.k_pages, uniform(page[u]), r0 + 16 * u, limit - r0 - 16 * u, RB);
-          if constexpr (FP8) {
 #pragma unroll
-            for (int c = 0; c < NC / 2; ++c) kraw[u][c] = ld128_nt(kr, (uint32_t)(lr * RB + 64 * c + 16 * lg));
-            const int valid = limit - r0 - 16 * u;
-            kcode[u] = ld8(code_rsrc<false>(a, a.k_scales, uniform(page[u]), r0 + 16 * u, valid, 16), lr);
-            vcode[u] = ld32(code_rsrc<true>(a, a.v_scales, uniform(page[u]), r0 + 16 * u, valid, 16), 4 * lg);
-          } else {
-#pragma unroll
-            for (int c = 0; c < NC; ++c) k[u][c] = gload_frag_nt<T>(kr, (uint32_t)(lr * RB + (32 * c + 8 * lg) * EB));
-          }
+          for (int c = 0; c < NC; ++c) k[u][c] = gload_frag_nt<T>(kr, (uint32_t)(lr * RB + (32 * c + 8 * lg) * EB));
         }
       };
       load(j0);
@@ -182,20 +157,6 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
 #pragma unroll
         for (int u = 0; u < U; ++u) page[u] = group_page(a, table, first_row(j + 1) + 16 * u, limit);
         wait_loads();  // this step's keys and values, the next one's pages
-        float vpow[U][4];
-        if constexpr (FP8) {
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const float p = power_of(kcode[u]);
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-              const u32x4 w = kraw[u][c / 2];
-              k[u][c] = widen_piece<T>(w[2 * (c % 2)], w[2 * (c % 2) + 1], p);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) vpow[u][i] = power_of(vcode[u] >> 8 * i & 0xFF);
-          }
-        }
         f32x4 y[QB][U];
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb)
@@ -212,7 +173,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
         if (j + 1 < j1) load(j + 1);
         char* vals = stage + (j & 1) * S::STAGE;
         if (r0 + STEP > first_seen && r0 < limit)
-          S::clean(vals, r0, max(first_seen - r0, 0), min(limit - r0, STEP), first_odd);
+          clean_values<EB, RB>(vals, r0, max(first_seen - r0, 0), min(limit - r0, STEP), first_odd, S::swizzle);
         float p[QB][U][4];
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
@@ -236,8 +197,6 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
               const float e = fast_exp2(fmaf(y[qb][u][i], a.c2, -ref));
               p[qb][u][i] = 16 * u + i < left ? e : 0.f;
               sum += p[qb][u][i];
-              // The value's power goes to its probability. (It may be infinite where the key is not seen.)
-              if constexpr (FP8) p[qb][u][i] = 16 * u + i < left ? e * vpow[u][i] : 0.f;
             }
           s[qb] = fmaf(s[qb], alpha, sum);
           if (__any(alpha != 1.f)) {
@@ -252,39 +211,18 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_kernel(PagedAttnArgs 
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               split_bf16(p[qb][e / 2][2 * (e % 2)], p[qb][e / 2][2 * (e % 2) + 1], piece[qb], e);
-          const int row = FP8 ? 4 * lg + (lr & 8) * 2 + lr / 2 % 4 : 4 * lg + lr / 4;  // T: and 16 on, the same swizzle
+          const int row = 4 * lg + lr / 4;  // and 16 further on: the same swizzle
           const char* vp = vals + row * RB + (lr & 1) * 8;
 #pragma unroll
           for (int d = 0; d < ND; ++d) {
+            const char* vd = vp + (((2 * d + (lr & 3) / 2) ^ S::swizzle(row)) * 16);
+            const u32x2 v0 = lds_transposed(vd), v1 = lds_transposed(vd + 16 * RB);
             Frag<__bf16> vt;
-            if constexpr (FP8) {
-              const u32x2 v = lds_transposed8(vp + ((d ^ S::swizzle(row)) * 16));
-              vt = widen_piece<__bf16>(v.x, v.y, 1.f);
-            } else {
-              const char* vd = vp + (((2 * d + (lr & 3) / 2) ^ S::swizzle(row)) * 16);
-              const u32x2 v0 = lds_transposed(vd), v1 = lds_transposed(vd + 16 * RB);
-              vt.v = u32x4{v0.x, v0.y, v1.x, v1.y};
-            }
+            vt.v = u32x4{v0.x, v0.y, v1.x, v1.y};
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
               for (int k = 0; k < 3; ++k) o[qb][d] = mma(vt, Frag<__bf16>{piece[qb][k]}, o[qb][d]);
-          }
-        } else if constexpr (FP8) {
-          const int row = 4 * lg + (lr & 8) * 2 + lr / 2 % 4;
-          const char* vp = vals + row * RB + (lr & 1) * 8;
-#pragma unroll
-          for (int d = 0; d < ND; ++d) {
-            const u32x2 v = lds_transposed8(vp + ((d ^ S::swizzle(row)) * 16));
-            const Frag<float> vt = widen_piece<float>(v.x, v.y, 1.f);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int qb = 0; qb < QB; ++qb) {
-                const float v0 = __uint_as_float(vt.v0[i]), v1 = __uint_as_float(vt.v1[i]);
-                o[qb][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v0, p[qb][0][i], o[qb][d], 0, 0, 0);
-                o[qb][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v1, p[qb][U - 1][i], o[qb][d], 0, 0, 0);
-              }
           }
         } else {
 #pragma unroll
@@ -456,23 +394,36 @@ __global__ __launch_bounds__(kAttnBlock) void paged_merge_kernel(PagedAttnArgs a
   }
 }
 
-template <typename T, typename KV, int D, int QB>
+template <typename T, int D, int QB>
 void launch_few(const PagedAttnArgs& a, hipStream_t stream) {
-  paged_few_kernel<T, KV, D, QB><<<dim3(kPagedWorkers), dim3(kAttnBlock), 0, stream>>>(a);
+  paged_few_kernel<T, D, QB><<<dim3(kPagedWorkers), dim3(kAttnBlock), 0, stream>>>(a);
 }
 
-template <typename T, typename KV, int D>
+template <typename T, int D>
 void launch_few_rows(const PagedAttnArgs& a, hipStream_t stream) {
   switch (a.tile_rows) {
-    case 16: return launch_few<T, KV, D, 1>(a, stream);
-    case 32: return launch_few<T, KV, D, 2>(a, stream);
+    case 16: return launch_few<T, D, 1>(a, stream);
+    case 32: return launch_few<T, D, 2>(a, stream);
     default:
-      if constexpr (sizeof(T) == 2) launch_few<T, KV, D, 3>(a, stream);
+      if constexpr (sizeof(T) == 2) launch_few<T, D, 3>(a, stream);
   }
 }
 
-// Joins the parts of shared tiles after an attention kernel.
-hipError_t launch_merge(const PagedAttnArgs& a, hipStream_t stream) {
+}  // namespace
+
+PagedAttnShape paged_attn_shape(int dtype, int G, int max_new) {
+  const int64_t rows = (int64_t)max_new * G;
+  if (rows <= (dtype ? kFewRowsBf16 : kFewRowsF32)) return {16 * (int)((rows + 15) / 16), dtype ? 128 : 64};
+  return {128, dtype ? 64 : 32};
+}
+
+hipError_t launch_paged_few(const PagedAttnArgs& a, hipStream_t stream) {
+  if (a.dtype) a.D == 128 ? launch_few_rows<__bf16, 128>(a, stream) : launch_few_rows<__bf16, 64>(a, stream);
+  else a.D == 128 ? launch_few_rows<float, 128>(a, stream) : launch_few_rows<float, 64>(a, stream);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_merge(const PagedAttnArgs& a, hipStream_t stream) {
   prof_begin("paged_merge", stream);
   // A workgroup per row of a tile where that makes at most 4096, at least one per row group.
   const int rows = std::min(a.max_new, a.tokens) * a.G, entries = a.by_tile ? a.S * a.max_tiles : kPagedWorkers;
@@ -484,56 +435,12 @@ hipError_t launch_merge(const PagedAttnArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-}  // namespace
-
-PagedAttnShape paged_attn_shape(int dtype, int G, int max_new) {
-  const int64_t rows = (int64_t)max_new * G;
-  if (rows <= (dtype ? kFewRowsBf16 : kFewRowsF32)) return {16 * (int)((rows + 15) / 16), dtype ? 128 : 64};
-  return {128, dtype ? 64 : 32};
-}
-
-PagedAttnShape paged_attn_fp8_shape(int dtype, int G, int max_new) {
-  PagedAttnShape s = paged_attn_shape(dtype, G, max_new);
-  if (s.rows < 128) s.key_tile = 128;  // bytes: two 16-row groups a wave and step whatever the queries' type
-  return s;
-}
-
-hipError_t launch_paged_few(const PagedAttnArgs& a, hipStream_t stream) {
-  if (a.dtype) {
-    if (a.D == 128) launch_few_rows<__bf16, __bf16, 128>(a, stream);
-    else launch_few_rows<__bf16, __bf16, 64>(a, stream);
-  } else {
-    if (a.D == 128) launch_few_rows<float, float, 128>(a, stream);
-    else launch_few_rows<float, float, 64>(a, stream);
-  }
-  return hipGetLastError();
-}
-
-hipError_t launch_paged_few_fp8(const PagedAttnArgs& a, hipStream_t stream) {
-  if (a.dtype) {
-    if (a.D == 128) launch_few_rows<__bf16, E4m3, 128>(a, stream);
-    else launch_few_rows<__bf16, E4m3, 64>(a, stream);
-  } else {
-    if (a.D == 128) launch_few_rows<float, E4m3, 128>(a, stream);
-    else launch_few_rows<float, E4m3, 64>(a, stream);
-  }
-  return hipGetLastError();
-}
-
 hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream) {
   const bool few = a.tile_rows < 128;
   prof_begin("paged_attention", stream);
   hipError_t e = few ? launch_paged_few(a, stream) : launch_paged_many(a, stream);
   prof_end(stream);
-  return e != hipSuccess ? e : launch_merge(a, stream);
-}
-
-hipError_t launch_paged_attention_fp8(const PagedAttnArgs& a, hipStream_t stream) {
-  const bool few = a.tile_rows < 128;
-  prof_begin("paged_attention_fp8", stream);
-  hipError_t e = few ? launch_paged_few_fp8(a, stream) : launch_paged_many_fp8(a, stream);
-  prof_end(stream);
-  return e != hipSuccess ? e : launch_merge(a, stream);
+  return e != hipSuccess ? e : launch_paged_merge(a, stream);
 }
 
 }  // namespace sgdkv
