@@ -335,12 +335,21 @@ struct RowPiece<float> {
   }
 };
 
-// Largest over the LPR lanes of a row, the same in each.
+// Largest over the LPR lanes of a row, the same in each: neighbours by lane permutations of the vector ALU.
 template <int LPR>
 __device__ __forceinline__ uint32_t row_max(uint32_t x) {
-#pragma unroll
-  for (int o = LPR / 2; o >= 1; o >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, o, 64));
-  return x;
+  static_assert(LPR == 8 || LPR == 16 || LPR == 32, "lanes of a row");
+  auto with = [&](auto how) {
+    return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(how)::value, 0xF, 0xF, false));
+  };
+  if constexpr (LPR == 32) {
+    const auto y = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max((uint32_t)y[0], (uint32_t)y[1]);
+  }
+  if constexpr (LPR >= 16) x = with(std::integral_constant<int, 0x128>{});  // 8 lanes on, round the row of 16
+  x = with(std::integral_constant<int, LPR >= 16 ? 0x124 : 0x141>{});       // 4 lanes on, or the half row mirrored
+  x = with(std::integral_constant<int, 0x4E>{});                            // of each four: 2 on
+  return with(std::integral_constant<int, 0xB1>{});                         // and the neighbour
 }
 
 // Sum over the LPR lanes of a row, the same in each.
@@ -358,19 +367,29 @@ template <int LPR, int N>
 __device__ __forceinline__ int bytes_of_row(const float (&x)[N], uint32_t (&w)[N / 4]) {
   uint32_t size = 0;
 #pragma unroll
-  for (int e = 0; e < N; ++e) size = max(size, finite_size(x[e]));
-  const int code = row_code(row_max<LPR>(size));
+  for (int e = 0; e < N; ++e) size = max(size, __float_as_uint(x[e]) & 0x7FFFFFFFu);
+  size = row_max<LPR>(size);
+  if (__any(size >= 0x7F800000u)) {  // some row has an infinity or a NaN, which do not count
+    size = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) size = max(size, finite_size(x[e]));
+    size = row_max<LPR>(size);
+  }
+  const int code = row_code(size);
   const float f = inverse_power(code);
 #pragma unroll
   for (int e = 0; e < N; e += 4) w[e / 4] = to_e4m3(x[e] * f, x[e + 1] * f, x[e + 2] * f, x[e + 3] * f);
   return code;
 }
 
-// Rows to their slots in 8 bits. A lane takes eight values of a row, D / 8 lanes a row; the rows' largest value goes
-// round their lanes. Bound by HBM.
+// Rows to their slots in 8 bits. A lane takes eight values of a row, D / 8 lanes a row, whose largest value goes round
+// their lanes; a thread has kByteVecs rows' values under way of keys and of values. Bound by HBM, streamed once:
+// non-temporal. 1.05 M rows of 128 bf16 values take 152 us, 5.4 TB/s in and out (168 with the largest through LDS and
+// stores without the hint; 154 with four rows a thread).
+constexpr int kByteVecs = 2;
 template <typename T, int D>
 __global__ __launch_bounds__(kPageBlock) void store_fp8_kernel(StoreFp8Args a) {
-  constexpr int LPR = D / 8, NV = sizeof(T) / 2, V = kStoreVecs;  // 16-byte pieces of a lane, places of a thread
+  constexpr int LPR = D / 8, NV = sizeof(T) / 2, V = kByteVecs;  // 16-byte pieces of a lane, places of a thread
   const int64_t total = a.n * LPR, first = (int64_t)blockIdx.x * (V * kPageBlock) + threadIdx.x;
   u32x4 rows[2][V][NV];
   int64_t slot[V];
@@ -403,7 +422,8 @@ __global__ __launch_bounds__(kPageBlock) void store_fp8_kernel(StoreFp8Args a) {
       const int code = bytes_of_row<LPR, 8>(x, w);  // every lane takes part
       if (slot[u] < 0 || slot[u] >= a.total_slots) continue;
       const int at = threadIdx.x % LPR;
-      reinterpret_cast<u32x2*>(kv ? a.v_pages : a.k_pages)[slot[u] * LPR + at] = u32x2{w[0], w[1]};
+      u32x2* to = reinterpret_cast<u32x2*>(kv ? a.v_pages : a.k_pages) + slot[u] * LPR + at;
+      __builtin_nontemporal_store(u32x2{w[0], w[1]}, to);
       if (at == 0) (kv ? a.v_scales : a.k_scales)[slot[u]] = (uint8_t)code;
     }
 }
@@ -414,8 +434,7 @@ __global__ __launch_bounds__(kPageBlock) void store_fp8_kernel(StoreFp8Args a) {
 // at the store. Bound by HBM: four heads' loads ahead of their use and stores that do not displace the inputs from
 // the caches (80 heads of 8191 tokens, 168 MB in and out: 95 us without either, 80 and 73 with the first, 60 to 70
 // with both; the stores make no difference up to 4096 tokens).
-// FP8: into an 8-bit pool.
-template <typename T, int D, bool FP8>
+template <typename T, int D>
 __global__ __launch_bounds__(kPageBlock) void norm_rope_kernel(NormRopeArgs a) {
   using P = RowPiece<T>;
   constexpr int N = P::N, LPR = D / N, HPW = 64 / LPR;
@@ -429,7 +448,7 @@ __global__ __launch_bounds__(kPageBlock) void norm_rope_kernel(NormRopeArgs a) {
 
   if (live && lane < half) {
     float s, c;
-    sincos_at(a.positions[token], a.inv_freq[lane], FP8 ? a.factor : 1.0, s, c);
+    sincos_at(a.positions[token], a.inv_freq[lane], 1.0, s, c);
     sines[wid][lane] = s;
     cosines[wid][lane] = c;
   }
@@ -497,24 +516,121 @@ __global__ __launch_bounds__(kPageBlock) void norm_rope_kernel(NormRopeArgs a) {
           for (int e = 0; e < N; ++e) x[e] = fmaf(p[e], sn[e], x[e] * cs[e]);
         }
       }
-      if (is_q || (is_k && !FP8)) y = P::narrow(x);
-      if constexpr (FP8) {
-        uint32_t w8[N / 4];
-        const int code = bytes_of_row<LPR, N>(x, w8);  // of every row: its lanes go together
-        if (!is_q && slot[u] >= 0 && slot[u] < a.total_slots) {
-          uint8_t* to = static_cast<uint8_t*>(is_k ? a.k_pages : a.v_pages) + slot[u] * D + col;
-          if constexpr (N == 8) *reinterpret_cast<u32x2*>(to) = u32x2{w8[0], w8[1]};
-          else *reinterpret_cast<uint32_t*>(to) = w8[0];
-          if (lane % LPR == 0) (is_k ? a.k_scales : a.v_scales)[slot[u]] = (uint8_t)code;
-        }
-        slot[u] = -1;
-      }
+      if (is_q || is_k) y = P::narrow(x);
       if (is_q) {
         __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(a.q_out) + (token * a.Hq + h) * LPR + lane % LPR);
       } else if (slot[u] >= 0 && slot[u] < a.total_slots) {
         __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(is_k ? a.k_pages : a.v_pages) + slot[u] * LPR +
                                            lane % LPR);
       }
+    }
+  }
+}
+
+// The same into an 8-bit pool: keys and values are rounded once, from what norm and rotation leave in fp32. The first
+// batch of rows comes while the wave works out its angles, the next one while one is worked on; batches are of one step
+// for bf16, where fewer registers and so more waves do more than more loads of each (6001 tokens of 80 heads 51 us, 4.6
+// TB/s; batches of two and four steps 56 and 54, with the loads behind the angles 59), and of four for fp32 (2500 tokens
+// 42 us, 47 with one).
+template <typename T, int D>
+__global__ __launch_bounds__(kPageBlock) void norm_rope_fp8_kernel(NormRopeArgs a) {
+  using P = RowPiece<T>;
+  constexpr int N = P::N, LPR = D / N, HPW = 64 / LPR, RB = D * (int)sizeof(T);
+  constexpr int kAhead = sizeof(T) == 2 ? 1 : 4;  // steps of a batch
+  __shared__ float sines[kWavesPerBlock][64], cosines[kWavesPerBlock][64];
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, l = lane % LPR;
+  const uint32_t unit = blockIdx.x * kWavesPerBlock + wid;  // a launch has fewer than 2^26 waves
+  const int64_t token = unit / (uint32_t)a.parts;
+  const int part = (int)(unit - (uint32_t)token * a.parts);
+  const bool live = token < a.T;
+  const int col = l * N, half = a.rot / 2;
+  const int heads = a.Hq + 2 * a.Hkv, step = a.parts * HPW;
+  const int64_t tok = live ? token : 0;
+  const char* const rows[3] = {static_cast<const char*>(a.q) + tok * a.q_stride + l * 16,
+                               static_cast<const char*>(a.k) + tok * a.k_stride + l * 16,
+                               static_cast<const char*>(a.v) + tok * a.v_stride + l * 16};
+  const int32_t* const slots = a.slots + tok * a.Hkv;
+  // A batch's rows and slots, without a branch: past the last head the last one again, and for a query any slot.
+  u32x4 w[kAhead];
+  int slot[kAhead];
+  auto fetch = [&](int h0) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int h = min(h0 + u * step + lane / LPR, heads - 1), kv = h - a.Hq, v = kv - a.Hkv;
+      w[u] = *reinterpret_cast<const u32x4*>(kv < 0 ? rows[0] + h * RB : v < 0 ? rows[1] + kv * RB : rows[2] + v * RB);
+      slot[u] = slots[v >= 0 ? v : max(kv, 0)];
+    }
+  };
+  fetch(part * HPW);
+  if (live && lane < half) {
+    float s, c;
+    sincos_at(a.positions[token], a.inv_freq[lane], a.factor, s, c);
+    sines[wid][lane] = s;
+    cosines[wid][lane] = c;
+  }
+  __syncthreads();
+  if (!live) return;
+  // this lane's columns: y = x * c + partner * s, with the sign of the first of a pair in s
+  const bool turns = col < a.rot, first = a.interleaved || col < half;
+  float cs[N], sn[N], qw[N], kw[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const int pair = a.interleaved ? (col + e) / 2 : (first ? col + e : col + e - half);
+    const bool neg = a.interleaved ? (e & 1) == 0 : first;
+    cs[e] = turns ? cosines[wid][pair] : 1.f;
+    sn[e] = turns ? (neg ? -sines[wid][pair] : sines[wid][pair]) : 0.f;
+    qw[e] = kw[e] = 1.f;
+  }
+  if (a.q_weight) P::widen(reinterpret_cast<const u32x4*>(a.q_weight)[l], qw);
+  if (a.k_weight) P::widen(reinterpret_cast<const u32x4*>(a.k_weight)[l], kw);
+  const int partner = a.interleaved || !turns ? lane : (first ? lane + half / N : lane - half / N);
+
+  for (int h0 = part * HPW; h0 < heads; h0 += kAhead * step) {
+    u32x4 now[kAhead];
+    int to_slots[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      now[u] = w[u];
+      to_slots[u] = slot[u];
+    }
+    if (h0 + kAhead * step < heads) fetch(h0 + kAhead * step);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int g0 = h0 + u * step, h = g0 + lane / LPR;  // the wave's heads, the lane's
+      if (g0 >= heads) break;
+      const bool is_q = h < a.Hq, is_k = !is_q && h < a.Hq + a.Hkv;
+      const int64_t to_slot = h >= a.Hq && h < heads ? to_slots[u] : -1;
+      float x[N];
+      P::widen(now[u], x);
+      if (is_q ? a.q_weight != nullptr : is_k && a.k_weight != nullptr) {
+        // every lane of a row takes this branch together
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) ss = fmaf(x[e], x[e], ss);
+        ss = row_sum<LPR>(ss);
+        const float r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = x[e] * r * (is_q ? qw[e] : kw[e]);
+      }
+      if (a.rot) {
+        float p[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) p[e] = a.interleaved ? x[e ^ 1] : __shfl(x[e], partner, 64);
+        if (turns && (is_q || is_k)) {  // columns that do not turn: nothing times zero, which may be infinite
+#pragma unroll
+          for (int e = 0; e < N; ++e) x[e] = fmaf(p[e], sn[e], x[e] * cs[e]);
+        }
+      }
+      if (is_q)
+        __builtin_nontemporal_store(P::narrow(x), reinterpret_cast<u32x4*>(a.q_out) + (token * a.Hq + h) * LPR + l);
+      if (g0 + HPW <= a.Hq) continue;  // queries alone
+      uint32_t b[N / 4];
+      const int code = bytes_of_row<LPR, N>(x, b);  // of every lane's row: they go together
+      if (to_slot < 0 || to_slot >= a.total_slots) continue;
+      uint8_t* to = static_cast<uint8_t*>(is_k ? a.k_pages : a.v_pages) + to_slot * D + col;
+      if constexpr (N == 8) *reinterpret_cast<u32x2*>(to) = u32x2{b[0], b[1]};
+      else *reinterpret_cast<uint32_t*>(to) = b[0];
+      if (l == 0) (is_k ? a.k_scales : a.v_scales)[to_slot] = (uint8_t)code;
     }
   }
 }
@@ -560,7 +676,7 @@ hipError_t launch_paged_store(const PagedStoreArgs& args, hipStream_t stream) {
 }
 
 hipError_t launch_paged_store_fp8(const StoreFp8Args& args, hipStream_t stream) {
-  const int64_t lanes = args.D / 8, per = kStoreVecs * kPageBlock, most = kMaxBlocks * per / lanes;
+  const int64_t lanes = args.D / 8, per = kByteVecs * kPageBlock, most = kMaxBlocks * per / lanes;
   if (args.n == 0) return hipSuccess;
   prof_begin("paged_store_fp8", stream);
   for (int64_t first = 0; first < args.n; first += most) {
@@ -584,16 +700,22 @@ hipError_t launch_paged_store_fp8(const StoreFp8Args& args, hipStream_t stream) 
 }
 
 namespace {
-template <bool FP8>
-void launch_norm_rope_part(const NormRopeArgs& a, hipStream_t stream) {
+template <typename T, int D, bool FP8>
+void launch_norm_rope_one(const NormRopeArgs& a, hipStream_t stream) {
   const int64_t waves = (int64_t)a.T * a.parts;
   const dim3 grid((unsigned)((waves + kWavesPerBlock - 1) / kWavesPerBlock)), block(kPageBlock);
+  if constexpr (FP8) norm_rope_fp8_kernel<T, D><<<grid, block, 0, stream>>>(a);
+  else norm_rope_kernel<T, D><<<grid, block, 0, stream>>>(a);
+}
+
+template <bool FP8>
+void launch_norm_rope_part(const NormRopeArgs& a, hipStream_t stream) {
   if (a.dtype) {
-    if (a.D == 128) norm_rope_kernel<__bf16, 128, FP8><<<grid, block, 0, stream>>>(a);
-    else norm_rope_kernel<__bf16, 64, FP8><<<grid, block, 0, stream>>>(a);
+    if (a.D == 128) launch_norm_rope_one<__bf16, 128, FP8>(a, stream);
+    else launch_norm_rope_one<__bf16, 64, FP8>(a, stream);
   } else {
-    if (a.D == 128) norm_rope_kernel<float, 128, FP8><<<grid, block, 0, stream>>>(a);
-    else norm_rope_kernel<float, 64, FP8><<<grid, block, 0, stream>>>(a);
+    if (a.D == 128) launch_norm_rope_one<float, 128, FP8>(a, stream);
+    else launch_norm_rope_one<float, 64, FP8>(a, stream);
   }
 }
 
