@@ -102,24 +102,22 @@ struct ByteRows {
       code[i] = ld8(powers, r);
     }
   }
+  // Row i of the lane's to the tile at `to`.
   template <typename F>
-  __device__ __forceinline__ void store(char* to, int my_row, int lane, F swizzle) const {
+  __device__ __forceinline__ void store(int i, char* to, int my_row, int lane, F swizzle) const {
+    const int r = i * RPL + lane / VPR, c = lane % VPR;
+    if (RPL > S::RPW && r >= S::RPW) return;
+    char* row = to + (my_row + r) * S::RB;
+    const int sw = swizzle(my_row + r);
+    const float p = power_of(code[i]);
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int r = i * RPL + lane / VPR, c = lane % VPR;
-      if (RPL > S::RPW && r >= S::RPW) continue;
-      char* row = to + (my_row + r) * S::RB;
-      const int sw = swizzle(my_row + r);
-      const float p = power_of(code[i]);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const Frag<T> f = widen_piece<T>(raw[i][2 * e], raw[i][2 * e + 1], p);
-        if constexpr (sizeof(T) == 2) {
-          *reinterpret_cast<u32x4*>(row + ((2 * c + e) ^ sw) * 16) = f.v;
-        } else {
-          *reinterpret_cast<u32x4*>(row + ((4 * c + 2 * e) ^ sw) * 16) = f.v0;
-          *reinterpret_cast<u32x4*>(row + ((4 * c + 2 * e + 1) ^ sw) * 16) = f.v1;
-        }
+    for (int e = 0; e < 2; ++e) {
+      const Frag<T> f = widen_piece<T>(raw[i][2 * e], raw[i][2 * e + 1], p);
+      if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<u32x4*>(row + ((2 * c + e) ^ sw) * 16) = f.v;
+      } else {
+        *reinterpret_cast<u32x4*>(row + ((4 * c + 2 * e) ^ sw) * 16) = f.v0;
+        *reinterpret_cast<u32x4*>(row + ((4 * c + 2 * e + 1) ^ sw) * 16) = f.v1;
       }
     }
   }
@@ -209,10 +207,15 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
     for (int i = 0; i < NL; ++i) load_to_lds(vr, voff[i], to + S::TILE + i * 1024);
   };
   // The rows under way into LDS (those of other pools are there already).
+  constexpr int NB = 2 * ByteRows<T, D>::NL;
+  auto arrive_part = [&](int j, int i) {
+    if (i < NB / 2) kbytes.store(i, lds[j & 1][0], my_row, lane, S::key_swizzle);
+    else vbytes.store(i - NB / 2, lds[j & 1][1], my_row, lane, S::value_swizzle);
+  };
   auto arrive = [&](int j) {
     if constexpr (FP8) {
-      kbytes.store(lds[j & 1][0], my_row, lane, S::key_swizzle);
-      vbytes.store(lds[j & 1][1], my_row, lane, S::value_swizzle);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) arrive_part(j, i);
     } else {
       wait_loads();
     }
@@ -450,6 +453,11 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
             for (int d = 0; d < ND; ++d)
               o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[t & 1][d]),
                                                              __builtin_bit_cast(bf16x8, piece[k]), o[d], 0, 0, 0);
+          // 8-bit pools: the next tile's rows are widened beside these products. (After the last tile they are old
+          // ones, to a buffer that nobody reads any more.)
+          if constexpr (FP8) {
+            if (t >= KT / 16 - NB) arrive_part(key0 / KT + 1, t - (KT / 16 - NB));
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
       } else {
@@ -482,7 +490,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
         const int page2 = group_page(a, table, (j + 2) * KT + my_row, limit);
         if (j + 1 < now.j1) load(now, j + 1);
         if (j * KT < hi) attend(lds[j & 1][0], edge, j * KT, j == now.j0);
-        if (!FP8 || j + 1 < now.j1) arrive(j + 1);
+        if (!FP8 || EB == 4 || j * KT >= hi) arrive(j + 1);
         page = uniform(page2);
         __syncthreads();
       }
