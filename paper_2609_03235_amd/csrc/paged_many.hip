@@ -131,11 +131,14 @@ struct ManyTile {
   bool own;        // not shared
 };
 
-// KV: the pool's rows, T or E4m3.
-template <typename T, typename KV, int D, bool FINE>
+// KV: the pool's rows, T or E4m3. QT: bf16 terms of a query; 3 of them hold an fp32 one, so that fp32 queries over an
+// 8-bit pool take bf16 products, three times as many at nine times the rate (3 x 300 tokens over 3000 rows of 64 columns
+// 33 us, 2048 over 8000 120; with fp32 products 49 and 307). There are registers for that where rows have 64 columns.
+template <typename T, typename KV, int D, bool FINE, int QT = 1>
 __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs a) {
   using S = ManyShape<T, D>;
   constexpr bool FP8 = sizeof(KV) == 1;
+  constexpr int QRB = QT == 1 ? S::RB : D * 4;  // bytes of a query
   constexpr int EB = S::EB, RB = S::RB, KT = S::KT, NC = S::NC, NK = S::NK, ND = S::ND, NL = S::NL;
   constexpr int M = 128;
   __shared__ __attribute__((aligned(16))) char lds[2][2][S::TILE];  // two buffers of keys and values
@@ -189,7 +192,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
   const int r = wid * 32 + lq, tok = r / a.G, hd = r - tok * a.G;  // the lane's row of a tile
   const int32_t* table;
   int page;
-  u32x4 q[NC];
+  u32x4 q[QT][NC], qraw[QT == 1 ? 1 : 2 * NC];
   ByteRows<T, D> kbytes, vbytes;  // 8-bit pools: of the tile under way
   auto load = [&](const ManyTile& t, int j) {
     const int r0 = j * KT + my_row;
@@ -231,12 +234,17 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
     page = page2;
     const int tok0 = t.at.tile * a.tokens, ntok = min(a.tokens, t.at.g.n - tok0);
     const rsrc_t qr = make_rsrc(
-        static_cast<const char*>(a.q) + ((int64_t)(t.at.g.t0 + tok0) * a.Hq + t.at.seg % a.Hkv * a.G) * RB,
-        ((uint64_t)(ntok - 1) * a.Hq + a.G) * RB);
-    uint32_t from = r < ntok * a.G ? (uint32_t)((tok * a.Hq + hd) * RB + 16 * half) : 0xFFFFF000u;  // or past the end
+        static_cast<const char*>(a.q) + ((int64_t)(t.at.g.t0 + tok0) * a.Hq + t.at.seg % a.Hkv * a.G) * QRB,
+        ((uint64_t)(ntok - 1) * a.Hq + a.G) * QRB);
+    uint32_t from = r < ntok * a.G ? (uint32_t)((tok * a.Hq + hd) * QRB + (QT == 1 ? 16 : 32) * half) : 0xFFFFF000u;  // or past the end
     asm("" : "+v"(from));  // one path for both: the compiler makes two of every load otherwise
+    if constexpr (QT == 1) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) q[c] = ld128(qr, from + 32 * c);
+      for (int c = 0; c < NC; ++c) q[0][c] = ld128(qr, from + 32 * c);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 2 * NC; ++c) qraw[c] = ld128(qr, from + 64 * (c / 2) + 16 * (c % 2));
+    }
     if (tid < D) odd[which][tid] = 0x7FFFFFFF;
   };
 
@@ -295,7 +303,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
             }
           }
         };
-        if (FINE || (EB == 4 && !a.out_dtype)) store(float{});
+        if ((FINE && QT == 1) || ((EB == 4 || QT == 3) && !a.out_dtype)) store(float{});
         else store(__bf16{});
         if (on && a.lse && half == 0) a.lse[row0 + tok * a.Hq + hd] = lse_of(m, s);
       } else if (on) {
@@ -362,10 +370,12 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
           if (g + 1 < NK * NC / 4) read(g + 1);
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            y[e % NK] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[g & 1][e]),
-                                                                __builtin_bit_cast(bf16x8, q[2 * g + e / NK]),
-                                                                y[e % NK], 0, 0, 0);
+          for (int k = 0; k < QT; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              y[e % NK] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[g & 1][e]),
+                                                                  __builtin_bit_cast(bf16x8, q[k][2 * g + e / NK]),
+                                                                  y[e % NK], 0, 0, 0);
           __builtin_amdgcn_sched_barrier(0);
         }
       } else {
@@ -376,7 +386,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
             const u32x4 kf = key(n, c);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              y[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(q[c][e]), y[n], 0, 0,
+              y[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(q[0][c][e]), y[n], 0, 0,
                                                           0);
           }
       }
@@ -480,7 +490,20 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
     arrive(now.j0);
     // Tells the compiler that the queries are there too: it would wait for them in the loop, and so for its loads.
 #pragma unroll
-    for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(q[c]));
+    for (int c = 0; c < NC; ++c) {
+      if constexpr (QT == 1) {
+        asm volatile("" : "+v"(q[0][c]));
+      } else {
+        u32x4 terms[3];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const u32x4 x = qraw[2 * c + e / 2];
+          split_bf16(__uint_as_float(x[2 * (e % 2)]), __uint_as_float(x[2 * (e % 2) + 1]), terms, e);
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) q[k][c] = terms[k];
+      }
+    }
     __syncthreads();
     // the tiles that every row sees whole, then the others
     int j = now.j0;
@@ -522,7 +545,8 @@ hipError_t launch_paged_many(const PagedAttnArgs& a, hipStream_t stream) {
 
 hipError_t launch_paged_many_fp8(const PagedAttnArgs& a, hipStream_t stream) {
   if (a.dtype) a.D == 128 ? launch_many<__bf16, E4m3, 128>(a, stream) : launch_many<__bf16, E4m3, 64>(a, stream);
-  else a.D == 128 ? launch_many<float, E4m3, 128>(a, stream) : launch_many<float, E4m3, 64>(a, stream);
+  else if (a.D == 128) launch_many<float, E4m3, 128>(a, stream);
+  else paged_many_kernel<__bf16, E4m3, 64, true, 3><<<dim3(kPagedWorkers), dim3(kAttnBlock), 0, stream>>>(a);
   return hipGetLastError();
 }
 
