@@ -319,7 +319,7 @@ def test_paged_attention_fp8_far_logits(new, spread, dtype):
 
 
 @pytest.mark.parametrize("new", [[1], [3], [40]])
-@pytest.mark.parametrize("low,high", [(-100, -70), (60, 90), (-40, 40)])
+@pytest.mark.parametrize("low,high", [(-124, -112), (-100, -70), (60, 90), (-40, 40)])
 def test_paged_attention_fp8_powers(new, low, high):
     """Values whose rows' powers lie far from 1, and far from each other."""
     _say(f"powers {new} {low} to {high}")
@@ -685,3 +685,64 @@ def test_two_captured_fp8_calls_share_a_workspace():
             eager = c.call()
             torch.cuda.synchronize()
             assert torch.equal(out, wo) and torch.equal(lse, wl) and torch.equal(eager[0], wo)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("new", [[1], [20], [70]])
+def test_fp8_table_of_repeated_pages_past_2_to_25_rows(new, dtype):
+    """A segment of 40 million rows whose table names the same 64 pages over and over: its softmax is that of the
+    pages' rows, each many times, so out is that of one round of them and lse larger by the log of the rounds. A worker
+    adds 79000 rows, 16 or more at a time per lane group and product: 2500 roundings at most meet in a sum."""
+    _say(f"long table {new} {dtype}")
+    d, page, P, rounds = 64, 1024, 64, 620
+    g = torch.Generator(device=DEV).manual_seed(0)
+    pool = pool_of(P, page, d)
+    k, v = (torch.randn(P * page, d, generator=g, device=DEV) for _ in range(2))
+    sg.paged_store_fp8(k, v, torch.arange(P * page, dtype=torch.int32, device=DEV), *pool)
+    kd, vd = decoded(pool[0], pool[2]).view(-1, d), decoded(pool[1], pool[3]).view(-1, d)
+    tables = torch.arange(P, dtype=torch.int32, device=DEV).repeat(rounds)[None].contiguous()
+    q = torch.randn(sum(new), 4, d, generator=g, device=DEV).to(dtype)
+    out, lse = sg.paged_attention_fp8(q, *pool, tables, _i32([P * page * rounds]), _i32([0, len(q)]), 1,
+                                      max_new=max(new), causal=False, out_dtype=F32)
+    y = q.double().flatten(0, 1) @ kd.T / 8
+    want, wlse = torch.softmax(y, 1) @ vd, torch.logsumexp(y, 1) + math.log(rounds)
+    assert (out.double().flatten(0, 1) - want).abs().max() < 2500 * 2.0 ** -24 + 2e-5
+    assert (lse.double().flatten() - wlse).abs().max() < 2500 * 2.0 ** -24 + 2e-5
+
+
+def test_fp8_shared_pages_and_padding():
+    """Two sequences whose tables name the same pages read the same rows; tokens behind the last sequence's keep what
+    out and lse held."""
+    _say("shared pages")
+    c = Case8([1, 3], [500, 90, 500, 90], 8, 2, 128, 16, BF, seed=51, pad=5)
+    c.tables[2:] = c.tables[:2]
+    c.k[2:], c.v[2:] = c.k[:2], c.v[:2]
+    out, lse = torch.full((c.T, 8, 128), 9.0, device=DEV), torch.full((c.T, 8), 9.0, device=DEV)
+    c.call(out_dtype=F32, out=out, lse=lse)
+    c.check(out, lse)
+    assert (out[4:] == 9.0).all() and (lse[4:] == 9.0).all()
+
+
+def test_norm_rope_store_fp8_of_more_tokens_than_a_launch_holds():
+    """2^26 + 37 tokens, a wave each, go in several launches; tokens around each power of two from 2^24 on are
+    compared, and the slots of the others are -1."""
+    _say("norm_rope_fp8 of 2^26 + 37 tokens")
+    T, d = 2**26 + 37, 64
+    g = torch.Generator(device=DEV).manual_seed(4)
+    k = torch.zeros(T, 1, d, device=DEV, dtype=BF)
+    pos = torch.zeros(T, device=DEV, dtype=torch.int32)
+    slots = torch.full((T, 1), -1, device=DEV, dtype=torch.int32)
+    some = torch.tensor([0, *(2**i + j for i in (24, 25, 26) for j in (-1, 0, 1)), T - 1], device=DEV)
+    k[some] = torch.randn(len(some), 1, d, generator=g, device=DEV).to(BF)
+    pos[some] = (some % 100003).to(torch.int32)
+    slots[some, 0] = torch.arange(len(some), device=DEV, dtype=torch.int32)
+    inv = (1e4 ** (-torch.arange(0, d, 2, device=DEV) / d)).float()
+    a, b = pool_of(1, 16, d), pool_of(1, 16, d)
+    out = sg.norm_rope_store_fp8(k, k, k, pos, slots, *a, inv_freq=inv)
+    want = sg.norm_rope_store_fp8(k[some], k[some], k[some], pos[some], slots[some], *b, inv_freq=inv)
+    assert torch.equal(out[some], want)
+    for x, y in zip(a, b):
+        assert torch.equal(x.view(U8), y.view(U8))
+    rows = _plain_rope(k[some], None, pos[some], inv, 0.0, False)
+    (kn, kc), _ = rows_of(b, slots[some, 0], d)
+    _check_bytes(kn, kc, rows[:, 0], 2 ** 0.5 * rows[:, 0].abs().amax(-1, keepdim=True), 32)
