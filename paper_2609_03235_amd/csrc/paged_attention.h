@@ -247,14 +247,12 @@ __device__ __forceinline__ u32x4 group_words(const PagedAttnArgs& a, const void*
 }
 
 // The codes of the same rows (8-bit pools), one byte each. A code may mean NaN where no row is, and NaN times the zeros
-// read there is NaN: those who use a code before the masks read none past the last row (zero, a power that zeros do
-// not mind). With ROUND, for reads of four codes at once, all 16 of the group are there: they lie in its page.
-template <bool ROUND>
+// read there is NaN: none past the last row is read (zero, a power that zeros do not mind).
 __device__ __forceinline__ rsrc_t code_rsrc(const PagedAttnArgs& a, const uint8_t* codes, int page, int r0, int valid,
                                             int rows) {
   const bool ok = page >= 0 && page < a.num_pages && valid > 0;
   const int64_t row = ok ? ((int64_t)page << a.page_shift) + (r0 & ((1 << a.page_shift) - 1)) : 0;
-  return make_rsrc(codes + row, ok ? (ROUND ? 16 : min(valid, rows)) : 0);
+  return make_rsrc(codes + row, ok ? min(valid, rows) : 0);
 }
 
 // 64 x 16 bytes from a buffer into LDS at lds + 16 * lane; out-of-range lanes write zeros. The compiler does not

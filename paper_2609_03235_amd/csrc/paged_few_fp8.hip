@@ -34,6 +34,10 @@ struct FewBytes {
   }
 };
 
+__device__ __forceinline__ rsrc_t rows_buffer(const void* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, bytes, kRsrcWord3);
+}
+
 // Eight columns of a query row from `off` on, as QT terms of bf16; `flip` holds the sign bits of a negative scale.
 template <int QT>
 __device__ __forceinline__ void query_terms(rsrc_t qr, uint32_t off, uint32_t flip, Frag<__bf16> (&to)[QT]) {
@@ -185,16 +189,22 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_fp8_kernel(PagedAttnA
       u32x4 raw[U][NK];             // the keys as they come: 16 numbers of row lr
       uint32_t kcode[U], vcode[U];  // the codes of row lr, and of rows 4lg .. 4lg + 3
       auto load = [&](int j, int u) {
-        const int r = first_row(j) + 16 * u, pg = uniform(page[u]), valid = stop - r;
+        // the group's rows: none of a page outside the pool or past the last one (all scalar, from one row number)
+        const int r = first_row(j) + 16 * u, pg = uniform(page[u]);
+        const bool ok = (uint32_t)pg < (uint32_t)a.num_pages && r < stop;
+        const int n = ok ? min(stop - r, 16) : 0;
+        const int64_t row = ok ? ((int64_t)pg << a.page_shift) + (r & ((1 << a.page_shift) - 1)) : 0;
+        const uint64_t vp = reinterpret_cast<uint64_t>(a.v_pages) + row * D;
+        const u32x4 vr = {(uint32_t)vp, (uint32_t)(vp >> 32), (uint32_t)(n * D), (uint32_t)kRsrcWord3};
         const uint32_t to = uniform((int)(stage0 + (j & 1) * STAGE)) + u * 16 * D;
-        const u32x4 vr = group_words(a, a.v_pages, pg, r, valid, 16, D);
 #pragma unroll
         for (int i = 0; i < NV; ++i) load_to_lds_nt(vr, voff[u % 2][i], to + i * 1024);
-        const rsrc_t kr = group_rsrc(a, a.k_pages, pg, r, valid, D);
+        const rsrc_t kr = rows_buffer(static_cast<const char*>(a.k_pages) + row * D, n * D);
 #pragma unroll
         for (int c = 0; c < NK; ++c) raw[u][c] = ld128_nt(kr, (uint32_t)(lr * D + 64 * c + 16 * lg));
-        kcode[u] = ld8(code_rsrc<false>(a, a.k_scales, pg, r, valid, 16), lr);
-        vcode[u] = ld32(code_rsrc<true>(a, a.v_scales, pg, r, valid, 16), 4 * lg);
+        // Of the values' codes all 16 are read, four at once; those past the last row go to no result.
+        kcode[u] = ld8(rows_buffer(a.k_scales + row, n), lr);
+        vcode[u] = ld32(rows_buffer(a.v_scales + row, ok ? 16 : 0), 4 * lg);
       };
 #pragma unroll
       for (int u = 0; u < U; ++u) load(0, u);

@@ -94,7 +94,7 @@ struct ByteRows {
   __device__ __forceinline__ void load(const PagedAttnArgs& a, const void* pool, const uint8_t* codes, int page, int r0,
                                        int valid, int lane) {
     const rsrc_t rows = rows_rsrc(a, pool, page, r0, valid, S::RPW, D);
-    const rsrc_t powers = code_rsrc<false>(a, codes, page, r0, valid, S::RPW);
+    const rsrc_t powers = code_rsrc(a, codes, page, r0, valid, S::RPW);
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int r = i * RPL + lane / VPR;
