@@ -576,9 +576,12 @@ sgdkv_status sgdkv_paged_attention_fp8_workspace_size(const sgdkv_page_pool_fp8*
 /* sgdkv_paged_attention over such a pool: q is row_dtype, and the rows' values
  * enter the formula as they are held, none rounded again. Rows past a segment's
  * last one and the codes of those are not read into a result, whatever they
- * hold. Probabilities as there; a value that is not finite makes the outputs of
- * its column, of the tokens that see its row, not finite, and no others; a row
- * of code 255 (e8m0's NaN) all columns'.
+ * hold. Probabilities keep their fp32 bits but for bf16 out of bf16 q: there
+ * each is off by 2^-16 of itself at most, and with more than 48 query rows per
+ * KV head (min(max_new, T) * Hq/Hkv) rounded to bf16. Sums are fp32, of
+ * products up to 2^10 times a row's values. A value that is not finite makes
+ * the outputs of its column, of the tokens that see its row, not finite, and no
+ * others; a row of code 255 (e8m0's NaN) all columns'.
  * Errors (nothing enqueued): those of sgdkv_paged_attention. */
 sgdkv_status sgdkv_paged_attention_fp8(const sgdkv_page_pool_fp8* pool, const sgdkv_paged_desc* desc, const void* q,
                                        const int32_t* tables, const int32_t* rows, const int32_t* cu_new, void* out,

@@ -30,25 +30,10 @@ template <int HI>
 __device__ __forceinline__ uint32_t e4m3_to_bf16(uint32_t w, float power) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, HI));
 }
-template <int HI>
-__device__ __forceinline__ f32x2 e4m3_to_f32(uint32_t w, float power) {
-  return __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, power, HI));
-}
-
 // Eight numbers (two words) as an operand.
-template <typename T>
-__device__ __forceinline__ Frag<T> widen_piece(uint32_t w0, uint32_t w1, float power) {
-  Frag<T> f;
-  if constexpr (sizeof(T) == 2) {
-    f.v = u32x4{e4m3_to_bf16<0>(w0, power), e4m3_to_bf16<1>(w0, power), e4m3_to_bf16<0>(w1, power),
-                e4m3_to_bf16<1>(w1, power)};
-  } else {
-    const f32x2 a = e4m3_to_f32<0>(w0, power), b = e4m3_to_f32<1>(w0, power);
-    const f32x2 c = e4m3_to_f32<0>(w1, power), d = e4m3_to_f32<1>(w1, power);
-    f.v0 = u32x4{__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y)};
-    f.v1 = u32x4{__float_as_uint(c.x), __float_as_uint(c.y), __float_as_uint(d.x), __float_as_uint(d.y)};
-  }
-  return f;
+__device__ __forceinline__ Frag<__bf16> widen_piece(uint32_t w0, uint32_t w1, float power) {
+  return {u32x4{e4m3_to_bf16<0>(w0, power), e4m3_to_bf16<1>(w0, power), e4m3_to_bf16<0>(w1, power),
+                e4m3_to_bf16<1>(w1, power)}};
 }
 
 // |x| where it counts for the row's power.

@@ -136,7 +136,8 @@ __device__ __forceinline__ I block_prefix(I mine, int64_t* wave_sum, I& total) {
 // PAD (segments of one tile): where all workers' least pieces cover the segments rounded up to whole pieces,
 // the line is that, and no worker has parts of two tiles. Short calls are bound by latency: one token over four
 // segments of 8K rows took 14.9 us with, 10.4 without the three workers that had two.
-template <bool PAD>
+// ONE: every call's segments have one tile at most.
+template <bool PAD, bool ONE = true>
 __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, LineScratch& sc, int w, int64_t& share,
                                            int64_t& end, bool& padded, LineTile& at) {
   const int tid = threadIdx.x;
@@ -158,6 +159,7 @@ __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, LineScratch& 
     int n;
     run = (int64_t)block_prefix(pieces, sc.wave_sum, n) << a.min_shift;
     padded = uniform(n) <= kPagedWorkers;
+    if constexpr (!ONE) padded &= a.max_tiles == 1;
     all = (int64_t)uniform(n) << a.min_shift;
     if (!padded) __syncthreads();
   }

@@ -58,9 +58,9 @@ __device__ __forceinline__ void query_terms(rsrc_t qr, uint32_t off, uint32_t fl
   for (int t = 0; t < QT; ++t) to[t].v ^= flip;
 }
 
-// QT: terms of a query (1: bf16, 3: fp32). QB: 16-row query blocks of a full tile. FINE (fp32 output): the probabilities
-// go in as three bf16 terms, all their bits; for bf16 output as two, off by 2^-16 of each (16 x 6 tokens over 25K rows,
-// 64 / 8 heads, 230 us and 205).
+// QT: terms of a query (1: bf16, 3: fp32). QB: 16-row query blocks of a full tile. FINE: the
+// probabilities go in as three bf16 terms, all their bits; for bf16 output of bf16 queries as two, off by 2^-16 of each
+// (16 x 6 tokens over 25K rows, 64 / 8 heads, 225 us and 205).
 // A wave's step is U 16-row groups, 2 or UMAX of them: with 4, twice the bytes are under way (40 x 1 tokens over 30K
 // rows 222 us, 206 so), and a worker with no more than one key tile has all its waves at work with 2 (1 token over 9K
 // rows 15.6 us, 17.2 with 4).
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_fp8_kernel(PagedAttnA
   bool padded;
   LineTile at;
   if (!a.by_tile && tid == 0) a.shared[w] = make_int4(0, 0, 0, -1);
-  if (!find_piece<true>(a, sc, w, share, end, padded, at)) return;
+  if (!find_piece<true, QT == 1>(a, sc, w, share, end, padded, at)) return;
   int64_t pos = share * w;
   char* stage = lds[wid];
   const uint32_t stage0 = lds_address(stage);
@@ -229,7 +229,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_fp8_kernel(PagedAttnA
           const float kpow = power_of(kcode[u]);
 #pragma unroll
           for (int c = 0; c < NC; ++c)
-            k[u][c] = widen_piece<__bf16>(raw[u][c / 2][2 * (c % 2)], raw[u][c / 2][2 * (c % 2) + 1], kpow);
+            k[u][c] = widen_piece(raw[u][c / 2][2 * (c % 2)], raw[u][c / 2][2 * (c % 2) + 1], kpow);
 #pragma unroll
           for (int i = 0; i < 4; ++i) vpow[u][i] = power_of(vcode[u] >> 8 * i & 0xFF);
 #pragma unroll
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_fp8_kernel(PagedAttnA
 #pragma unroll
           for (int d = 0; d < ND; ++d) {
             const u32x2 v = lds_transposed8(vp + u * 16 * D + ((d ^ S::swizzle(row)) * 16));
-            const Frag<__bf16> vt = widen_piece<__bf16>(v.x, v.y, 1.f);
+            const Frag<__bf16> vt = widen_piece(v.x, v.y, 1.f);
 #pragma unroll
             for (int k = 0; k < PT; ++k)
 #pragma unroll
@@ -394,8 +394,13 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_fp8_kernel(PagedAttnA
 template <int D, int QT, int QB>
 void launch_few(const PagedAttnArgs& a, hipStream_t stream) {
   const dim3 grid(kPagedWorkers), block(kAttnBlock);
-  if (a.out_dtype) paged_few_fp8_kernel<D, QT, QB, false><<<grid, block, 0, stream>>>(a);
-  else paged_few_fp8_kernel<D, QT, QB, true><<<grid, block, 0, stream>>>(a);
+  if constexpr (QT == 1) {
+    if (a.out_dtype) {
+      paged_few_fp8_kernel<D, QT, QB, false><<<grid, block, 0, stream>>>(a);
+      return;
+    }
+  }
+  paged_few_fp8_kernel<D, QT, QB, true><<<grid, block, 0, stream>>>(a);
 }
 
 template <int D, int QT>
@@ -409,10 +414,18 @@ void launch_few_rows(const PagedAttnArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-PagedAttnShape paged_attn_fp8_shape(int dtype, int G, int max_new) {
+// More rows than a tile of few holds: tiles of 128 (paged_many.hip) but for fp32 queries of 128 columns, whose three
+// terms have no room beside 128 rows' other registers: those take several tiles of few rows. (16 x 16 tokens over 25K
+// rows, 64 / 8 heads, 670 us, 2048 over 8000, 28 / 4, 830, 3 x 50 over 1000, 4 / 2, 28; with tiles of 128 and fp32
+// products 1575, 1967 and 37.)
+PagedAttnShape paged_attn_fp8_shape_64(int, int G, int max_new) {
   const int64_t rows = (int64_t)max_new * G;
   if (rows <= kFewRows) return {16 * (int)((rows + 15) / 16), kKeyTile};
-  return {128, dtype ? 64 : 32};
+  return {128, 64};
+}
+PagedAttnShape paged_attn_fp8_shape_128(int dtype, int G, int max_new) {
+  const PagedAttnShape s = paged_attn_fp8_shape_64(dtype, G, max_new);
+  return dtype || s.rows < 128 ? s : PagedAttnShape{kFewRows, kKeyTile};
 }
 
 hipError_t launch_paged_few_fp8(const PagedAttnArgs& a, hipStream_t stream) {

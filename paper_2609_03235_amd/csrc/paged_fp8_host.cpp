@@ -25,14 +25,8 @@ sgdkv_status plan(const sgdkv_page_pool_fp8* pool, const sgdkv_paged_desc* d, Pa
   if (pool->reserved != 0) return fail(SGDKV_ERR_INVALID_ARG, "pool reserved must be 0");
   if (sgdkv_status st = check_dtype(pool->row_dtype, "pool row_dtype")) return st;
   if (sgdkv_status st = check_head_dim(pool->head_dim)) return st;
-  if (sgdkv_status st = plan_paged(pool->row_dtype, pool->head_dim, paged_attn_fp8_shape, d, a, bytes)) return st;
-  if (a.dtype == SGDKV_DTYPE_F32 && a.D == 64 && a.tile_rows == 128) {
-    // bf16 products, as bf16 queries take. (20 x 60 tokens over 300 rows 26.5 us with 128 keys for what a tile takes,
-    // 29.7 with 256, 32 with 64; 5 x 37 over 900 22.7, 25.5 and 21.5.)
-    a.key_tile = 64;
-    a.min_shift = log2_of(128);
-  }
-  return SGDKV_OK;
+  const auto shape = pool->head_dim == 128 ? paged_attn_fp8_shape_128 : paged_attn_fp8_shape_64;
+  return plan_paged(pool->row_dtype, pool->head_dim, shape, d, a, bytes);
 }
 
 }  // namespace

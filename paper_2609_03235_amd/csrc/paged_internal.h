@@ -131,8 +131,9 @@ struct PagedAttnShape {
 };
 PagedAttnShape paged_attn_shape(int dtype, int G, int max_new);
 hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream);
-// The same over a pool in 8 bits; dtype is the queries'.
-PagedAttnShape paged_attn_fp8_shape(int dtype, int G, int max_new);
+// The same over a pool in 8 bits, for rows of 64 and 128 columns; dtype is the queries'.
+PagedAttnShape paged_attn_fp8_shape_64(int dtype, int G, int max_new);
+PagedAttnShape paged_attn_fp8_shape_128(int dtype, int G, int max_new);
 hipError_t launch_paged_attention_fp8(const PagedAttnArgs& a, hipStream_t stream);
 
 }  // namespace sgdkv

@@ -84,11 +84,12 @@ struct Probs<__bf16, true, NK> : Probs<float, false, NK> {
 };
 
 // Rows of an 8-bit pool on their way to LDS: a wave's share of a tile, a lane's 16 numbers of NL rows, which are
-// widened to T on the way (row `row` of the wave's, piece `col` of 16 numbers).
-template <typename T, int D>
+// widened to bf16 on the way. (A write's lanes touch every other piece of a row, and so half of the banks twice; eight
+// numbers a lane, whose writes touch all once, take twice the loads: 2 x 6000 tokens over 20K rows 9.35 ms, 9.62 so.)
+template <int D>
 struct ByteRows {
-  using S = ManyShape<T, D>;
-  static constexpr int VPR = D / 16, RPL = 64 / VPR, NL = (S::RPW + RPL - 1) / RPL;
+  using S = ManyShape<__bf16, D>;
+  static constexpr int VPR = D / 16, RPL = 64 / VPR, NL = S::RPW / RPL;
   u32x4 raw[NL];
   uint32_t code[NL];
   __device__ __forceinline__ void load(const PagedAttnArgs& a, const void* pool, const uint8_t* codes, int page, int r0,
@@ -105,21 +106,13 @@ struct ByteRows {
   // Row i of the lane's to the tile at `to`.
   template <typename F>
   __device__ __forceinline__ void store(int i, char* to, int my_row, int lane, F swizzle) const {
-    const int r = i * RPL + lane / VPR, c = lane % VPR;
-    if (RPL > S::RPW && r >= S::RPW) return;
-    char* row = to + (my_row + r) * S::RB;
-    const int sw = swizzle(my_row + r);
+    const int r = my_row + i * RPL + lane / VPR, c = lane % VPR, sw = swizzle(r);
+    char* row = to + r * S::RB;
     const float p = power_of(code[i]);
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const Frag<T> f = widen_piece<T>(raw[i][2 * e], raw[i][2 * e + 1], p);
-      if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<u32x4*>(row + ((2 * c + e) ^ sw) * 16) = f.v;
-      } else {
-        *reinterpret_cast<u32x4*>(row + ((4 * c + 2 * e) ^ sw) * 16) = f.v0;
-        *reinterpret_cast<u32x4*>(row + ((4 * c + 2 * e + 1) ^ sw) * 16) = f.v1;
-      }
-    }
+    for (int e = 0; e < 2; ++e)
+      *reinterpret_cast<u32x4*>(row + ((2 * c + e) ^ sw) * 16) =
+          widen_piece(raw[i][2 * e], raw[i][2 * e + 1], p).v;
   }
 };
 
@@ -131,7 +124,7 @@ struct ManyTile {
   bool own;        // not shared
 };
 
-// KV: the pool's rows, T or E4m3. QT: bf16 terms of a query; 3 of them hold an fp32 one, so that fp32 queries over an
+// KV: the pool's rows, T or, for bf16 products, E4m3. QT: bf16 terms of a query; 3 of them hold an fp32 one, so that fp32 queries over an
 // 8-bit pool take bf16 products, three times as many at nine times the rate (3 x 300 tokens over 3000 rows of 64 columns
 // 33 us, 2048 over 8000 120; with fp32 products 49 and 307). There are registers for that where rows have 64 columns.
 template <typename T, typename KV, int D, bool FINE, int QT = 1>
@@ -193,7 +186,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
   const int32_t* table;
   int page;
   u32x4 q[QT][NC], qraw[QT == 1 ? 1 : 2 * NC];
-  ByteRows<T, D> kbytes, vbytes;  // 8-bit pools: of the tile under way
+  ByteRows<D> kbytes, vbytes;  // 8-bit pools: of the tile under way
   auto load = [&](const ManyTile& t, int j) {
     const int r0 = j * KT + my_row;
     if constexpr (FP8) {
@@ -210,7 +203,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
     for (int i = 0; i < NL; ++i) load_to_lds(vr, voff[i], to + S::TILE + i * 1024);
   };
   // The rows under way into LDS (those of other pools are there already).
-  constexpr int NB = 2 * ByteRows<T, D>::NL;
+  constexpr int NB = 2 * ByteRows<D>::NL;
   auto arrive_part = [&](int j, int i) {
     if (i < NB / 2) kbytes.store(i, lds[j & 1][0], my_row, lane, S::key_swizzle);
     else vbytes.store(i - NB / 2, lds[j & 1][1], my_row, lane, S::value_swizzle);
@@ -513,7 +506,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
         const int page2 = group_page(a, table, (j + 2) * KT + my_row, limit);
         if (j + 1 < now.j1) load(now, j + 1);
         if (j * KT < hi) attend(lds[j & 1][0], edge, j * KT, j == now.j0);
-        if (!FP8 || EB == 4 || j * KT >= hi) arrive(j + 1);
+        if (!FP8 || j * KT >= hi) arrive(j + 1);
         page = uniform(page2);
         __syncthreads();
       }
@@ -544,8 +537,8 @@ hipError_t launch_paged_many(const PagedAttnArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_paged_many_fp8(const PagedAttnArgs& a, hipStream_t stream) {
-  if (a.dtype) a.D == 128 ? launch_many<__bf16, E4m3, 128>(a, stream) : launch_many<__bf16, E4m3, 64>(a, stream);
-  else if (a.D == 128) launch_many<float, E4m3, 128>(a, stream);
+  if (a.D == 128) launch_many<__bf16, E4m3, 128>(a, stream);
+  else if (a.dtype) launch_many<__bf16, E4m3, 64>(a, stream);
   else paged_many_kernel<__bf16, E4m3, 64, true, 3><<<dim3(kPagedWorkers), dim3(kAttnBlock), 0, stream>>>(a);
   return hipGetLastError();
 }

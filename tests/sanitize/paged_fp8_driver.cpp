@@ -12,8 +12,11 @@ namespace sgdkv {
 hipError_t launch_paged_store_fp8(const StoreFp8Args&, hipStream_t) { return hipErrorNoDevice; }
 hipError_t launch_norm_rope_fp8(const NormRopeArgs&, hipStream_t) { return hipErrorNoDevice; }
 hipError_t launch_paged_attention_fp8(const PagedAttnArgs&, hipStream_t) { return hipErrorNoDevice; }
-PagedAttnShape paged_attn_fp8_shape(int dtype, int G, int max_new) {
-  return (int64_t)max_new * G <= 48 ? PagedAttnShape{48, 128} : PagedAttnShape{128, dtype ? 64 : 32};
+PagedAttnShape paged_attn_fp8_shape_64(int, int G, int max_new) {
+  return (int64_t)max_new * G <= 48 ? PagedAttnShape{48, 128} : PagedAttnShape{128, 64};
+}
+PagedAttnShape paged_attn_fp8_shape_128(int dtype, int G, int max_new) {
+  return (int64_t)max_new * G <= 48 || !dtype ? PagedAttnShape{48, 128} : PagedAttnShape{128, 64};
 }
 }  // namespace sgdkv
 
