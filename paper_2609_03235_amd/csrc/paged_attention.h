@@ -1,5 +1,5 @@
 // Attention of new tokens over a paged per-head KV cache (gfx950): shared by the instances for few query
-// rows (paged_few.hip) and for many (paged_many.hip).
+// rows (paged_few.hip, paged_few_fp8.hip for pools in 8 bits) and for many (paged_many.hip).
 //
 // Segment (b, h) holds the rows of KV head h of sequence b, the new tokens' own rows last. Token i of the n
 // new ones sees rows 0 .. rows - n + i; the G query heads of the group see the same rows, so the n * G query

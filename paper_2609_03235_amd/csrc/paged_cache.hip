@@ -8,8 +8,9 @@
 //                    entries, the slot of every new row
 //   paged_store      rows copied to their slots
 //   norm_rope_store  new tokens: norm and rotation per head, q to a dense tensor, k and v to their slots
+//   ..._fp8          the last two into a pool in 8 bits (fp8_rows.h)
 //
-// All three are bound by latency or by HBM. The pools may pass 4 GiB, so their rows are addressed with
+// All are bound by latency or by HBM. The pools may pass 4 GiB, so their rows are addressed with
 // 64-bit pointers; every slot is compared with the pool's size first.
 #include <algorithm>
 #include <type_traits>
@@ -529,9 +530,9 @@ __global__ __launch_bounds__(kPageBlock) void norm_rope_kernel(NormRopeArgs a) {
 
 // The same into an 8-bit pool: keys and values are rounded once, from what norm and rotation leave in fp32. The first
 // batch of rows comes while the wave works out its angles, the next one while one is worked on; batches are of one step
-// for bf16, where fewer registers and so more waves do more than more loads of each (6001 tokens of 80 heads 51 us, 4.6
-// TB/s; batches of two and four steps 56 and 54, with the loads behind the angles 59), and of four for fp32 (2500 tokens
-// 42 us, 47 with one).
+// for bf16, where fewer registers and so more waves do more than more loads of each (6001 tokens of 80 heads 51 us,
+// 4.6 TB/s; batches of two and four steps 56 and 54, with the loads behind the angles 59), and of four for fp32 (2500
+// tokens 42 us, 47 with one).
 template <typename T, int D>
 __global__ __launch_bounds__(kPageBlock) void norm_rope_fp8_kernel(NormRopeArgs a) {
   using P = RowPiece<T>;

@@ -124,9 +124,10 @@ struct ManyTile {
   bool own;        // not shared
 };
 
-// KV: the pool's rows, T or, for bf16 products, E4m3. QT: bf16 terms of a query; 3 of them hold an fp32 one, so that fp32 queries over an
-// 8-bit pool take bf16 products, three times as many at nine times the rate (3 x 300 tokens over 3000 rows of 64 columns
-// 33 us, 2048 over 8000 120; with fp32 products 49 and 307). There are registers for that where rows have 64 columns.
+// KV: the pool's rows, T or, for bf16 products, E4m3. QT: bf16 terms of a query; 3 of them hold an fp32 one, so that
+// fp32 queries over an 8-bit pool take bf16 products, three times as many at nine times the rate (3 x 300 tokens over
+// 3000 rows of 64 columns 33 us, 2048 over 8000 120; with fp32 products 49 and 307). There are registers for that where
+// rows have 64 columns.
 template <typename T, typename KV, int D, bool FINE, int QT = 1>
 __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs a) {
   using S = ManyShape<T, D>;
@@ -229,7 +230,8 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
     const rsrc_t qr = make_rsrc(
         static_cast<const char*>(a.q) + ((int64_t)(t.at.g.t0 + tok0) * a.Hq + t.at.seg % a.Hkv * a.G) * QRB,
         ((uint64_t)(ntok - 1) * a.Hq + a.G) * QRB);
-    uint32_t from = r < ntok * a.G ? (uint32_t)((tok * a.Hq + hd) * QRB + (QT == 1 ? 16 : 32) * half) : 0xFFFFF000u;  // or past the end
+    constexpr int kPiece = QT == 1 ? 16 : 32;  // bytes of a lane's eight columns (four, for fp32 products)
+    uint32_t from = r < ntok * a.G ? (uint32_t)((tok * a.Hq + hd) * QRB + kPiece * half) : 0xFFFFF000u;  // past the end
     asm("" : "+v"(from));  // one path for both: the compiler makes two of every load otherwise
     if constexpr (QT == 1) {
 #pragma unroll
@@ -379,8 +381,8 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs
             const u32x4 kf = key(n, c);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              y[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(q[0][c][e]), y[n], 0, 0,
-                                                          0);
+              y[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(q[0][c][e]), y[n], 0,
+                                                          0, 0);
           }
       }
       __builtin_amdgcn_s_setprio(0);
