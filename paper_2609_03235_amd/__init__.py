@@ -603,7 +603,7 @@ def norm_rope_store(q, k, v, positions, slots, k_pages, v_pages, *, inv_freq=Non
                               interleaved=interleaved, q_out=q_out))
     Hq = desc.num_q_heads
     if Hq and q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
     st = load_library().sgdkv_norm_rope_store(
         ctypes.byref(pool), ctypes.byref(desc), q.data_ptr() if Hq else None, k.data_ptr(), v.data_ptr(),
         positions.data_ptr(), slots.data_ptr(), None if inv_freq is None else inv_freq.data_ptr(),
@@ -656,8 +656,7 @@ def _attention_desc(q, tables, rows, cu_new, num_kv_heads, max_new, causal, scal
 def _attend(call, workspace_size, pool, desc, q, tables, rows, cu_new, with_lse, out, lse, workspace, handle):
     import torch
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.bfloat16 if desc.out_dtype == DTYPE_BF16 else torch.float32,
-                          device=q.device)
+        out = torch.empty_like(q, dtype=torch.bfloat16 if desc.out_dtype == DTYPE_BF16 else torch.float32)
     if with_lse and lse is None:
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
     if workspace is None:
@@ -754,7 +753,7 @@ def norm_rope_store_fp8(q, k, v, positions, slots, k_pages, v_pages, k_scales, v
                               interleaved=interleaved, rope_factor=rope_factor, q_out=q_out))
     Hq = desc.num_q_heads
     if Hq and q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
     st = load_library().sgdkv_norm_rope_store_fp8(
         ctypes.byref(pool), ctypes.byref(desc), rope_factor, q.data_ptr() if Hq else None, k.data_ptr(), v.data_ptr(),
         positions.data_ptr(), slots.data_ptr(), None if inv_freq is None else inv_freq.data_ptr(),
