@@ -658,7 +658,7 @@ def _attend(call, workspace_size, pool, desc, q, tables, rows, cu_new, with_lse,
     if out is None:
         out = torch.empty_like(q, dtype=torch.bfloat16 if desc.out_dtype == DTYPE_BF16 else torch.float32)
     if with_lse and lse is None:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        lse = q.new_empty(q.shape[:2], dtype=torch.float32)
     if workspace is None:
         size = workspace_size(q, desc.num_kv_heads, desc.batch, max_new=desc.max_new)
         workspace = alloc_workspace(size, q.device)
