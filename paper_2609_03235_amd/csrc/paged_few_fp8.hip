@@ -41,6 +41,14 @@ __device__ __forceinline__ rsrc_t rows_buffer(const void* p, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, bytes, kRsrcWord3);
 }
 
+// The same number, for the compiler a new one. What follows from a thread's number alone stays the same over all tiles,
+// and is kept for the next one in registers, some 20 of them, which the steps want (16 x 5 tokens over 25K rows 209 us,
+// 199 so); before and after the steps it is worked out again instead.
+__device__ __forceinline__ int anew(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // Eight columns of a query row from `off` on, as QT terms of bf16; `flip` holds the sign bits of a negative scale.
 template <int QT>
 __device__ __forceinline__ void query_terms(rsrc_t qr, uint32_t off, uint32_t flip, Frag<__bf16> (&to)[QT]) {
@@ -168,7 +176,7 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_fp8_kernel(PagedAttnA
         }
       }
       if constexpr (QLDS) {
-        for (int i = tid; i < 16 * NB * (D / 8); i += kAttnBlock) {
+        for (int i = anew(tid); i < 16 * NB * (D / 8); i += kAttnBlock) {
           const int r = i / (D / 8), c = i % (D / 8);
           Frag<__bf16> x[QT];
           query_terms<QT>(qr, query_off(r) + c * 8 * QEB, flip, x);
@@ -338,12 +346,13 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_fp8_kernel(PagedAttnA
       }
 #pragma unroll
       for (int qb = 0; qb < NB; ++qb) {
+        const int l = anew(lane);
         __syncthreads();
 #pragma unroll
         for (int d = 0; d < ND; ++d)
-          *reinterpret_cast<f32x4*>(stage + (lr * OP + 16 * d + 4 * lg) * 4) = o[qb][d];
+          *reinterpret_cast<f32x4*>(stage + (l % 16 * OP + 16 * d + 4 * (l / 16)) * 4) = o[qb][d];
         __syncthreads();
-        for (int idx = tid; idx < 16 * (D / 4); idx += kAttnBlock) {
+        for (int idx = anew(tid); idx < 16 * (D / 4); idx += kAttnBlock) {
           const int lrow = idx / (D / 4), r = 16 * qb + lrow, col = 4 * (idx % (D / 4));
           if (r >= nrow) break;
           float mm = -INFINITY;
