@@ -36,9 +36,6 @@ __device__ __forceinline__ u32x4 ld128(rsrc_t r, uint32_t byte_off) {
 __device__ __forceinline__ uint32_t ld32(rsrc_t r, uint32_t byte_off) {
   return __builtin_amdgcn_raw_buffer_load_b32(r, (int)byte_off, 0, 0);
 }
-__device__ __forceinline__ uint32_t ld8(rsrc_t r, uint32_t byte_off) {
-  return __builtin_amdgcn_raw_buffer_load_b8(r, (int)byte_off, 0, 0);
-}
 __device__ __forceinline__ float ldf(rsrc_t r, uint32_t byte_off) {
   return __uint_as_float(ld32(r, byte_off));
 }

@@ -22,6 +22,11 @@ constexpr int kMinRowExp = -110;
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
+// A code of a row, through a buffer.
+__device__ __forceinline__ uint32_t ld8(rsrc_t r, uint32_t byte_off) {
+  return __builtin_amdgcn_raw_buffer_load_b8(r, (int)byte_off, 0, 0);
+}
+
 // The power of two of a code; 255 becomes an infinity, which the conversions below take for NaN.
 __device__ __forceinline__ float power_of(uint32_t code) { return __uint_as_float(code << 23); }
 

@@ -63,6 +63,20 @@ def test_source_hash_ignores_comments_but_not_code(tmp_path, monkeypatch):
     assert bench.source_sha("gather") != base
 
 
+def test_committed_counters_belong_to_the_code():
+    """The HBM bytes that the default workload reports: a change to a header that its kernels are built from, be it an
+    addition that none of them uses, loses them without an error."""
+    bench.traffic_of(None, "qwen25_128k", 0.25, 64)
+    try:
+        with open(bench.traffic_path("qwen25_128k", 0.25, 64)) as fh:
+            kernels = json.load(fh)["kernels"]
+        assert {"score_lse", "score_colsum", "gather", "decode_split"} <= set(kernels)
+        for name, rec in kernels.items():
+            assert bench.traffic_of(name) == rec["hbm_bytes_per_launch"] > 0, name
+    finally:
+        bench._TRAFFIC.clear()
+
+
 def _csv(path, counter, rows):
     with open(path, "w") as fh:
         fh.write("Dispatch_Id,Kernel_Name,Counter_Name,Counter_Value\n")
