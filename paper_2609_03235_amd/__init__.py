@@ -656,7 +656,8 @@ def _attention_desc(q, tables, rows, cu_new, num_kv_heads, max_new, causal, scal
 def _attend(call, workspace_size, pool, desc, q, tables, rows, cu_new, with_lse, out, lse, workspace, handle):
     import torch
     if out is None:
-        out = torch.empty_like(q, dtype=torch.bfloat16 if desc.out_dtype == DTYPE_BF16 else torch.float32)
+        out = torch.empty_like(q, dtype=torch.bfloat16 if desc.out_dtype == DTYPE_BF16 else torch.float32,
+                               memory_format=torch.contiguous_format)
     if with_lse and lse is None:
         lse = q.new_empty(q.shape[:2], dtype=torch.float32)
     if workspace is None:

@@ -148,6 +148,21 @@ def test_binding_refuses_shapes_types_and_host_tensors():
         _refused(sg.page_pool_fp8, *pool, dtype)
 
 
+@pytest.mark.parametrize("out_dtype", [None, torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_results_are_dense_whatever_the_strides_of_one_token(dtype, out_dtype):
+    """One token cut from a wider projection is contiguous for torch with any stride between tokens; the results that
+    the attention calls allocate are not laid out after it."""
+    q = torch.zeros(1, 12, 64, dtype=dtype)[:, :4]
+    assert q.is_contiguous() and q.stride() == (768, 64, 1)
+    i32 = torch.zeros(4, dtype=torch.int32)
+    desc = sg._paged_desc(q, 2, 1, 1, 4, out_dtype, True, 0.0)
+    done = lambda *args: 0  # stands in for the library's call
+    out, lse = sg._attend(done, None, sg.PagePool(), desc, q, i32, i32, i32, True, None, None, i32, None)
+    assert out.shape == (1, 4, 64) and out.stride() == (256, 64, 1) and out.dtype is (out_dtype or dtype)
+    assert lse.shape == (1, 4) and lse.stride() == (4, 1) and lse.dtype is torch.float32
+
+
 # ------------------------------------------------------------------ sanitizers
 @pytest.mark.skipif(shutil.which("g++") is None or not os.path.exists("/opt/rocm/lib/libamdhip64.so"),
                     reason="needs g++ and the HIP host runtime")
