@@ -534,7 +534,13 @@ sgdkv_status sgdkv_paged_attention(const sgdkv_page_pool* pool, const sgdkv_page
  * is at most 448 2^e, and at least 2^-110 (a row of zeros has that one); a value
  * x becomes the e4m3 number nearest to x / 2^e, ties to even: off by 2^-4 of x
  * at most, or by 2^(e - 10) where that is more. An infinity or a NaN becomes
- * NaN and the others keep their values. */
+ * NaN and the others keep their values. Values of 1.9375 * 2^127 and more are
+ * nearest to 2^128, which is how they are held and which fp32 is not able to
+ * hold: reading such a value gives an infinity.
+ *
+ * So the stores here write codes 17 to 247. A pool filled elsewhere may have
+ * others: 255 makes its row NaN, values of 2^128 and more are infinite, and
+ * of codes below 17 see sgdkv_paged_attention_fp8. */
 typedef struct sgdkv_page_pool_fp8 {
   void* k_pages;      /* device [num_pages][page_size][head_dim] e4m3 */
   void* v_pages;      /* the same shape */
@@ -581,7 +587,11 @@ sgdkv_status sgdkv_paged_attention_fp8_workspace_size(const sgdkv_page_pool_fp8*
  * KV head (min(max_new, T) * Hq/Hkv) rounded to bf16. Sums are fp32, of
  * products up to 2^10 times a row's values. A value that is not finite makes
  * the outputs of its column, of the tokens that see its row, not finite, and no
- * others; a row of code 255 (e8m0's NaN) all columns'.
+ * others; a row of code 255 (e8m0's NaN) all columns'. (A value of 2^128 or
+ * more, whose product with a small probability may be finite again, may leave
+ * outputs finite.) Of rows with codes below 17, far below what the stores
+ * write, each adds an error of up to 2^-125 to an output, and of codes below 3
+ * numbers are rounded to multiples of 2^-133.
  * Errors (nothing enqueued): those of sgdkv_paged_attention. */
 sgdkv_status sgdkv_paged_attention_fp8(const sgdkv_page_pool_fp8* pool, const sgdkv_paged_desc* desc, const void* q,
                                        const int32_t* tables, const int32_t* rows, const int32_t* cu_new, void* out,

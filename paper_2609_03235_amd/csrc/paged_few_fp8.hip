@@ -239,10 +239,10 @@ __global__ __launch_bounds__(kAttnBlock, 2) void paged_few_fp8_kernel(PagedAttnA
         Frag<__bf16> k[U][NC];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const float kpow = power_of(kcode[u]);
+          const float kscale = conversion_scale(kcode[u]);
 #pragma unroll
           for (int c = 0; c < NC; ++c)
-            k[u][c] = widen_piece(raw[u][c / 2][2 * (c % 2)], raw[u][c / 2][2 * (c % 2) + 1], kpow);
+            k[u][c] = widen_piece(raw[u][c / 2][2 * (c % 2)], raw[u][c / 2][2 * (c % 2) + 1], kscale);
 #pragma unroll
           for (int i = 0; i < 4; ++i) vpow[u][i] = power_of(vcode[u] >> 8 * i & 0xFF);
 #pragma unroll

@@ -108,11 +108,11 @@ struct ByteRows {
   __device__ __forceinline__ void store(int i, char* to, int my_row, int lane, F swizzle) const {
     const int r = my_row + i * RPL + lane / VPR, c = lane % VPR, sw = swizzle(r);
     char* row = to + r * S::RB;
-    const float p = power_of(code[i]);
+    const float scale = conversion_scale(code[i]);
 #pragma unroll
     for (int e = 0; e < 2; ++e)
       *reinterpret_cast<u32x4*>(row + ((2 * c + e) ^ sw) * 16) =
-          widen_piece(raw[i][2 * e], raw[i][2 * e + 1], p).v;
+          widen_piece(raw[i][2 * e], raw[i][2 * e + 1], scale).v;
   }
 };
 

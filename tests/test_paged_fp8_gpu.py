@@ -333,6 +333,69 @@ def test_paged_attention_fp8_powers(new, low, high):
     c.check(out, lse)
 
 
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("G,n", [(1, 1), (8, 3), (8, 5), (1, 64), (8, 9)])
+def test_paged_attention_fp8_of_one_row_of_every_code(dtype, d, G, n):
+    """Segments of one row, with the codes 0 to 247, the keys' counted down: the last of a segment's n tokens sees the
+    row, the ones before see nothing. Queries of zeros give it the probability 1 exactly, and the fp32 output is the
+    row's values, bit for bit: numbers of 2^-6 to 240 are multiples of 2^-6, so that values are multiples of 2^-133,
+    which bf16 holds, and below 2^128. Queries that undo their key's power give logits of ordinary size, of one product
+    each: the log-sum-exp is off by a few fp32 roundings, 2^-21 of 1 and itself, and the output by 2^-21 of itself and
+    2^-125."""
+    _say(f"every code {dtype} d {d}, {G} heads, {n} tokens")
+    g = torch.Generator(device=DEV).manual_seed(d + n)
+    codes = torch.arange(248, device=DEV)
+    bits = lambda: (torch.randint(4 << 3, 15 << 3, (248, d), generator=g, device=DEV)
+                    | torch.randint(0, 2, (248, d), generator=g, device=DEV) << 7).to(U8)
+    pool = pool_of(248, 16, d)  # segment s has page s; the bytes behind its row are no numbers
+    key_codes = (247 - codes).clamp(min=3)
+    pool[0].view(U8)[:, 0], pool[2].view(U8)[:, 0] = bits(), key_codes.to(U8)
+    pool[1].view(U8)[:, 0], pool[3].view(U8)[:, 0] = bits(), codes.to(U8)
+    k, v = decoded(pool[0][:, 0], pool[2][:, 0]), decoded(pool[1][:, 0], pool[3][:, 0])
+    # two segments to a sequence; head i of a group looks at column 5 i + 1
+    q = torch.zeros(124, n, 2, G, d, device=DEV)
+    cols = (5 * torch.arange(G, device=DEV) + 1) % d
+    undo = torch.exp2(127 - key_codes.double()).float()
+    q[:, :, :, torch.arange(G, device=DEV), cols] = undo.view(124, 1, 2, 1).expand(124, n, 2, G)
+    tables = codes.to(torch.int32)[:, None].contiguous()
+    v = v.view(124, 2, 1, d).expand(124, 2, G, d)
+    for x in (torch.zeros_like(q), q):
+        out, lse = sg.paged_attention_fp8(x.view(124 * n, 2 * G, d).to(dtype), *pool, tables, _i32([1] * 248),
+                                          _i32([i * n for i in range(125)]), 2, max_new=n, out_dtype=F32)
+        out, lse = out.view(124, n, 2, G, d), lse.view(124, n, 2, G)
+        assert (out[:, :-1] == 0).all() and (lse[:, :-1] == -math.inf).all()
+        if x is q:
+            want = (k[:, cols].view(124, 2, G) * undo.double().view(124, 2, 1)) / math.sqrt(d)
+            assert ((lse[:, -1].double() - want).abs() <= 2.0 ** -21 * (1 + want.abs())).all()
+            assert ((out[:, -1].double() - v).abs() <= 2.0 ** -21 * v.abs() + 2.0 ** -125).all()
+        else:
+            assert (lse[:, -1] == 0).all() and torch.equal(out[:, -1].double(), v)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("n", [1, 64])
+def test_paged_attention_fp8_of_the_largest_values(dtype, d, n):
+    """Rows stored from the type's largest numbers: below 1.9375 * 2^127 they come back as the numbers that they were
+    rounded to, from there on as infinities, each in its own column alone."""
+    _say(f"largest values {dtype} d {d}, {n} tokens")
+    border = 1.9375 * 2.0 ** 127
+    v = torch.full((1, d), 3.0e38, device=DEV, dtype=F32)  # 225.7 * 2^120: held as 224
+    v[0, 3], v[0, 4], v[0, 9] = border, -border, torch.finfo(dtype).max
+    v[0, 7] = 1.9296875 * 2.0 ** 127  # 247 * 2^120, a number of bf16: held as 240
+    v[0, 8] = -1.0
+    v = v.to(dtype)
+    pool = pool_of(1, 16, d)
+    sg.paged_store_fp8(torch.zeros_like(v), v, _i32([0]), *pool)
+    q = torch.zeros(n, 1, d, device=DEV, dtype=dtype)
+    out, lse = sg.paged_attention_fp8(q, *pool, _i32([[0]]), _i32([1]), _i32([0, n]), 1, max_new=n, out_dtype=F32)
+    want = torch.full((d,), 224 * 2.0 ** 120, device=DEV, dtype=torch.float64)
+    want[7], want[8] = 240 * 2.0 ** 120, -0.0
+    want[3], want[4], want[9] = math.inf, -math.inf, math.inf
+    fine = torch.isfinite(want)
+    assert torch.equal(out[-1, 0].double()[fine], want[fine]) and not torch.isfinite(out[-1, 0][~fine]).any()
+    assert lse[-1, 0] == 0
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("new", [[1, 1], [20, 70]])
 def test_paged_attention_fp8_scale_and_bounds(dtype, new):
