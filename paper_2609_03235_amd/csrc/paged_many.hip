@@ -539,6 +539,9 @@ hipError_t launch_paged_many(const PagedAttnArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_paged_many_fp8(const PagedAttnArgs& a, hipStream_t stream) {
+  // No instance has fp32 queries of 128 columns (paged_attn_fp8_shape_128 gives them tiles of few rows): the one below
+  // would read their bytes as bf16.
+  if (a.D == 128 && !a.dtype) return hipErrorInvalidValue;
   if (a.D == 128) launch_many<__bf16, E4m3, 128>(a, stream);
   else if (a.dtype) launch_many<__bf16, E4m3, 64>(a, stream);
   else paged_many_kernel<__bf16, E4m3, 64, true, 3><<<dim3(kPagedWorkers), dim3(kAttnBlock), 0, stream>>>(a);

@@ -163,6 +163,22 @@ def test_results_are_dense_whatever_the_strides_of_one_token(dtype, out_dtype):
     assert lse.shape == (1, 4) and lse.stride() == (4, 1) and lse.dtype is torch.float32
 
 
+# ------------------------------------------------------------------ the launchers
+@pytest.mark.skipif(shutil.which("g++") is None or not os.path.exists("/opt/rocm/lib/libamdhip64.so"),
+                    reason="needs g++ and the HIP host runtime")
+@pytest.mark.skipif(_gpu(), reason="host-only run")
+def test_the_launcher_of_many_rows_refuses_queries_it_has_no_instance_for(tmp_path):
+    sg.load_library()
+    package = os.path.dirname(sg.__file__)
+    exe = str(tmp_path / "paged_fp8_launch")
+    subprocess.run(["g++", "-std=c++17", "-D__HIP_PLATFORM_AMD__", "-isystem", "/opt/rocm/include", "-I",
+                    os.path.join(package, "csrc"), os.path.join(ROOT, "tests", "sanitize", "paged_fp8_launch.cpp"), "-o",
+                    exe, "-L" + package, "-l:libsgdkv.so", "-Wl,-rpath," + package, "-L/opt/rocm/lib",
+                    "-Wl,-rpath,/opt/rocm/lib", "-lamdhip64"], check=True)
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and r.stdout == "REFUSED\n", r.stdout + r.stderr
+
+
 # ------------------------------------------------------------------ sanitizers
 @pytest.mark.skipif(shutil.which("g++") is None or not os.path.exists("/opt/rocm/lib/libamdhip64.so"),
                     reason="needs g++ and the HIP host runtime")
