@@ -429,6 +429,65 @@ __global__ __launch_bounds__(kPageBlock) void store_fp8_kernel(StoreFp8Args a) {
     }
 }
 
+// What a lane does to its 16 bytes of every head of one token, for pools of either kind: norm and rotation in 32 bits.
+template <typename T, int D>
+struct HeadColumns {
+  using P = RowPiece<T>;
+  static constexpr int N = P::N, LPR = D / N;
+  float cs[N], sn[N], qw[N], kw[N];  // y = x * c + partner * s, with the sign of the first of a pair in s; weights
+  int partner;                       // the lane that holds the columns' partners
+  bool turns;
+
+  // Of the sines and cosines of the token's angles.
+  __device__ __forceinline__ HeadColumns(const NormRopeArgs& a, int lane, const float* sines, const float* cosines) {
+    const int col = (lane % LPR) * N, half = a.rot / 2;
+    const bool first = a.interleaved || col < half;
+    turns = col < a.rot;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const int pair = a.interleaved ? (col + e) / 2 : (first ? col + e : col + e - half);
+      const bool neg = a.interleaved ? (e & 1) == 0 : first;
+      cs[e] = turns ? cosines[pair] : 1.f;
+      sn[e] = turns ? (neg ? -sines[pair] : sines[pair]) : 0.f;
+      qw[e] = kw[e] = 1.f;
+    }
+    if (a.q_weight) P::widen(reinterpret_cast<const u32x4*>(a.q_weight)[lane % LPR], qw);
+    if (a.k_weight) P::widen(reinterpret_cast<const u32x4*>(a.k_weight)[lane % LPR], kw);
+    partner = a.interleaved || !turns ? lane : (first ? lane + half / N : lane - half / N);
+  }
+
+  // A query's, a key's or (neither) a value's columns; the lanes of a row take the same branches.
+  __device__ __forceinline__ void norm_and_turn(const NormRopeArgs& a, float (&x)[N], bool is_q, bool is_k) const {
+    if (is_q ? a.q_weight != nullptr : is_k && a.k_weight != nullptr) {
+      float ss = 0.f;
+#pragma unroll
+      for (int e = 0; e < N; ++e) ss = fmaf(x[e], x[e], ss);
+      ss = row_sum<LPR>(ss);
+      const float r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float of_q = qw[e], of_k = kw[e];  // chosen as values: a choice of arrays would keep both in memory
+        x[e] = x[e] * r * (is_q ? of_q : of_k);
+      }
+    }
+    if (a.rot) {
+      float p[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) p[e] = a.interleaved ? x[e ^ 1] : __shfl(x[e], partner, 64);
+      if (turns && (is_q || is_k)) {  // columns that do not turn: nothing times zero, which may be infinite
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = fmaf(p[e], sn[e], x[e] * cs[e]);
+      }
+    }
+  }
+};
+
+// The token's angles, one a lane, to LDS.
+__device__ __forceinline__ void token_angles(const NormRopeArgs& a, int64_t token, int lane, double factor,
+                                             float* sines, float* cosines) {
+  if (lane < a.rot / 2) sincos_at(a.positions[token], a.inv_freq[lane], factor, sines[lane], cosines[lane]);
+}
+
 // A wave takes one token (or 1/parts of its heads): LPR lanes hold a head's row, 16 bytes each, so 64/LPR
 // heads go at once. Lane l computes the token's angle l; the sines and cosines go through LDS once and stay
 // in registers, where every head uses them. Sum of squares, norm and rotation are in 32 bits, rounded once
@@ -445,30 +504,11 @@ __global__ __launch_bounds__(kPageBlock) void norm_rope_kernel(NormRopeArgs a) {
   const int64_t token = unit / a.parts;
   const int part = (int)(unit - token * a.parts);
   const bool live = token < a.T;
-  const int col = (lane % LPR) * N, half = a.rot / 2;
 
-  if (live && lane < half) {
-    float s, c;
-    sincos_at(a.positions[token], a.inv_freq[lane], 1.0, s, c);
-    sines[wid][lane] = s;
-    cosines[wid][lane] = c;
-  }
+  if (live) token_angles(a, token, lane, 1.0, sines[wid], cosines[wid]);
   __syncthreads();
   if (!live) return;
-  // this lane's columns: y = x * c + partner * s, with the sign of the first of a pair in s
-  const bool turns = col < a.rot, first = a.interleaved || col < half;
-  float cs[N], sn[N], qw[N], kw[N];
-#pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const int pair = a.interleaved ? (col + e) / 2 : (first ? col + e : col + e - half);
-    const bool neg = a.interleaved ? (e & 1) == 0 : first;
-    cs[e] = turns ? cosines[wid][pair] : 1.f;
-    sn[e] = turns ? (neg ? -sines[wid][pair] : sines[wid][pair]) : 0.f;
-    qw[e] = kw[e] = 1.f;
-  }
-  if (a.q_weight) P::widen(reinterpret_cast<const u32x4*>(a.q_weight)[lane % LPR], qw);
-  if (a.k_weight) P::widen(reinterpret_cast<const u32x4*>(a.k_weight)[lane % LPR], kw);
-  const int partner = a.interleaved || !turns ? lane : (first ? lane + half / N : lane - half / N);
+  const HeadColumns<T, D> mine(a, lane, sines[wid], cosines[wid]);
 
   const int heads = a.Hq + 2 * a.Hkv;
   const char* qrow = static_cast<const char*>(a.q) + token * a.q_stride + (int64_t)(lane % LPR) * 16;
@@ -498,25 +538,7 @@ __global__ __launch_bounds__(kPageBlock) void norm_rope_kernel(NormRopeArgs a) {
       u32x4 y = w[u];
       float x[N];
       P::widen(y, x);
-      if (is_q ? a.q_weight != nullptr : is_k && a.k_weight != nullptr) {
-        // every lane of a row takes this branch together
-        float ss = 0.f;
-#pragma unroll
-        for (int e = 0; e < N; ++e) ss = fmaf(x[e], x[e], ss);
-        ss = row_sum<LPR>(ss);
-        const float r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = x[e] * r * (is_q ? qw[e] : kw[e]);
-      }
-      if (a.rot) {
-        float p[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e) p[e] = a.interleaved ? x[e ^ 1] : __shfl(x[e], partner, 64);
-        if (turns && (is_q || is_k)) {  // columns that do not turn: nothing times zero, which may be infinite
-#pragma unroll
-          for (int e = 0; e < N; ++e) x[e] = fmaf(p[e], sn[e], x[e] * cs[e]);
-        }
-      }
+      mine.norm_and_turn(a, x, is_q, is_k);
       if (is_q || is_k) y = P::narrow(x);
       if (is_q) {
         __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(a.q_out) + (token * a.Hq + h) * LPR + lane % LPR);
@@ -544,7 +566,6 @@ __global__ __launch_bounds__(kPageBlock) void norm_rope_fp8_kernel(NormRopeArgs 
   const int64_t token = unit / (uint32_t)a.parts;
   const int part = (int)(unit - (uint32_t)token * a.parts);
   const bool live = token < a.T;
-  const int col = l * N, half = a.rot / 2;
   const int heads = a.Hq + 2 * a.Hkv, step = a.parts * HPW;
   const int64_t tok = live ? token : 0;
   const char* const rows[3] = {static_cast<const char*>(a.q) + tok * a.q_stride + l * 16,
@@ -563,28 +584,10 @@ __global__ __launch_bounds__(kPageBlock) void norm_rope_fp8_kernel(NormRopeArgs 
     }
   };
   fetch(part * HPW);
-  if (live && lane < half) {
-    float s, c;
-    sincos_at(a.positions[token], a.inv_freq[lane], a.factor, s, c);
-    sines[wid][lane] = s;
-    cosines[wid][lane] = c;
-  }
+  if (live) token_angles(a, token, lane, a.factor, sines[wid], cosines[wid]);
   __syncthreads();
   if (!live) return;
-  // this lane's columns: y = x * c + partner * s, with the sign of the first of a pair in s
-  const bool turns = col < a.rot, first = a.interleaved || col < half;
-  float cs[N], sn[N], qw[N], kw[N];
-#pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const int pair = a.interleaved ? (col + e) / 2 : (first ? col + e : col + e - half);
-    const bool neg = a.interleaved ? (e & 1) == 0 : first;
-    cs[e] = turns ? cosines[wid][pair] : 1.f;
-    sn[e] = turns ? (neg ? -sines[wid][pair] : sines[wid][pair]) : 0.f;
-    qw[e] = kw[e] = 1.f;
-  }
-  if (a.q_weight) P::widen(reinterpret_cast<const u32x4*>(a.q_weight)[l], qw);
-  if (a.k_weight) P::widen(reinterpret_cast<const u32x4*>(a.k_weight)[l], kw);
-  const int partner = a.interleaved || !turns ? lane : (first ? lane + half / N : lane - half / N);
+  const HeadColumns<T, D> mine(a, lane, sines[wid], cosines[wid]);
 
   for (int h0 = part * HPW; h0 < heads; h0 += kAhead * step) {
     u32x4 now[kAhead];
@@ -603,32 +606,14 @@ __global__ __launch_bounds__(kPageBlock) void norm_rope_fp8_kernel(NormRopeArgs 
       const int64_t to_slot = h >= a.Hq && h < heads ? to_slots[u] : -1;
       float x[N];
       P::widen(now[u], x);
-      if (is_q ? a.q_weight != nullptr : is_k && a.k_weight != nullptr) {
-        // every lane of a row takes this branch together
-        float ss = 0.f;
-#pragma unroll
-        for (int e = 0; e < N; ++e) ss = fmaf(x[e], x[e], ss);
-        ss = row_sum<LPR>(ss);
-        const float r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = x[e] * r * (is_q ? qw[e] : kw[e]);
-      }
-      if (a.rot) {
-        float p[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e) p[e] = a.interleaved ? x[e ^ 1] : __shfl(x[e], partner, 64);
-        if (turns && (is_q || is_k)) {  // columns that do not turn: nothing times zero, which may be infinite
-#pragma unroll
-          for (int e = 0; e < N; ++e) x[e] = fmaf(p[e], sn[e], x[e] * cs[e]);
-        }
-      }
+      mine.norm_and_turn(a, x, is_q, is_k);
       if (is_q)
         __builtin_nontemporal_store(P::narrow(x), reinterpret_cast<u32x4*>(a.q_out) + (token * a.Hq + h) * LPR + l);
       if (g0 + HPW <= a.Hq) continue;  // queries alone
       uint32_t b[N / 4];
       const int code = bytes_of_row<LPR, N>(x, b);  // of every lane's row: they go together
       if (to_slot < 0 || to_slot >= a.total_slots) continue;
-      uint8_t* to = static_cast<uint8_t*>(is_k ? a.k_pages : a.v_pages) + to_slot * D + col;
+      uint8_t* to = static_cast<uint8_t*>(is_k ? a.k_pages : a.v_pages) + to_slot * D + l * N;
       if constexpr (N == 8) *reinterpret_cast<u32x2*>(to) = u32x2{b[0], b[1]};
       else *reinterpret_cast<uint32_t*>(to) = b[0];
       if (l == 0) (is_k ? a.k_scales : a.v_scales)[to_slot] = (uint8_t)code;
