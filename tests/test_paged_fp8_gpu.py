@@ -481,6 +481,60 @@ def test_paged_attention_fp8_rows_to_come(hq, new, rows, dtype):
         c.pool = [p.clone() for p in saved]
 
 
+@pytest.mark.parametrize("hq,new,rows,dtype", ODD_CASES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("what", ["key", "key code", "value code"])
+def test_paged_attention_fp8_nan_rows_within_a_segment(hq, new, rows, dtype, d, what):
+    """A NaN key in the first or the last column, or a code of 255, among the rows that all tokens see and on the row
+    of the last but one, in two segments: every instance, both types of output. Tokens and heads that do not see them
+    come out as ever; keys that are NaN reach the log-sum-exp too, values do not."""
+    _say(f"NaN rows: {what} {dtype} {new} over {rows} d {d}")
+    c = Case8(new, rows, hq, 2, d, 16, dtype, seed=23)
+    G, t0 = hq // 2, new[0]
+    for od in (BF, F32):
+        clean, clean_lse = c.call(out_dtype=od)
+        saved = [p.clone() for p in c.pool]
+        odd = torch.zeros(c.T, c.hq, dtype=torch.bool, device=DEV)
+        for s, row, col in ((0, rows[0] - 2, 0), (3, (rows[3] - new[1]) // 2, d - 1)):
+            slot = int(c.slots(s)[row])
+            if what == "key":
+                c.pool[0].view(U8).view(-1, d)[slot, col] = 0xFF
+            else:
+                c.pool[2 if what == "key code" else 3].view(U8).view(-1)[slot] = 255
+            b, h = divmod(s, 2)
+            first, n = t0 * b, new[b]
+            sees = torch.arange(n, device=DEV) >= row - (rows[s] - n)
+            odd[first:first + n, h * G:(h + 1) * G] |= sees[:, None]
+        assert odd.any() and not odd.all()
+        out, lse = c.call(out_dtype=od)
+        c.check(torch.where(odd[..., None], clean, out), torch.where(odd, clean_lse, lse))
+        assert not torch.isfinite(out[odd]).any()
+        if what == "value code":
+            assert torch.equal(lse, clean_lse)
+        else:
+            assert not torch.isfinite(lse[odd]).any()
+        c.pool = saved
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("hq,new", [(2, [1]), (8, [5]), (8, [11]), (8, [40])])
+@pytest.mark.parametrize("low,high", [(-112, -100), (-100, -60), (60, 90), (-40, 40)])
+def test_paged_attention_fp8_spread_powers(hq, new, dtype, d, low, high):
+    """Values whose rows' powers lie far from 1, and far from each other, in tiles of one, two and three blocks and of
+    many rows, for both types of output. (Rows no smaller than the stores write: at 2^-110 the probabilities' last bits
+    are bf16's smallest subnormals.)"""
+    _say(f"spread powers {dtype} d {d} {new} {low} to {high}")
+    c = Case8(new, [900, 77], hq, 2, d, 16, dtype, seed=3)
+    g = torch.Generator(device=DEV).manual_seed(low + 300)
+    for s in range(2):
+        n = c.rows_host[s]
+        e = torch.randint(low, high, (n, 1), generator=g, device=DEV)
+        c.put(s, 1, torch.randn(n, d, generator=g, device=DEV).double() * torch.exp2(e.double()))
+    for od in (BF, F32):
+        out, lse = c.call(out_dtype=od)
+        c.check(out, lse)
+
+
 def test_paged_attention_fp8_cuts_lengths_to_the_buffers():
     _say("cut lengths")
     c = Case8([5], [64, 64], 4, 2, 64, 16, BF, seed=8)
