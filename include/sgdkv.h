@@ -510,7 +510,9 @@ sgdkv_status sgdkv_paged_attention_workspace_size(const sgdkv_page_pool* pool, c
  * Probabilities are rounded to bf16 for bf16 out of bf16 inputs with more than
  * 48 query rows per KV head (min(max_new, T) * Hq/Hkv) and keep their fp32 bits
  * otherwise. A value that is not finite makes the outputs of its
- * column, of the tokens that see its row, not finite, and no others.
+ * column, of the tokens that see its row, not finite, and no others. Logits
+ * (scale*<q, k_r>) are to be below 2^30 in size: from there on fp32's steps
+ * are so wide that exponentials may overflow.
  * Errors (nothing enqueued): a bad pool; sizes out of range; Hq % Hkv; more
  * than 16 query heads per KV head, 8192 query heads or 65535 segments
  * (UNSUPPORTED); missing or misaligned pointers; small workspace (WORKSPACE). */

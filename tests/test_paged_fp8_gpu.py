@@ -318,6 +318,44 @@ def test_paged_attention_fp8_far_logits(new, spread, dtype):
         c.check(out, lse)
 
 
+@pytest.mark.parametrize("n", [1, 5, 64])
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_attention_of_logits_up_to_2_to_30(sign, dtype, d, n):
+    """The largest logits that the contract takes, about 2^30 and -2^30, in pools of either kind. Two rows far from each
+    other share the largest one, the others are smaller by 2^26 at least: the output is the mean of the two rows'
+    values. The exponentials' arguments are off from what they would be by half a step of fp32 at such logits, up to
+    2^6, but all by the same, so that the weights are 1/2 each, and the rest is a few roundings, 2^-21 of the values'
+    sizes (fp32 output keeps the probabilities' bits)."""
+    _say(f"large logits {sign} {dtype} d {d}, {n} tokens")
+    L, page = 9000, 16
+    g = torch.Generator(device=DEV).manual_seed(n + d)
+    k, v = torch.zeros(L, d, device=DEV), torch.randn(L, d, generator=g, device=DEV).bfloat16().float()
+    numbers = torch.tensor([1.0, 1.25, 1.5, 1.625, 1.75], device=DEV)  # of e4m3 and of bf16
+    k[:, 3] = numbers[torch.randint(0, 5, (L,), generator=g, device=DEV)] - (3.0 if sign < 0 else 0.0)
+    two = [77, 8001]
+    k[two, 3] = 1.875 if sign > 0 else -1.0
+    q = torch.zeros(n, 8, d, device=DEV)
+    q[:, :, 3] = 2.0 ** 29
+    pages = L // page + 1
+    tables = torch.randperm(pages, generator=g, device=DEV).to(torch.int32)[None]
+    at = torch.arange(L, device=DEV)
+    slots = (tables[0].long()[at // page] * page + at % page).to(torch.int32)
+    pool8 = pool_of(pages, page, d)
+    pool = [torch.zeros(pages, page, d, device=DEV, dtype=dtype) for _ in range(2)]
+    sg.paged_store(k.to(dtype), v.to(dtype), slots, *pool)
+    sg.paged_store_fp8(k.to(dtype), v.to(dtype), slots, *pool8)
+    _, (bits, codes) = rows_of(pool8, slots, d)
+    held = decoded(bits, codes)
+    for call, p, values in ((sg.paged_attention, pool, v.double()), (sg.paged_attention_fp8, pool8, held)):
+        out, lse = call(q.to(dtype), *p, tables, _i32([L]), _i32([0, n]), 1, max_new=n, causal=False, scale=1.0,
+                        out_dtype=F32)
+        want, size = values[two].mean(0), values[two].abs().sum(0)
+        assert ((out.double() - want).abs() <= 2.0 ** -21 * size).all()
+        top = float(k[two[0], 3]) * 2.0 ** 29
+        assert ((lse.double() - top).abs() <= 2.0 ** -21 * abs(top)).all()
+
+
 @pytest.mark.parametrize("new", [[1], [3], [40]])
 @pytest.mark.parametrize("low,high", [(-124, -112), (-100, -70), (60, 90), (-40, 40)])
 def test_paged_attention_fp8_powers(new, low, high):
