@@ -8,8 +8,9 @@
 // without, since a lane has a column of eight rows, whose powers go to the probabilities. The products are bf16 ones
 // for fp32 queries too, which go in as three bf16 terms that hold all 24 bits: a third of the bf16 rate is still three
 // times fp32's. (The matrix instructions that take e4m3 as it is keep 13 bits of a sum of products of different sizes.)
-// 40 x 1 tokens over 4 x 30K rows, 28 / 4 heads of 128, bf16, take 200 us and 5 for the merge, 6.2 TB/s; 16 x 2, 4 and
-// 6 tokens over 8 x 25K rows, 64 / 8 heads, fp32 output, 151, 184 and 231, of which the loads alone 142 to 158.
+// 40 x 1 tokens over 4 x 30K rows, 28 / 4 heads of 128, bf16, take 200 us and 5 for the merge, 6.2 TB/s; calls of 16 x
+// 2, 4 and 6 tokens over 8 x 25K rows, 64 / 8 heads, fp32 output, 149 to 154, 184 to 187 and 222 to 223, of which the
+// loads alone 142 to 158.
 #include <type_traits>
 
 #include "paged_attention.h"
@@ -71,7 +72,7 @@ __device__ __forceinline__ void query_terms(rsrc_t qr, uint32_t off, uint32_t fl
 
 // QT: terms of a query (1: bf16, 3: fp32). QB: 16-row query blocks of a full tile. FINE: the
 // probabilities go in as three bf16 terms, all their bits; for bf16 output of bf16 queries as two, off by 2^-16 of each
-// (16 x 6 tokens over 25K rows, 64 / 8 heads, 225 us and 205).
+// (16 x 6 tokens over 25K rows, 64 / 8 heads, 222 to 223 us and 202 to 205).
 // A wave's step is U 16-row groups, 2 or UMAX of them: with 4, twice the bytes are under way (40 x 1 tokens over 30K
 // rows 222 us, 206 so), and a worker with no more than one key tile has all its waves at work with 2 (1 token over 9K
 // rows 15.6 us, 17.2 with 4).
@@ -430,8 +431,8 @@ void launch_few_rows(const PagedAttnArgs& a, hipStream_t stream) {
 
 // More rows than a tile of few holds: tiles of 128 (paged_many.hip) but for fp32 queries of 128 columns, whose three
 // terms have no room beside 128 rows' other registers: those take several tiles of few rows. (16 x 16 tokens over 25K
-// rows, 64 / 8 heads, 670 us, 2048 over 8000, 28 / 4, 830, 3 x 50 over 1000, 4 / 2, 28; with tiles of 128 and fp32
-// products 1575, 1967 and 37.)
+// rows, 64 / 8 heads, 672 to 681 us, 2048 over 8000, 28 / 4, 825 to 838, 3 x 50 over 1000, 4 / 2, 28; with tiles of
+// 128 and fp32 products 1575, 1967 and 37.)
 PagedAttnShape paged_attn_fp8_shape_64(int, int G, int max_new) {
   const int64_t rows = (int64_t)max_new * G;
   if (rows <= kFewRows) return {16 * (int)((rows + 15) / 16), kKeyTile};

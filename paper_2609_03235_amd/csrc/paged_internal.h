@@ -1,5 +1,6 @@
-// Internal interface between the C-ABI layer of the paged cache (paged_host.cpp) and its HIP
-// kernels (paged_cache.hip, paged_few.hip, paged_many.hip). Not installed; not part of the ABI.
+// Internal interface between the C-ABI layer of the paged cache (paged_host.cpp, paged_fp8_host.cpp) and
+// its HIP kernels (paged_cache.hip, paged_few.hip, paged_few_fp8.hip, paged_many.hip). Not installed; not
+// part of the ABI.
 #pragma once
 
 #include <hip/hip_runtime.h>

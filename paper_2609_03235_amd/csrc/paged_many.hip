@@ -23,7 +23,7 @@ namespace {
 // Rows in LDS have no padding (a load writes its lanes' 16 bytes one after the other); the 16-byte pieces of a
 // row change places instead, piece c of row r lying at place c ^ key_swizzle(r) (value_swizzle): reads of one
 // piece of 16 rows, or of four pieces of four rows, touch every bank once.
-// T: the type of the queries, of the products and of the rows in LDS.
+// T: the type of the products and of the rows in LDS, and of the queries but for those that are taken as several terms.
 template <typename T, int D>
 struct ManyShape {
   static constexpr int EB = sizeof(T), RB = D * EB;
@@ -50,8 +50,11 @@ constexpr int kUnshared = sizeof(T) == 2 ? 512 : 128;
 constexpr float kFar = 1024.f;
 
 // A tile's probabilities of one lane, as the operand of the product with the values. bf16 output of bf16 inputs:
-// rounded to bf16, each off by up to 2^-8 of itself. The keys' errors average out: 1 x 1999 tokens over 8K rows, 28 / 4
-// heads, are off by 2.00e-3 of the output (rms), of which its own rounding to bf16 makes 1.66e-3. FINE (fp32 output)
+// rounded to bf16, each off by up to 2^-8 of itself. The keys' errors average out as their values do: 1 x 1999 tokens
+// over 8K rows, 28 / 4 heads, are off by 2.00e-3 of the output (rms), of which its own rounding to bf16 makes 1.66e-3;
+// 1 x 1501 over 10K and 2 x 6000 over 20K rows of 8 bits by 2.2e-3. Where values average to nothing but what chance
+// leaves, output and error shrink alike, and the error is as large as the output's rounding: 2.35e-3 with it, the most
+// that random values come to. FINE (fp32 output)
 // keeps all 24 bits in three terms, 6.6e-7, at three times these products: 445 us for 268, and 18.0 ms for 10.5 with
 // two sequences of 8192 tokens over 16K rows, 64 / 8 heads. A caller who wants them asks for fp32 output.
 template <typename T, bool FINE, int NK>
@@ -125,9 +128,11 @@ struct ManyTile {
 };
 
 // KV: the pool's rows, T or, for bf16 products, E4m3. QT: bf16 terms of a query; 3 of them hold an fp32 one, so that
-// fp32 queries over an 8-bit pool take bf16 products, three times as many at nine times the rate (3 x 300 tokens over
-// 3000 rows of 64 columns 33 us, 2048 over 8000 120; with fp32 products 49 and 307). There are registers for that where
-// rows have 64 columns.
+// fp32 queries over an 8-bit pool take bf16 products, three times as many at nine times the rate (2048 tokens over 8000
+// rows of 64 columns, 8 / 8 heads, 111 to 120 us; with fp32 products 307). There are registers for that where rows have
+// 64 columns.
+// The E4m3 instances of 128 columns and of three terms take all 256 registers and keep 2 of them (8 for fp32 output) in
+// scratch, 12 (36) bytes a lane, each read back once.
 template <typename T, typename KV, int D, bool FINE, int QT = 1>
 __global__ __launch_bounds__(kAttnBlock, 2) void paged_many_kernel(PagedAttnArgs a) {
   using S = ManyShape<T, D>;
